@@ -482,6 +482,148 @@ spider_status spider_prefill_online_ablation(const spider_decoder_cfg* cfg,
                                              size_t workspace_bytes, spider_stream stream);
 
 /* ------------------------------------------------------------------------
+ * Drafting over the cache.  A tree of drafted tokens (nodes) per sample is
+ * scored in one step: node t's key and value stand in slot lens[b] + t of the
+ * cache, behind the lens[b] slots of the context.  A tree mask says which
+ * nodes each node sees: uint64 [B][T][W], W = ceil(T / 64); node t of sample b
+ * sees node u if bit u % 64 of word u / 64 of row (b, t) is set.  NULL stands
+ * for a chain (u <= t).  Bits at u >= T are ignored, and so are those of nodes
+ * that are not alive: with n_nodes (device int32 [B], or NULL: all T) sample b
+ * has n_nodes[b] live nodes, the first ones.
+ *
+ * spider_tree_mask - the mask and the depths of trees given by their parents.
+ * Host only.  parents HOST int32 [B][T]: an earlier node, -1 (child of the
+ * context) or -2 (absent; the absent nodes come last).  A node sees its
+ * ancestors and itself, an absent one nothing.  mask_out HOST [B][T][W];
+ * depth_out HOST int32 [B][T] or NULL: 0 for a child of the context and for an
+ * absent node, one more per generation.  Limit: T <= 256.
+ * ------------------------------------------------------------------------ */
+spider_status spider_tree_mask(int B, int T, const int32_t* parents, uint64_t* mask_out, int32_t* depth_out);
+
+/* ------------------------------------------------------------------------
+ * spider_tree_attention - attention of the nodes over the cache, for grouped
+ * heads (query head h reads kv head h / (H / Hkv)); T = 1 is the attention of
+ * one decode step.  For every live node t, head h and its kv head:
+ *   s(j)  = scale * q[b,t,h] . k[b,j]   over the slots j that the node sees:
+ *           j < lens[b], and j = lens[b] + u of the live nodes u of its mask
+ *   out   = sum_j softmax(s)(j) v[b,j]      (0 where it sees no slot)
+ * Slots that a node does not see do not enter its sums, whatever they hold.
+ * q element (b,t,h,c) at q[b*q_stride_b + t*q_stride_t + h*dh + c]; k and v
+ * element (b,slot,head,c) at [b*kv_stride_b + slot*kv_stride_s +
+ * head*kv_stride_h + c] (the decoder's cache of one layer: kv_stride_b = cap*d,
+ * kv_stride_s = d, kv_stride_h = dh), cap slots; out [B][T][H][dh] contiguous
+ * in q's dtype.  lens: device int32 [B].  lens[b] is taken into [0, cap], the
+ * nodes past cap are not alive.  Rows of nodes that are not alive are left as
+ * they were.
+ * With weights_out (device fp32 [B][Hkv][cap], or NULL), the weight that every
+ * slot receives is added up over the live nodes and the heads of a group:
+ *   weights_out[b,hk,j] = (j < lens[b] ? weights_in[b,hk,j] : 0)
+ *                         + sum over live t, h of group hk of softmax(s)(j)
+ * for j < lens[b] + live nodes; later slots are left as they were.  weights_in
+ * (the same layout) may be NULL (zeros) or weights_out itself.
+ * Precision: products exact, sums, maxima and exponentials fp32; bf16: the
+ * softmax numerators enter the product with v as bf16 high and low parts (16
+ * significant bits), out is rounded once.
+ * Requires H % Hkv == 0, T <= 256, dh <= 256, dh and the strides multiples of
+ * 16 bytes, q, k, v, out 16-byte aligned; out overlaps no input.  Workspace:
+ * spider_tree_attention_workspace_size(...) bytes (weights != 0: with
+ * weights_out), 256-byte aligned.
+ * ------------------------------------------------------------------------ */
+size_t spider_tree_attention_workspace_size(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype dtype,
+                                            int weights);
+
+spider_status spider_tree_attention(int B, int T, int H, int Hkv, int dh, const void* q, int64_t q_stride_b,
+                                    int64_t q_stride_t, const void* k, const void* v, int64_t kv_stride_b,
+                                    int64_t kv_stride_s, int64_t kv_stride_h, int cap, const int32_t* lens,
+                                    const int32_t* n_nodes, const uint64_t* tree_mask, spider_dtype dtype,
+                                    float scale, void* out, const float* weights_in, float* weights_out,
+                                    void* workspace, size_t workspace_bytes, spider_stream stream);
+
+/* ------------------------------------------------------------------------
+ * spider_cache_select - the slots a cache keeps, by accumulated attention
+ * weight.  For every layer l, sample b and head group (each kv head its own
+ * choice, or with shared = 1 one for all of them, on the weights added over
+ * the heads in fp64 and rounded to fp32), of the n = lens[b] filled slots (taken
+ * into [0, cap]):
+ *   n <= keep: all of them;
+ *   else keep slots: the first n_first and the last n_last, and of the others
+ *   those with the largest weights, ties to the lower slot (-0.0 == +0.0; NaN
+ *   counts as -inf).
+ * weights device fp32 [L][B][Hkv][cap]; idx_out device int32
+ * [L][B][shared ? 1 : Hkv][keep]: the kept slots ascending, then -1; len_out
+ * device int32 [B] = min(n, keep).  Requires n_first + n_last <= keep <= cap.
+ * No workspace.
+ * ------------------------------------------------------------------------ */
+spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* weights, const int32_t* lens,
+                                  int keep, int n_first, int n_last, int shared, int32_t* idx_out,
+                                  int32_t* len_out, spider_stream stream);
+
+/* ------------------------------------------------------------------------
+ * spider_cache_compact - moves the chosen slots of a cache to the front, or
+ * into another cache: for every l, b, head and i < count[b]
+ *   slot base[b] + i of the output = slot base[b] + idx[l,b,head,i] of the input
+ * in keys, values and, if given, weights (fp32 [L][B][Hkv][cap_in], cap_out).
+ * Entries with idx < 0, or with either slot outside its cache, move nothing.
+ * idx device int32 [idx_layers][B][idx_heads][n_max], idx_layers 1 (the same
+ * for all layers) or L, idx_heads 1 or Hkv; count device int32 [B] or NULL
+ * (n_max each; taken into [0, n_max]); base device int32 [B] or NULL (0).  So
+ * eviction takes spider_cache_select's idx and len, and the accepted nodes of
+ * a tree move behind their context with base = lens, idx = their node numbers.
+ * Strides: HOST [4], elements of (layer, sample, slot, head); channels
+ * contiguous.  In place (k_out == k_in, v_out == v_in, the weights alike, equal
+ * strides and capacities) idx must ascend strictly within a row (so idx[i] >=
+ * i); a row that does not ends with unspecified contents in its own slots.
+ * Otherwise input and output must not overlap.  Slots that nothing is moved
+ * to are left as they were.
+ * Requires dh <= 256, dh and the strides multiples of 16 bytes, caches 16-byte
+ * aligned, L * B * Hkv <= 65535.  No workspace.
+ * ------------------------------------------------------------------------ */
+spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spider_dtype dtype, const void* k_in,
+                                   const void* v_in, const int64_t in_strides[4], int cap_in, void* k_out,
+                                   void* v_out, const int64_t out_strides[4], int cap_out, const int32_t* idx,
+                                   int idx_layers, int idx_heads, int n_max, const int32_t* count,
+                                   const int32_t* base, const float* weights_in, float* weights_out,
+                                   spider_stream stream);
+
+/* ------------------------------------------------------------------------
+ * spider_adjust_logits - a sampler's rules on the logits of B samples of T
+ * nodes (T = 1: a decode step), then the arg max.  For row r = b*T + t of a
+ * live node and token v:
+ *   said  = occurrences of v in history[b][i], n_prompt[b] <= i < n_history[b],
+ *           plus, with node_tokens ([B][T]), among the nodes that t sees by
+ *           tree_mask (its ancestors and itself; NULL: the chain)
+ *   seen  = said > 0, or v occurs in history[b][i], i < n_prompt[b]
+ *   x = logits[r][v];  if seen: x = x > 0 ? x / repetition[b] : x * repetition[b]
+ *   if said: x = (x - frequency[b] * said) - presence[b]
+ *   x = x + (the bias entries of v, added from 0 in list order), if n_bias > 0
+ *   x = -inf if bit v % 32 of mask word v / 32 of the row is clear
+ *   out[r][v] = x;  next_out[r] = arg max (ties to the lowest id; NaN is never
+ *   chosen; -1 if no x is above -inf)
+ * every operation rounded to fp32 once.  logits fp32 or bf16, row stride
+ * logits_stride; out fp32 (or NULL), row stride out_stride, may be logits itself
+ * (fp32, equal strides); next_out int32 [B*T] or NULL (not both NULL).
+ * history int32, row stride history_stride (n_history[b] is taken into [0,
+ * history_stride]), or NULL; n_prompt [B] or NULL (0: all of the history counts
+ * as said); repetition (> 0), frequency, presence fp32 [B] or NULL (1, 0, 0);
+ * bias_ids int32 and bias fp32 [B][n_bias]; mask uint32 rows of stride
+ * mask_stride words (0: one row for all) or NULL.  All on the device.  Ids
+ * outside [0, V) anywhere are ignored.  Rows of nodes that are not alive are left
+ * as they were in out and next_out.
+ * Limits: T <= 256, B*T <= 65535, V <= 2^28, n_bias <= 65536.  Workspace:
+ * spider_adjust_logits_workspace_size(B, T, V) bytes, 256-byte aligned (none
+ * without next_out).
+ * ------------------------------------------------------------------------ */
+size_t spider_adjust_logits_workspace_size(int B, int T, int V);
+
+spider_status spider_adjust_logits(
+    int B, int T, int V, const void* logits, int64_t logits_stride, spider_dtype dtype, const int32_t* history,
+    int64_t history_stride, const int32_t* n_history, const int32_t* n_prompt, const int32_t* n_nodes,
+    const int32_t* node_tokens, const uint64_t* tree_mask, const float* repetition, const float* frequency,
+    const float* presence, const int32_t* bias_ids, const float* bias, int n_bias, const uint32_t* mask,
+    int64_t mask_stride, float* out, int64_t out_stride, int32_t* next_out, void* workspace, size_t workspace_bytes,
+    spider_stream stream);
+
+/* ------------------------------------------------------------------------
  * Kernel-class profiler (process-global, not thread-safe; for benchmarks).
  * When enabled, every launch of the library records a pair of HIP events on
  * its stream.  spider_profile_read() synchronises on the recorded events and

@@ -79,6 +79,16 @@ _SIGS = {
     "spider_decode_workspace_size": ([ctypes.POINTER(DecoderCfg), _I, _I, _I], _SZ),
     "spider_decode_step": ([ctypes.POINTER(DecoderCfg), ctypes.POINTER(LayerWeights), _I, _VP, _VP,
                             ctypes.POINTER(KVCache), _VP, _VP, _I, _VP, _VP, _VP, _VP, _SZ, _VP], _I),
+    "spider_tree_mask": ([_I, _I, _VP, _VP, _VP], _I),
+    "spider_tree_attention_workspace_size": ([_I, _I, _I, _I, _I, _I, _I, _I], _SZ),
+    "spider_tree_attention": ([_I, _I, _I, _I, _I, _VP, _I64, _I64, _VP, _VP, _I64, _I64, _I64, _I, _VP, _VP, _VP, _I,
+                               _F, _VP, _VP, _VP, _VP, _SZ, _VP], _I),
+    "spider_cache_select": ([_I, _I, _I, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP], _I),
+    "spider_cache_compact": ([_I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _VP, _VP, _I, _VP, _I, _I, _I, _VP, _VP,
+                              _VP, _VP, _VP], _I),
+    "spider_adjust_logits_workspace_size": ([_I, _I, _I], _SZ),
+    "spider_adjust_logits": ([_I, _I, _I, _VP, _I64, _I, _VP, _I64, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
+                              _I, _VP, _I64, _VP, _I64, _VP, _VP, _SZ, _VP], _I),
     "spider_profile_enable": ([_I], _I),
     "spider_profile_mask": ([ctypes.c_uint32], _I),
     "spider_profile_classes": ([], _I),
@@ -446,6 +456,199 @@ def decode_step(cfg: DecoderCfg, weights, lens, x: torch.Tensor, kv: dict, final
                                     _ptr(final_norm), _ptr(w_unembed), V, _ptr(h), _ptr(logits), _ptr(nxt),
                                     _aligned(workspace), wsz, _stream(dev)))
     return h, logits, nxt
+
+
+# ----------------------------------------------------------------- drafting over the cache
+def _on(dev, fn, *args):
+    """Calls fn(*args, stream) on torch's current stream of ``dev``, with ``dev`` current."""
+    if dev.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+
+
+def _need(t: Optional[torch.Tensor], name: str, dtype, shape, dev):
+    """Device pointer (None for None) of a contiguous tensor of that dtype and shape on dev."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def tree_mask(parents):
+    """parents [B, T] ints (an earlier node, -1 = child of the context, -2 = absent) ->
+    (mask [B, T, W] int64, depth [B, T] int32), NumPy arrays for the host."""
+    p = np.ascontiguousarray(parents, dtype=np.int32)
+    if p.ndim != 2:
+        raise ValueError("parents must be [B, T]")
+    B, T = p.shape
+    mask = np.zeros((B, T, (T + 63) // 64), np.int64)
+    depth = np.zeros((B, T), np.int32)
+    _check(lib().spider_tree_mask(B, T, p.ctypes.data, mask.ctypes.data, depth.ctypes.data))
+    return mask, depth
+
+
+def tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, *,
+                   n_nodes: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                   weights_in: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the drafted nodes q [B, T, H, dh] over a cache k, v [B, cap, Hkv, dh]
+    (views of any layout whose channels are contiguous; a cache of one layer of kv_cache()
+    is kv["k"][l].view(B, cap, H, dh)) whose first lens[b] slots are the context and the
+    next ones the nodes.  tree_mask [B, T, W] int64 (None: a chain), n_nodes [B] int32.
+    ``scale`` defaults to dh ** -0.5.  With weights_out [B, Hkv, cap] fp32 the attention
+    weight of every slot goes there, added to weights_in for the context."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q must be [B, T, H, dh], k and v [B, cap, Hkv, dh]")
+    B, T, H, dh = q.shape
+    cap, Hkv = k.shape[1], k.shape[2]
+    dev = q.device
+    if k.shape[0] != B or k.shape[3] != dh or v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("k and v must be [B, cap, Hkv, dh] alike, with the B and dh of q")
+    if k.dtype != q.dtype or v.dtype != q.dtype or k.device != dev or v.device != dev:
+        raise ValueError("q, k and v must share dtype and device")
+    if q.stride(3) != 1 or (H > 1 and q.stride(2) != dh) or k.stride(3) != 1:
+        raise ValueError("channels must be contiguous, and the heads of a row of q side by side")
+    if out is None:
+        out = torch.empty(B, T, H, dh, dtype=q.dtype, device=dev)
+    dt = _dt(q)
+    L = lib()
+    weighted = weights_out is not None
+    wsz = L.spider_tree_attention_workspace_size(B, T, H, Hkv, dh, cap, dt, weighted)
+    if workspace is None:
+        workspace = _ws(wsz, dev)
+    elif workspace.device != dev or workspace.numel() * workspace.element_size() < wsz + 256:
+        raise ValueError(f"workspace must hold {wsz + 256} bytes on {dev}")
+    _on(dev, L.spider_tree_attention, B, T, H, Hkv, dh, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(),
+        v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), cap, _need(lens, "lens", torch.int32, (B,), dev),
+        _need(n_nodes, "n_nodes", torch.int32, (B,), dev),
+        _need(tree_mask, "tree_mask", torch.int64, (B, T, (T + 63) // 64), dev), dt,
+        dh ** -0.5 if scale is None else scale, _need(out, "out", q.dtype, (B, T, H, dh), dev),
+        _need(weights_in, "weights_in", torch.float32, (B, Hkv, cap), dev),
+        _need(weights_out, "weights_out", torch.float32, (B, Hkv, cap), dev), _aligned(workspace), wsz)
+    return out
+
+
+def cache_select(weights: torch.Tensor, lens: torch.Tensor, keep: int, *, n_first: int = 0, n_last: int = 0,
+                 shared: bool = False):
+    """The slots to keep by accumulated weight: weights [L, B, Hkv, cap] fp32, lens [B] int32
+    -> (idx [L, B, 1 if shared else Hkv, keep] int32 ascending then -1, new lens [B] int32)."""
+    if weights.dim() != 4:
+        raise ValueError("weights must be [L, B, Hkv, cap]")
+    L_, B, Hkv, cap = weights.shape
+    dev = weights.device
+    if keep < 1:
+        raise ValueError("keep must be at least 1")
+    idx = torch.empty(L_, B, 1 if shared else Hkv, keep, dtype=torch.int32, device=dev)
+    new = torch.empty(B, dtype=torch.int32, device=dev)
+    _on(dev, lib().spider_cache_select, L_, B, Hkv, cap,
+        _need(weights, "weights", torch.float32, (L_, B, Hkv, cap), dev), _need(lens, "lens", torch.int32, (B,), dev),
+        keep, n_first, n_last, int(bool(shared)), idx.data_ptr(), new.data_ptr())
+    return idx, new
+
+
+def cache_compact(k: torch.Tensor, v: torch.Tensor, idx: torch.Tensor, count: Optional[torch.Tensor] = None, *,
+                  base: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                  v_out: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+                  weights_out: Optional[torch.Tensor] = None):
+    """Moves slot base[b] + idx[l, b, h, i] of k and v [L, B, cap, Hkv, dh] (views of any
+    layout whose channels are contiguous) to slot base[b] + i for i < count[b], in place or
+    into k_out and v_out; idx [1 or L, B, 1 or Hkv, n] int32.  ``weights`` [L, B, Hkv, cap]
+    fp32 move alike (in place, or into weights_out)."""
+    if k.dim() != 5 or idx.dim() != 4:
+        raise ValueError("k and v must be [L, B, cap, Hkv, dh], idx [1 or L, B, 1 or Hkv, n]")
+    if (k_out is None) != (v_out is None) or (weights_out is not None and (weights is None or k_out is None)):
+        raise ValueError("k_out and v_out go together, and weights_out with them and weights")
+    k_out, v_out = (k, v) if k_out is None else (k_out, v_out)
+    L_, B, cap, Hkv, dh = k.shape
+    cap_out = k_out.shape[2] if k_out.dim() == 5 else -1
+    dev = k.device
+    if k_out.shape != (L_, B, cap_out, Hkv, dh) or v.shape != k.shape or v_out.shape != k_out.shape:
+        raise ValueError("the caches must be [L, B, cap, Hkv, dh] alike but for cap")
+    if v.stride() != k.stride() or v_out.stride() != k_out.stride() or k.stride(4) != 1 or k_out.stride(4) != 1:
+        raise ValueError("keys and values must share their strides, with contiguous channels")
+    if any(t.dtype != k.dtype or t.device != dev for t in (v, k_out, v_out)):
+        raise ValueError("the caches must share dtype and device")
+    if idx.shape[1] != B:
+        raise ValueError("idx must be [1 or L, B, 1 or Hkv, n]")
+    if weights is not None and weights_out is None:
+        if k_out is not k:
+            raise ValueError("weights_out is needed where the cache goes elsewhere")
+        weights_out = weights
+    si = (ctypes.c_int64 * 4)(*k.stride()[:4])
+    so = (ctypes.c_int64 * 4)(*k_out.stride()[:4])
+    _on(dev, lib().spider_cache_compact, L_, B, Hkv, dh, _dt(k), k.data_ptr(), v.data_ptr(), si, cap,
+        k_out.data_ptr(), v_out.data_ptr(), so, cap_out, _need(idx, "idx", torch.int32, tuple(idx.shape), dev),
+        idx.shape[0], idx.shape[2], idx.shape[3], _need(count, "count", torch.int32, (B,), dev),
+        _need(base, "base", torch.int32, (B,), dev), _need(weights, "weights", torch.float32, (L_, B, Hkv, cap), dev),
+        _need(weights_out, "weights_out", torch.float32, (L_, B, Hkv, cap_out), dev))
+    return k_out, v_out
+
+
+def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
+                  n_history: Optional[torch.Tensor] = None, *, n_prompt: Optional[torch.Tensor] = None,
+                  n_nodes: Optional[torch.Tensor] = None, node_tokens: Optional[torch.Tensor] = None,
+                  tree_mask: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                  frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                  bias_ids: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                  mask: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  next_ids: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Penalties, biases and grammar masks on logits [B, T, V] (or [B, V]), and the arg max.
+    history [B, n] int32 with n_history [B] filled and n_prompt [B] of them the prompt;
+    node_tokens [B, T] int32 and tree_mask [B, T, W] int64 for drafted nodes; repetition,
+    frequency, presence [B] fp32; bias_ids int32 and bias fp32 [B, n_bias]; mask int32 bits
+    [B, T, W32], [B, W32] with T = 1, or [W32] for all rows, W32 = ceil(V / 32).
+    Returns (out fp32 like logits, next ids int32 [B, T] or [B])."""
+    flat = logits.dim() == 2
+    x = logits.unsqueeze(1) if flat else logits
+    if x.dim() != 3 or x.stride(2) != 1 or (min(x.shape[:2]) > 1 and x.stride(0) != x.shape[1] * x.stride(1)):
+        raise ValueError("logits must be [B, T, V] or [B, V] with contiguous rows at one distance")
+    B, T, V = x.shape
+    dev = logits.device
+    row = x.stride(1) if T > 1 or B == 1 else x.stride(0)
+    row = max(row, V) if B * T == 1 else row
+    lead = (B,) if flat else (B, T)
+    if out is None:
+        out = torch.empty(lead + (V,), dtype=torch.float32, device=dev)
+    inplace = out.data_ptr() == logits.data_ptr()
+    if inplace and (out.dtype != logits.dtype or out.shape != logits.shape or out.stride() != logits.stride()):
+        raise ValueError("in place, out must be logits")
+    if next_ids is None:
+        next_ids = torch.empty(lead, dtype=torch.int32, device=dev)
+    if history is not None and (history.dim() != 2 or n_history is None):
+        raise ValueError("history must be [B, n] and needs n_history")
+    n = history.shape[1] if history is not None else 0
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("bias_ids and bias go together")
+    nb = bias_ids.shape[1] if bias_ids is not None else 0
+    words = (V + 31) // 32
+    ms = 0
+    if mask is not None and mask.dim() > 1:
+        ms = words
+        mask = mask.unsqueeze(1) if flat and mask.dim() == 2 else mask
+    L = lib()
+    wsz = L.spider_adjust_logits_workspace_size(B, T, V)
+    if workspace is None:
+        workspace = _ws(wsz, dev)
+    elif workspace.device != dev or workspace.numel() * workspace.element_size() < wsz + 256:
+        raise ValueError(f"workspace must hold {wsz + 256} bytes on {dev}")
+    i32, f32 = torch.int32, torch.float32
+    _on(dev, L.spider_adjust_logits, B, T, V, logits.data_ptr(), row, _dt(logits),
+        _need(history, "history", i32, (B, n), dev), n, _need(n_history, "n_history", i32, (B,), dev),
+        _need(n_prompt, "n_prompt", i32, (B,), dev), _need(n_nodes, "n_nodes", i32, (B,), dev),
+        _need(node_tokens, "node_tokens", i32, (B, T), dev),
+        _need(tree_mask, "tree_mask", torch.int64, (B, T, (T + 63) // 64), dev),
+        _need(repetition, "repetition", f32, (B,), dev), _need(frequency, "frequency", f32, (B,), dev),
+        _need(presence, "presence", f32, (B,), dev), _need(bias_ids, "bias_ids", i32, (B, nb), dev),
+        _need(bias, "bias", f32, (B, nb), dev), nb,
+        _need(mask, "mask", i32, (B, T, words) if ms else (words,), dev), ms,
+        logits.data_ptr() if inplace else _need(out, "out", f32, lead + (V,), dev), row if inplace else V,
+        _need(next_ids, "next_ids", i32, lead, dev), _aligned(workspace), wsz)
+    return out, next_ids
 
 
 # ----------------------------------------------------------------- profiler

@@ -69,6 +69,11 @@ enum KernelClass {
   KC_CLS_ATTN,
   KC_PROJECTOR,
   KC_LM_HEAD,
+  KC_TREE_ATTN,
+  KC_TREE_WEIGHTS,
+  KC_CACHE_SELECT,
+  KC_CACHE_COMPACT,
+  KC_ADJUST_LOGITS,
   KC_COUNT
 };
 

@@ -71,7 +71,8 @@ const char* kClassNames[KC_COUNT] = {
     "score_prep", "anchor_topk", "kmeans",   "anchor_maxsim", "score_final",
     "select",     "assemble",    "embed",    "rmsnorm",       "gemm_qkv",
     "qkv_finalize", "attention", "gemm_o",   "gemm_gateup",   "gemm_down",
-    "residual_add", "lens_prep", "gemm_lens", "lens_admit", "anchor_colmean", "cls_attention", "projector", "lm_head"};
+    "residual_add", "lens_prep", "gemm_lens", "lens_admit", "anchor_colmean", "cls_attention", "projector", "lm_head",
+    "tree_attention", "tree_weights", "cache_select", "cache_compact", "adjust_logits"};
 }  // namespace
 
 void prof_begin(int cls, hipStream_t s) {
@@ -228,6 +229,35 @@ spider_status spider_plan_skips(int L, int n_vis, const float* s_sa, int s_sa_st
     }
   if (admit_out)
     for (int i = 0; i < n_vis; ++i) admit_out[i] = admit[i];
+  return SPIDER_OK;
+}
+
+spider_status spider_tree_mask(int B, int T, const int32_t* parents, uint64_t* mask_out, int32_t* depth_out) {
+  clear_error();
+  SPIDER_REQUIRE(parents && mask_out, SPIDER_ERR_INVALID_ARG, "spider_tree_mask: null pointer");
+  SPIDER_REQUIRE(B >= 1 && T >= 1, SPIDER_ERR_INVALID_ARG, "spider_tree_mask: B and T must be >= 1");
+  SPIDER_REQUIRE(T <= 256, SPIDER_ERR_UNSUPPORTED, "spider_tree_mask: T = %d exceeds 256", T);
+  for (int b = 0; b < B; ++b) {
+    bool ended = false;
+    for (int t = 0; t < T; ++t) {
+      const int p = parents[(size_t)b * T + t];
+      SPIDER_REQUIRE(p >= -2 && p < t, SPIDER_ERR_INVALID_ARG,
+                     "spider_tree_mask: parent %d of node %d (sample %d) is not an earlier node, -1 or -2", p, t, b);
+      SPIDER_REQUIRE(p == -2 || !ended, SPIDER_ERR_INVALID_ARG,
+                     "spider_tree_mask: node %d (sample %d) comes after an absent one", t, b);
+      ended = p == -2;
+    }
+  }
+  const int W = (T + 63) / 64;
+  for (int b = 0; b < B; ++b)
+    for (int t = 0; t < T; ++t) {
+      const size_t r = (size_t)b * T + t;
+      const int p = parents[r];
+      uint64_t* row = mask_out + r * W;
+      for (int w = 0; w < W; ++w) row[w] = p >= 0 ? mask_out[((size_t)b * T + p) * W + w] : 0;
+      if (p >= -1) row[t >> 6] |= 1ull << (t & 63);
+      if (depth_out) depth_out[r] = p >= 0 ? depth_out[(size_t)b * T + p] + 1 : 0;
+    }
   return SPIDER_OK;
 }
 
