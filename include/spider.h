@@ -524,8 +524,9 @@ spider_status spider_tree_mask(int B, int T, const int32_t* parents, uint64_t* m
  * Precision: products exact, sums, maxima and exponentials fp32; bf16: the
  * softmax numerators enter the product with v as bf16 high and low parts (16
  * significant bits), out is rounded once.
- * Requires H % Hkv == 0, T <= 256, dh <= 256, dh and the strides multiples of
- * 16 bytes, q, k, v, out 16-byte aligned; out overlaps no input.  Workspace:
+ * Requires H % Hkv == 0, T <= 256, dh <= 256, B and H <= 65535, B*H*T and
+ * B*Hkv*ceil(cap/64) below 2^24, dh and the strides multiples of 16 bytes, q, k,
+ * v, out 16-byte aligned; out overlaps no input.  Workspace:
  * spider_tree_attention_workspace_size(...) bytes (weights != 0: with
  * weights_out), 256-byte aligned.
  * ------------------------------------------------------------------------ */

@@ -4,12 +4,16 @@
 //   s(r, j) = scale q_r . k_j,  o_r = sum_j softmax_j(s(r, .)) v_j
 // over the slots j that row r = (node t, head h) sees: the context j < lens[b]
 // and the nodes u = j - lens[b] whose bit is set in the node's mask.
+#include <algorithm>
 #include <cmath>
 
 #include "kernels.h"
 
 namespace spider {
 namespace {
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 
 constexpr int kTreeMaxNodes = 256;
 constexpr int kTreeMaxDh = 256;
@@ -25,11 +29,14 @@ struct TreeArgs {
   const uint64_t* mask;
   const float* w_in;
   float* w_out;
-  float2* stat;  // [B][T][H] (largest score, 1 / sum of exponentials)
+  float2* stat;     // [B][T][H] (largest score in powers of two, 1 / sum of exponentials), with w_out
+  float2* part_ml;  // [B][Hkv][T * G][splits] (largest raw score, sum) of a split
+  float* part_o;    // .. [dh] its unscaled output
   int64_t qb, qt;         // strides of q, elements
   int64_t kvb, kvs, kvh;  // strides of k and v
   int B, T, H, Hkv, dh, cap;
   float scale;
+  int groups, splits, min_tiles;  // of the launch, see TreePlan
 };
 
 // The filled slots and live nodes of sample b, clamped to the cache.
@@ -39,124 +46,653 @@ __device__ __forceinline__ int2 tree_extent(const TreeArgs& a, int b) {
   return make_int2(len, min(nn, a.cap - len));
 }
 
-// Whether node t of sample b sees node u.
-__device__ __forceinline__ bool tree_sees(const TreeArgs& a, int b, int t, int u) {
-  if (!a.mask) return u <= t;
-  const int W = (a.T + 63) / 64;
-  return (a.mask[((int64_t)b * a.T + t) * W + (u >> 6)] >> (u & 63)) & 1;
-}
-
+// Four outputs x / l (0 where the row saw nothing) at element i, a multiple of 4.
 template <typename AT>
-__device__ __forceinline__ float tree_load(const void* p, int64_t i) {
-  if constexpr (sizeof(AT) == 4) return reinterpret_cast<const float*>(p)[i];
-  else return bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(p)[i]);
-}
-
-template <typename AT>
-__device__ __forceinline__ float tree_dot(const TreeArgs& a, const float* qs, int64_t kp) {
-  float s = 0.f;
-  for (int c = 0; c < a.dh; ++c) s = fmaf(qs[c], tree_load<AT>(a.k, kp + c), s);
-  return s * a.scale;
-}
-
-// One block per (node, head, sample): the keys in pieces of 256, a thread per key
-// for the scores and per channel for the values, with the running maximum and sum.
-template <typename AT>
-__global__ void __launch_bounds__(256) tree_rows_kernel(TreeArgs a) {
-  __shared__ float qs[kTreeMaxDh];
-  __shared__ float p[256];
-  __shared__ float red[4];
-  const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H, b = blockIdx.y;
-  const int hk = h / (a.H / a.Hkv);
-  const int tid = threadIdx.x, wave = tid >> 6;
-  const int2 ext = tree_extent(a, b);
-  if (t >= ext.y) return;
-  const int n = ext.x + ext.y;
-  const int64_t qp = b * a.qb + t * a.qt + (int64_t)h * a.dh;
-  const int64_t kv = b * a.kvb + hk * a.kvh;
-  if (tid < a.dh) qs[tid] = tree_load<AT>(a.q, qp + tid);
-  __syncthreads();
-  float top = -INFINITY, sum = 0.f, o = 0.f;
-  for (int j0 = 0; j0 < n; j0 += 256) {
-    const int j = j0 + tid;
-    const bool sees = j < n && (j < ext.x || tree_sees(a, b, t, j - ext.x));
-    const float s = sees ? tree_dot<AT>(a, qs, kv + j * a.kvs) : -INFINITY;
-    const float wm = wave_max(s);
-    if ((tid & 63) == 0) red[wave] = wm;
-    __syncthreads();
-    const float m = fmaxf(top, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    const float ms = m == -INFINITY ? 0.f : m;
-    const float e = sees ? expf(s - ms) : 0.f;
-    p[tid] = sees ? e : -1.f;  // -1: not seen, its value is not read
-    __syncthreads();
-    const float ws = wave_sum(e);
-    if ((tid & 63) == 0) red[wave] = ws;
-    __syncthreads();
-    const float f = top == -INFINITY ? 0.f : expf(top - ms);
-    sum = sum * f + ((red[0] + red[1]) + (red[2] + red[3]));
-    o *= f;
-    top = m;
-    if (tid < a.dh)
-      for (int i = 0; i < min(256, n - j0); ++i)
-        if (p[i] != -1.f) o = fmaf(p[i], tree_load<AT>(a.v, kv + (j0 + i) * a.kvs + tid), o);
-    __syncthreads();
+__device__ __forceinline__ void tree_store(void* out, int64_t i, floatx4 x, float l) {
+  const float f = l == 0.f ? 0.f : 1.f / l;
+  x *= f;
+  if constexpr (sizeof(AT) == 4) {
+    *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(out) + i) = x;
+  } else {
+    const uint32_t w0 = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{x[0], x[1]}, bf16x2v));
+    const uint32_t w1 = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{x[2], x[3]}, bf16x2v));
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + i) = make_uint2(w0, w1);
   }
-  const int64_t row = ((int64_t)b * a.T + t) * a.H + h;
-  if (tid < a.dh) {
-    const float x = sum == 0.f ? 0.f : o / sum;
-    if constexpr (sizeof(AT) == 4) reinterpret_cast<float*>(a.out)[row * a.dh + tid] = x;
-    else reinterpret_cast<uint16_t*>(a.out)[row * a.dh + tid] = f32_to_bf16_bits(x);
-  }
-  if (tid == 0 && a.stat) a.stat[row] = make_float2(top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum);
 }
 
-// A thread per (slot, kv head, sample): the weight that all live rows of the head
-// group give the slot, from the rows' final maximum and sum.
-template <typename AT>
-__global__ void __launch_bounds__(256) tree_weights_kernel(TreeArgs a) {
-  const int j = blockIdx.x * 256 + threadIdx.x, hk = blockIdx.y, b = blockIdx.z;
-  const int2 ext = tree_extent(a, b);
-  if (j >= ext.x + ext.y) return;
-  const int G = a.H / a.Hkv;
-  const int64_t kp = b * a.kvb + hk * a.kvh + j * a.kvs;
-  const int64_t w = ((int64_t)b * a.Hkv + hk) * a.cap + j;
-  float sum = 0.f;
-  for (int t = 0; t < ext.y; ++t) {
-    if (j >= ext.x && !tree_sees(a, b, t, j - ext.x)) continue;
-    for (int g = 0; g < G; ++g) {
-      const int h = hk * G + g;
-      const int64_t qp = b * a.qb + t * a.qt + (int64_t)h * a.dh;
-      float s = 0.f;
-      for (int c = 0; c < a.dh; ++c) s = fmaf(tree_load<AT>(a.q, qp + c), tree_load<AT>(a.k, kp + c), s);
-      const float2 st = a.stat[((int64_t)b * a.T + t) * a.H + h];
-      sum += expf(s * a.scale - st.x) * st.y;
+// ------------------------------------------------------------------ tiles
+// A wave takes KEYS keys and RT tiles of 16 rows (queries of one kv head) at a time and
+// computes S^T = K Q^T and O^T += V^T P^T with 16x16 MFMAs, so a lane owns query
+// lane % 16 in both: the softmax runs in registers and P needs no exchange, because the
+// order of the keys within a product is free.  With g = lane / 16 the lane holds the
+// scores of keys 4g .. 4g+3 of each 16-key tile, so it also loads the values of these
+// keys: a 16-byte piece of consecutive channels each, 16 lanes a whole row.  Value
+// product n then takes channel n of every lane's piece.
+// Operands come straight from global memory: every key and value is used by one wave
+// (or by the few waves of other row groups, through L2), so LDS would only add a trip.
+template <typename AT, int DH>
+struct TreeTile;
+
+// bf16: 32 keys, v_mfma_f32_16x16x32_bf16.  k index 8g + e of the value product is key
+// 4g + e (e < 4) or 16 + 4g + e - 4.
+template <int DH>
+struct TreeTile<uint16_t, DH> {
+  static constexpr int KEYS = 32, KT = 2, NK = DH / 32, CPL = DH / 16;  // CPL: channels of a lane
+  static constexpr int VW = CPL / 2;                                     // words of a key's piece
+  struct Q {
+    bf16x8 f[NK];
+  };
+  struct K {
+    bf16x8 f[KT][NK];
+  };
+  struct V {
+    uint32_t w[8][VW];
+  };
+  // channel of accumulator n, operand row m
+  __device__ static __forceinline__ int channel(int n, int m) {
+    return DH <= 128 ? CPL * m + n : 128 * (n / 8) + 8 * m + n % 8;
+  }
+  __device__ static __forceinline__ int value_key(int e, int g) { return e < 4 ? 4 * g + e : 12 + 4 * g + e; }
+
+  template <bool FULL>
+  __device__ static __forceinline__ bf16x8 chunk(const uint16_t* p, int c, int dh) {
+    if (!FULL && c >= dh) return __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + c));
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_q(Q& q, const uint16_t* row, int g, int dh, bool flip) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      u32x4 x = __builtin_bit_cast(u32x4, chunk<FULL>(row, 32 * i + 8 * g, dh));
+      if (flip) x ^= 0x80008000u;
+      q.f[i] = __builtin_bit_cast(bf16x8, x);
     }
   }
-  a.w_out[w] = (j < ext.x && a.w_in ? a.w_in[w] : 0.f) + sum;
+  template <bool FULL>
+  __device__ static __forceinline__ void load_k(K& k, const uint16_t* base, int64_t stride, int j0, int n, int lane,
+                                                int dh) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const uint16_t* row = base + (int64_t)min(j0 + 16 * t + (lane & 15), n - 1) * stride;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) k.f[t][i] = chunk<FULL>(row, 32 * i + 8 * (lane >> 4), dh);
+    }
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_v(V& v, const uint16_t* base, int64_t stride, int j0, int n, int lane,
+                                                int dh) {
+    const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint16_t* row = base + (int64_t)min(j0 + value_key(e, g), n - 1) * stride;
+      if constexpr (DH == 64) {
+        uint2 x = make_uint2(0, 0);
+        if (FULL || 4 * m < dh) x = *reinterpret_cast<const uint2*>(row + 4 * m);
+        v.w[e][0] = x.x;
+        v.w[e][1] = x.y;
+      } else {
+#pragma unroll
+        for (int q = 0; q < DH / 128; ++q) {
+          const u32x4 x = __builtin_bit_cast(u32x4, chunk<FULL>(row, 128 * q + 8 * m, dh));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v.w[e][4 * q + i] = x[i];
+        }
+      }
+    }
+  }
+  __device__ static __forceinline__ void scores(floatx4* s, const K& k, const Q& q) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      s[t] = floatx4{};
+#pragma unroll
+      for (int i = 0; i < NK; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.f[t][i], q.f[i], s[t], 0, 0, 0);
+    }
+  }
+  // whether a value of the lane's keys is infinite or NaN
+  __device__ static __forceinline__ bool nonfinite(const V& v) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < VW; ++i)
+        bad = bad || (v.w[e][i] & 0x7F80u) == 0x7F80u || (v.w[e][i] & 0x7F800000u) == 0x7F800000u;
+    return bad;
+  }
+  __device__ static __forceinline__ void drop_nonfinite(V& v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < VW; ++i) {
+        const uint32_t x = v.w[e][i];
+        v.w[e][i] = ((x & 0x7F80u) == 0x7F80u ? 0u : x & 0xFFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : x & 0xFFFF0000u);
+      }
+  }
+  // adds inf (kind 0), -inf (1) or NaN (2) to every output whose row sees such a value
+  template <int RT>
+  __device__ static __forceinline__ void special(floatx4 (*o)[CPL], const V& v, const float (*on)[KT * 4], int kind) {
+    uint32_t bits = kind == 2 ? 0x7FFFu : 0xFFFFu, lo = kind == 0 ? 0x7F80u : (kind == 1 ? 0xFF80u : 0x7F81u);
+    uint32_t span = kind == 2 ? 0x7Eu : 0u;
+    asm volatile("" : "+s"(bits), "+s"(lo), "+s"(span));  // not three sets of comparisons, kept ahead of time
+    auto is = [=](uint32_t h) { return (h & bits) - lo <= span ? 0x3F80u : 0u; };
+    const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
+#pragma unroll
+    for (int n = 0; n < CPL; ++n) {
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t sh = 16 * (n % 2);
+        x[e] = is(v.w[2 * e][n / 2] >> sh & 0xFFFFu) | is(v.w[2 * e + 1][n / 2] >> sh & 0xFFFFu) << 16;
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        u32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{on[r][2 * e], on[r][2 * e + 1]}, bf16x2v));
+        const floatx4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
+                                                                  __builtin_bit_cast(bf16x8, y), floatx4{}, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[r][n][i] += c[i] > 0.f ? add : 0.f;
+      }
+    }
+  }
+  // O^T += V^T P^T; the fp32 weights enter as bf16 high and low parts
+  template <int RT>
+  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const V& v, const float (*p)[KT * 4]) {
+    bf16x8 hi[RT], lo[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      u32x4 wh, wl;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a0 = p[r][2 * e], a1 = p[r][2 * e + 1];
+        const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
+        const float2v rest{a0 - __uint_as_float(h << 16), a1 - __uint_as_float(h & 0xFFFF0000u)};
+        wh[e] = h;
+        wl[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
+      }
+      hi[r] = __builtin_bit_cast(bf16x8, wh);
+      lo[r] = __builtin_bit_cast(bf16x8, wl);
+    }
+#pragma unroll
+    for (int n = 0; n < CPL; ++n) {
+      // channel n of the lane's eight keys
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = __builtin_amdgcn_perm(v.w[2 * e + 1][n / 2], v.w[2 * e][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
+      const bf16x8 a = __builtin_bit_cast(bf16x8, x);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[r], o[r][n], 0, 0, 0);
+        o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[r], o[r][n], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// fp32: 16 keys, v_mfma_f32_16x16x4_f32 (exact products, fp32 sums).  Channels of the
+// score product go in the order of the lanes' 16-byte pieces; value product (i, n) takes
+// key 4g + i.
+template <int DH>
+struct TreeTile<float, DH> {
+  static constexpr int KEYS = 16, KT = 1, NK = DH / 16, CPL = DH / 16;
+  struct Q {
+    floatx4 f[NK];
+  };
+  struct K {
+    floatx4 f[NK];
+  };
+  struct V {
+    floatx4 f[4][DH / 64];
+  };
+  __device__ static __forceinline__ int channel(int n, int m) { return 64 * (n / 4) + 4 * m + n % 4; }
+  __device__ static __forceinline__ int value_key(int e, int g) { return 4 * g + e; }
+
+  template <bool FULL>
+  __device__ static __forceinline__ floatx4 chunk(const float* p, int c, int dh) {
+    if (!FULL && c >= dh) return floatx4{};
+    return *reinterpret_cast<const floatx4*>(p + c);
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_q(Q& q, const float* row, int g, int dh, bool flip) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const floatx4 x = chunk<FULL>(row, 16 * i + 4 * g, dh);
+      q.f[i] = flip ? -x : x;
+    }
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_k(K& k, const float* base, int64_t stride, int j0, int n, int lane,
+                                                int dh) {
+    const float* row = base + (int64_t)min(j0 + (lane & 15), n - 1) * stride;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) k.f[i] = chunk<FULL>(row, 16 * i + 4 * (lane >> 4), dh);
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_v(V& v, const float* base, int64_t stride, int j0, int n, int lane,
+                                                int dh) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float* row = base + (int64_t)min(j0 + value_key(e, lane >> 4), n - 1) * stride;
+#pragma unroll
+      for (int q = 0; q < DH / 64; ++q) v.f[e][q] = chunk<FULL>(row, 64 * q + 4 * (lane & 15), dh);
+    }
+  }
+  __device__ static __forceinline__ void scores(floatx4* s, const K& k, const Q& q) {
+    s[0] = floatx4{};
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[i][c], q.f[i][c], s[0], 0, 0, 0);
+  }
+  __device__ static __forceinline__ bool nonfinite(const V& v) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int n = 0; n < CPL; ++n)
+        bad = bad || (__float_as_uint(v.f[e][n / 4][n % 4]) & 0x7F800000u) == 0x7F800000u;
+    return bad;
+  }
+  __device__ static __forceinline__ void drop_nonfinite(V& v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int n = 0; n < CPL; ++n)
+        if ((__float_as_uint(v.f[e][n / 4][n % 4]) & 0x7F800000u) == 0x7F800000u) v.f[e][n / 4][n % 4] = 0.f;
+  }
+  template <int RT>
+  __device__ static __forceinline__ void special(floatx4 (*o)[CPL], const V& v, const float (*on)[4], int kind) {
+    uint32_t bits = kind == 2 ? 0x7FFFFFFFu : ~0u, span = kind == 2 ? 0x7FFFFEu : 0u;
+    uint32_t lo = kind == 0 ? 0x7F800000u : (kind == 1 ? 0xFF800000u : 0x7F800001u);
+    asm volatile("" : "+s"(bits), "+s"(lo), "+s"(span));  // not three sets of comparisons, kept ahead of time
+    const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
+#pragma unroll
+    for (int n = 0; n < CPL; ++n)
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        floatx4 c = floatx4{};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t x = __float_as_uint(v.f[e][n / 4][n % 4]);
+          c = __builtin_amdgcn_mfma_f32_16x16x4f32((x & bits) - lo <= span ? 1.f : 0.f, on[r][e], c, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[r][n][i] += c[i] > 0.f ? add : 0.f;
+      }
+  }
+  template <int RT>
+  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const V& v, const float (*p)[4]) {
+#pragma unroll
+    for (int n = 0; n < CPL; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          o[r][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.f[e][n / 4][n % 4], p[r][e], o[r][n], 0, 0, 0);
+  }
+};
+
+// Bits of the KEYS keys from j0 that node t sees: the context, then its mask.
+template <int KEYS>
+__device__ __forceinline__ uint32_t tree_window(const TreeArgs& a, int b, int t, int j0, int2 ext) {
+  const int u0 = j0 - ext.x;  // node of the first key, negative within the context
+  uint64_t x;
+  if (!a.mask) {
+    const int c = t - u0 + 1;
+    x = c >= 64 ? ~0ull : (c <= 0 ? 0ull : (1ull << c) - 1ull);
+  } else {
+    const int W = (a.T + 63) / 64;
+    const uint64_t* row = a.mask + ((int64_t)b * a.T + t) * W;
+    if (u0 >= 0) {
+      const int w = u0 >> 6, sh = u0 & 63;
+      x = w < W ? row[w] >> sh : 0ull;
+      if (sh && w + 1 < W) x |= row[w + 1] << (64 - sh);
+    } else {
+      x = u0 <= -64 ? ~0ull : (row[0] << -u0) | ((1ull << -u0) - 1ull);
+    }
+  }
+  const int left = ext.x + ext.y - j0;  // keys up to the last live node
+  const uint32_t v = left >= 32 ? ~0u : (1u << max(left, 0)) - 1u;
+  return (uint32_t)x & v & (KEYS == 32 ? ~0u : (1u << KEYS) - 1u);
 }
 
-size_t tree_ws_bytes(int B, int T, int H, bool weights) {
-  return weights ? align_up((size_t)B * T * H * sizeof(float2), 256) : 0;
+// Splits of the keys of one sample: at most a.splits, each of at least a.min_tiles tiles.
+__device__ __forceinline__ int tree_splits(const TreeArgs& a, int tiles) {
+  return max(1, min(a.splits, tiles / a.min_tiles));
 }
 
+// The maximum may lag behind by this much (in powers of two) before the sums are
+// rescaled: the exponentials then stay below 2^8.
+constexpr float kLazyMax = 8.f;
+
+// grid: row groups x units (sample, kv head, split), see tree_place; 4 waves, wave w
+// takes tiles w, w + 4, .. of the block's split; their sums meet in LDS.
+template <typename AT, int DH, int RT, bool FULL>
+__global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_kernel(TreeArgs a) {
+  using T = TreeTile<AT, DH>;
+  constexpr int KEYS = T::KEYS, KT = T::KT, CPL = T::CPL;
+  constexpr int ROWS = 16 * RT, LD = DH + 4;
+  __shared__ float xm[4][ROWS], xl[4][ROWS];
+  __shared__ float xo[4][ROWS][LD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int m = lane & 15, g = lane >> 4;
+  // row groups of a unit lie 8 blocks apart: on the same XCD, whose L2 holds the unit's keys
+  const int slot = blockIdx.x >> 3;
+  const int unit = slot / a.groups * 8 + (blockIdx.x & 7), group = slot % a.groups;
+  if (unit >= a.B * a.Hkv * a.splits) return;
+  const int split = unit % a.splits, bh = unit / a.splits, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int G = a.H / a.Hkv;
+  const int2 ext = tree_extent(a, b);
+  const int n = ext.x + ext.y, R = ext.y * G, r0 = group * ROWS;
+  if (r0 >= R) return;
+  const int tiles = (n + KEYS - 1) / KEYS, ns = tree_splits(a, tiles);
+  if (split >= ns) return;
+  const int per = (tiles + ns - 1) / ns, t0 = split * per, t1 = min(tiles, t0 + per);
+  const AT* kb = reinterpret_cast<const AT*>(a.k) + b * a.kvb + hk * a.kvh;
+  const AT* vb = reinterpret_cast<const AT*>(a.v) + b * a.kvb + hk * a.kvh;
+  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  typename T::Q q[RT];
+  int node[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = min(r0 + 16 * r + m, R - 1);
+    node[r] = row / G;
+    const AT* qp = reinterpret_cast<const AT*>(a.q) + b * a.qb + node[r] * a.qt + (int64_t)(hk * G + row % G) * a.dh;
+    T::template load_q<FULL>(q[r], qp, g, a.dh, a.scale < 0.f);
+  }
+  floatx4 o[RT][CPL];
+  float top[RT], sum[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    top[r] = -INFINITY;
+    sum[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) o[r][c] = floatx4{};
+  }
+  typename T::K k;
+  typename T::V v;
+  if (t0 + wave < t1) T::template load_k<FULL>(k, kb, a.kvs, (t0 + wave) * KEYS, n, lane, a.dh);
+  auto step = [&](int t, auto tail_) {
+    constexpr bool tail = decltype(tail_)::value;  // some key is a node, or past the last one
+    const int j0 = t * KEYS;
+    T::template load_v<FULL>(v, vb, a.kvs, j0, n, lane, a.dh);
+    float p[RT][KT * 4];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      floatx4 s[KT];
+      T::scores(s, k, q[r]);
+#pragma unroll
+      for (int i = 0; i < KT * 4; ++i) p[r][i] = s[i / 4][i % 4];
+    }
+    if (t + 4 < t1) T::template load_k<FULL>(k, kb, a.kvs, j0 + 4 * KEYS, n, lane, a.dh);
+    uint32_t seen[RT];  // the lane's keys that its row sees, bit i for score i
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      seen[r] = ~0u;
+      if constexpr (tail) {
+        const uint32_t w = tree_window<KEYS>(a, b, node[r], j0, ext) >> (4 * g);
+        seen[r] = (w & 15u) | (KT == 2 ? (w >> 12) & 0xF0u : 0u);
+#pragma unroll
+        for (int i = 0; i < KT * 4; ++i) p[r][i] = (seen[r] >> i) & 1u ? p[r][i] : -INFINITY;
+      }
+    }
+    bool grows = false;
+    float mx[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      mx[r] = p[r][0];
+#pragma unroll
+      for (int i = 1; i < KT * 4; ++i) mx[r] = fmaxf(mx[r], p[r][i]);
+      float2 x = lanes_x16(mx[r]);
+      x = lanes_x32(fmaxf(x.x, x.y));
+      mx[r] = fmaxf(x.x, x.y);
+      grows = grows || mx[r] * sc > top[r] * sc + kLazyMax || (top[r] == -INFINITY && mx[r] > -INFINITY);
+    }
+    if (__any(grows)) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const float nt = fmaxf(top[r], mx[r]);
+        const float f = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top[r] - nt) * sc);
+        top[r] = nt;
+        sum[r] *= f;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) o[r][c] *= f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const float mc = top[r] == -INFINITY ? 0.f : top[r] * sc;
+      float s0 = 0.f;
+#pragma unroll
+      for (int i = 0; i < KT * 4; ++i) {
+        float e = __builtin_amdgcn_exp2f(fmaf(p[r][i], sc, -mc));
+        if constexpr (tail) e = (seen[r] >> i) & 1u ? e : 0.f;
+        p[r][i] = e;
+        s0 += e;
+      }
+      sum[r] += s0;
+    }
+    if constexpr (tail) if (__any(T::nonfinite(v))) {
+      // infinite and NaN values count for the rows that see them, and for no other (0 times
+      // one of them is NaN): a product of its own for each kind, then they leave v
+      float on[RT][KT * 4];
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < KT * 4; ++i) on[r][i] = (seen[r] >> i) & 1u ? 1.f : 0.f;
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) T::template special<RT>(o, v, on, kind);
+      T::drop_nonfinite(v);
+    }
+    T::template values<RT>(o, v, p);
+  };
+  int t = t0 + wave;
+  for (; t < min(t1, ext.x / KEYS); t += 4) step(t, std::false_type{});
+  for (; t < t1; t += 4) step(t, std::true_type{});
+
+  // the waves' sums onto their common maximum, in wave order
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    float2 x = lanes_x16(sum[r]);
+    x = lanes_x32(x.x + x.y);
+    if (g == 0) {
+      xm[wave][16 * r + m] = top[r];
+      xl[wave][16 * r + m] = x.x + x.y;
+    }
+#pragma unroll
+    for (int c = 0; c < CPL; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xo[wave][16 * r + m][T::channel(c, 4 * g + i)] = o[r][c][i];
+  }
+  __syncthreads();
+  constexpr int PER = 256 / ROWS >= 4 ? 256 / ROWS : 4;  // threads of a row
+  const int c0 = 4 * (tid % PER);
+  for (int row = tid / PER; row < min(ROWS, R - r0); row += 256 / PER) {
+    float mx = -INFINITY, l = 0.f, f[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, xm[w][row]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[w] = xm[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm[w][row] - mx) * sc);
+      // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
+      l += xm[w][row] == -INFINITY ? xl[w][row] : xl[w][row] * f[w];
+    }
+    const int rr = r0 + row, node_ = rr / G, h = hk * G + rr % G;
+    const int64_t out_row = ((int64_t)b * a.T + node_) * a.H + h;
+    const int64_t part_row = ((int64_t)bh * a.T * G + rr) * a.splits + split;
+    if (tid % PER == 0) {
+      if (ns > 1) a.part_ml[part_row] = make_float2(mx, l);
+      else if (a.stat) a.stat[out_row] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
+    }
+    for (int c = c0; c < a.dh; c += 4 * PER) {
+      floatx4 x = floatx4{};
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += xo[w][row][c + i] * f[w];
+      if (ns > 1) {
+        *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + c) = x;
+      } else {
+        tree_store<AT>(a.out, out_row * a.dh + c, x, l);
+      }
+    }
+  }
+}
+
+// The splits of one row joined: grid (rows of T * H, B), a thread per four channels.
 template <typename AT>
-spider_status run_tree(const TreeArgs& a, hipStream_t st) {
+__global__ void __launch_bounds__(64) tree_join_kernel(TreeArgs a) {
+  const int t = blockIdx.x / a.H, h = blockIdx.x % a.H, b = blockIdx.y;
+  const int2 ext = tree_extent(a, b);
+  if (t >= ext.y) return;
+  constexpr int KEYS = sizeof(AT) == 2 ? 32 : 16;
+  const int ns = tree_splits(a, (ext.x + ext.y + KEYS - 1) / KEYS);
+  if (ns == 1) return;
+  const int G = a.H / a.Hkv, hk = h / G;
+  const int64_t part = (((int64_t)b * a.Hkv + hk) * a.T * G + (int64_t)t * G + h % G) * a.splits;
+  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  float mx = -INFINITY;
+  for (int s = 0; s < ns; ++s) mx = fmaxf(mx, a.part_ml[part + s].x);
+  const int64_t row = ((int64_t)b * a.T + t) * a.H + h;
+  const int c = 4 * threadIdx.x;
+  float l = 0.f;
+  floatx4 x = floatx4{};
+  for (int s = 0; s < ns; ++s) {
+    const float2 ml = a.part_ml[part + s];
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mx) * sc);
+    l += ml.x == -INFINITY ? ml.y : ml.y * f;
+    if (c < a.dh) x += *reinterpret_cast<const floatx4*>(a.part_o + (part + s) * a.dh + c) * f;
+  }
+  if (c < a.dh) tree_store<AT>(a.out, row * a.dh + c, x, l);
+  if (a.stat && threadIdx.x == 0)
+    a.stat[row] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
+}
+
+// The weight of every slot: a wave per KEYS keys of one kv head, all live rows of the
+// head group in tiles of 16; exp2(s - max) / sum from the rows' final statistics.
+template <typename AT, int DH, bool FULL>
+__global__ void __launch_bounds__(256) tree_weights_kernel(TreeArgs a) {
+  using T = TreeTile<AT, DH>;
+  constexpr int KEYS = T::KEYS, KT = T::KT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int m = lane & 15, g = lane >> 4;
+  const int blocks = (a.cap + 4 * KEYS - 1) / (4 * KEYS), bh = blockIdx.x / blocks;
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int G = a.H / a.Hkv;
+  const int2 ext = tree_extent(a, b);
+  const int n = ext.x + ext.y, R = ext.y * G;
+  const int j0 = (4 * (blockIdx.x % blocks) + wave) * KEYS;
+  if (j0 >= n) return;
+  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  typename T::K k;
+  T::template load_k<FULL>(k, reinterpret_cast<const AT*>(a.k) + b * a.kvb + hk * a.kvh, a.kvs, j0, n, lane, a.dh);
+  const bool tail = j0 + KEYS > ext.x;
+  float acc[KT * 4] = {};
+  for (int r0 = 0; r0 < R; r0 += 16) {
+    const int row = min(r0 + m, R - 1), t = row / G, h = hk * G + row % G;
+    typename T::Q q;
+    T::template load_q<FULL>(q, reinterpret_cast<const AT*>(a.q) + b * a.qb + t * a.qt + (int64_t)h * a.dh, g, a.dh,
+                             a.scale < 0.f);
+    const float2 st = a.stat[((int64_t)b * a.T + t) * a.H + h];
+    floatx4 s[KT];
+    T::scores(s, k, q);
+    uint32_t w = ~0u;
+    if (tail) w = tree_window<KEYS>(a, b, t, j0, ext);
+    if (r0 + m >= R) w = 0;
+    w >>= 4 * g;
+#pragma unroll
+    for (int i = 0; i < KT * 4; ++i) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], sc, -st.x)) * st.y;
+      acc[i] += (w >> (i / 4 * 16 + i % 4)) & 1u ? e : 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < KT * 4; ++i) {
+    const float x = row16_sum(acc[i]);
+    const int j = j0 + 16 * (i / 4) + 4 * g + i % 4;
+    const int64_t at = (int64_t)bh * a.cap + j;
+    if (m == i && j < n) a.w_out[at] = (j < ext.x && a.w_in ? a.w_in[at] : 0.f) + x;
+  }
+}
+
+// Tiles, row groups and splits of a call, and its workspace.
+struct TreePlan {
+  int dhp;     // kernel width: 64, 128 or 256
+  int rt;      // row tiles of a wave
+  int groups;  // row groups of a unit
+  int splits, min_tiles;
+  size_t ml_off, o_off, bytes;
+};
+
+TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype dtype, bool weights) {
+  TreePlan p{};
+  const bool bf16 = dtype == SPIDER_BF16;
+  const int R = T * (H / Hkv), keys = bf16 ? 32 : 16;
+  p.dhp = dh <= 64 ? 64 : (dh <= 128 ? 128 : 256);
+  p.rt = R <= 16 ? 1 : (R <= 32 || !bf16 || p.dhp == 256 ? 2 : 4);
+  p.groups = ceil_div(R, 16 * p.rt);
+  p.min_tiles = 8;
+  const int64_t units = (int64_t)B * Hkv * p.groups;
+  const int tiles = ceil_div(cap, keys);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((768 + units - 1) / units, tiles / p.min_tiles));
+  size_t off = weights ? align_up((size_t)B * T * H * sizeof(float2), 256) : 0;
+  p.ml_off = off;
+  if (p.splits > 1) {
+    const size_t rows = (size_t)B * T * H * p.splits;
+    off = align_up(off + rows * sizeof(float2), 256);
+    p.o_off = off;
+    off = align_up(off + rows * dh * sizeof(float), 256);
+  }
+  p.bytes = off;
+  return p;
+}
+
+template <typename AT, int DH, int RT>
+void launch_tree(const TreeArgs& a, hipStream_t st) {
+  const int units = (a.B * a.Hkv * a.splits + 7) / 8 * 8;
+  if (a.dh == DH) tree_attention_kernel<AT, DH, RT, true><<<(unsigned)(units * a.groups), 256, 0, st>>>(a);
+  else tree_attention_kernel<AT, DH, RT, false><<<(unsigned)(units * a.groups), 256, 0, st>>>(a);
+}
+
+template <typename AT, int DH>
+void launch_tree_weights(const TreeArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)ceil_div(a.cap, 4 * TreeTile<AT, DH>::KEYS) * (unsigned)(a.B * a.Hkv);
+  if (a.dh == DH) tree_weights_kernel<AT, DH, true><<<grid, 256, 0, st>>>(a);
+  else tree_weights_kernel<AT, DH, false><<<grid, 256, 0, st>>>(a);
+}
+
+template <typename AT, int DH>
+spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   {
     ProfScope ps(KC_TREE_ATTN, st);
-    tree_rows_kernel<AT><<<dim3((unsigned)(a.T * a.H), (unsigned)a.B), 256, 0, st>>>(a);
-    SPIDER_LAUNCHED("tree_rows");
+    if (p.rt == 1) launch_tree<AT, DH, 1>(a, st);
+    else if (p.rt == 2) launch_tree<AT, DH, 2>(a, st);
+    else if constexpr (sizeof(AT) == 2 && DH <= 128) launch_tree<AT, DH, 4>(a, st);
+    SPIDER_LAUNCHED("tree_attention");
+    if (a.splits > 1) {
+      tree_join_kernel<AT><<<dim3((unsigned)(a.T * a.H), (unsigned)a.B), 64, 0, st>>>(a);
+      SPIDER_LAUNCHED("tree_join");
+    }
   }
   if (a.w_out) {
     ProfScope ps(KC_TREE_WEIGHTS, st);
-    tree_weights_kernel<AT><<<dim3((unsigned)ceil_div(a.cap, 256), (unsigned)a.Hkv, (unsigned)a.B), 256, 0, st>>>(a);
+    launch_tree_weights<AT, DH>(a, st);
     SPIDER_LAUNCHED("tree_weights");
   }
   return SPIDER_OK;
 }
 
+template <typename AT>
+spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
+  return p.dhp == 64 ? run_tree<AT, 64>(a, p, st) : (p.dhp == 128 ? run_tree<AT, 128>(a, p, st) : run_tree<AT, 256>(a, p, st));
+}
+
 bool tree_shape_ok(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype dtype) {
   return B >= 1 && B <= 65535 && T >= 1 && T <= kTreeMaxNodes && H >= 1 && H <= 65535 && Hkv >= 1 && H % Hkv == 0 &&
-         dh >= 1 && dh <= kTreeMaxDh && cap >= 1 && (dtype == SPIDER_BF16 || dtype == SPIDER_F32);
+         dh >= 1 && dh <= kTreeMaxDh && cap >= 1 && (int64_t)B * H * T < (1 << 24) &&
+         (int64_t)B * Hkv * ceil_div(cap, 64) < (1 << 24) && (dtype == SPIDER_BF16 || dtype == SPIDER_F32);
 }
 
 }  // namespace
@@ -167,7 +703,7 @@ using namespace spider;
 extern "C" size_t spider_tree_attention_workspace_size(int B, int T, int H, int Hkv, int dh, int cap,
                                                        spider_dtype dtype, int weights) {
   if (!tree_shape_ok(B, T, H, Hkv, dh, cap, dtype)) return 0;
-  return tree_ws_bytes(B, T, H, weights != 0);
+  return tree_plan(B, T, H, Hkv, dh, cap, dtype, weights != 0).bytes;
 }
 
 extern "C" spider_status spider_tree_attention(int B, int T, int H, int Hkv, int dh, const void* q,
@@ -188,6 +724,9 @@ extern "C" spider_status spider_tree_attention(int B, int T, int H, int Hkv, int
   SPIDER_REQUIRE(H % Hkv == 0, SPIDER_ERR_SHAPE, "spider_tree_attention: %d heads over %d kv heads", H, Hkv);
   SPIDER_REQUIRE(T <= kTreeMaxNodes && dh <= kTreeMaxDh && B <= 65535 && H <= 65535, SPIDER_ERR_UNSUPPORTED,
                  "spider_tree_attention: T <= %d, dh <= %d, B and H <= 65535", kTreeMaxNodes, kTreeMaxDh);
+  // blocks of the largest launch (a grid holds 2^24 blocks of 256 threads)
+  SPIDER_REQUIRE((int64_t)B * H * T < (1 << 24) && (int64_t)B * Hkv * ceil_div(cap, 64) < (1 << 24),
+                 SPIDER_ERR_UNSUPPORTED, "spider_tree_attention: B * H * T or B * Hkv * cap / 64 reach 2^24");
   const int64_t per16 = dtype == SPIDER_BF16 ? 8 : 4;
   SPIDER_REQUIRE(dh % per16 == 0, SPIDER_ERR_UNSUPPORTED, "spider_tree_attention: dh must be a multiple of 16 bytes");
   SPIDER_REQUIRE(q_stride_b % per16 == 0 && q_stride_t % per16 == 0 && kv_stride_b % per16 == 0 &&
@@ -198,14 +737,21 @@ extern "C" spider_status spider_tree_attention(int B, int T, int H, int Hkv, int
   const uintptr_t bits = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) |
                          reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out);
   SPIDER_REQUIRE(bits % 16 == 0, SPIDER_ERR_INVALID_ARG, "spider_tree_attention: q, k, v and out must be 16-byte aligned");
-  const size_t need = tree_ws_bytes(B, T, H, weights_out != nullptr);
+  const TreePlan p = tree_plan(B, T, H, Hkv, dh, cap, dtype, weights_out != nullptr);
+  const size_t need = p.bytes;
   SPIDER_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), SPIDER_ERR_WORKSPACE,
                  "spider_tree_attention: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
   SPIDER_REQUIRE(need == 0 || reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG,
                  "spider_tree_attention: workspace must be 256-byte aligned");
-  TreeArgs a{q, k, v, out, lens, n_nodes, tree_mask, weights_in, weights_out, reinterpret_cast<float2*>(workspace),
-             q_stride_b, q_stride_t, kv_stride_b, kv_stride_s, kv_stride_h, B, T, H, Hkv, dh, cap, scale};
-  if (!weights_out) a.stat = nullptr;
+  char* ws = reinterpret_cast<char*>(workspace);
+  TreeArgs a{q, k, v, out, lens, n_nodes, tree_mask, weights_in, weights_out, nullptr, nullptr, nullptr,
+             q_stride_b, q_stride_t, kv_stride_b, kv_stride_s, kv_stride_h, B, T, H, Hkv, dh, cap, scale,
+             p.groups, p.splits, p.min_tiles};
+  if (weights_out) a.stat = reinterpret_cast<float2*>(ws);
+  if (p.splits > 1) {
+    a.part_ml = reinterpret_cast<float2*>(ws + p.ml_off);
+    a.part_o = reinterpret_cast<float*>(ws + p.o_off);
+  }
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  return dtype == SPIDER_BF16 ? run_tree<uint16_t>(a, st) : run_tree<float>(a, st);
+  return dtype == SPIDER_BF16 ? run_tree<uint16_t>(a, p, st) : run_tree<float>(a, p, st);
 }
