@@ -541,6 +541,34 @@ spider_status spider_tree_attention(int B, int T, int H, int Hkv, int dh, const 
                                     void* workspace, size_t workspace_bytes, spider_stream stream);
 
 /* ------------------------------------------------------------------------
+ * spider_decode_tree - spider_decode_step over the nodes of a tree per sample:
+ * node t of sample b (input row x[b*T + t]) runs through every layer with
+ * nothing bypassed, its key and value go to cache slot lens[b] + t, its query
+ * attends by spider_tree_attention, and its RoPE position is pos[b] + its depth.
+ * After verification the accepted nodes move behind the context with
+ * spider_cache_compact (base = lens), and lens and pos advance by their number;
+ * after an eviction lens falls and pos does not.
+ * parents: HOST int32 [B][T] as for spider_tree_mask, or NULL (a chain: T rows
+ * one after another).  lens HOST int32 [B]: filled slots, lens[b] + present
+ * nodes <= kv->cap; pos HOST int32 [B] or NULL (= lens).  x device [B*T, d];
+ * final_norm, w_unembed, V, h_out [B*T, d], logits_out [B*T, V] and next_out
+ * [B*T] as for spider_decode_step, row b*T + t for node t; rows of absent nodes
+ * hold unspecified values, and their slots are not written.  weights: device
+ * fp32 [L][B][H][cap] or NULL: the attention weight of every slot is added up
+ * in each layer, spider_tree_attention's weights_in = weights_out.
+ * Limits: T <= 256, B*T <= 65535, dh a multiple of 16 bytes, at most 256 (bf16:
+ * 128).  Workspace: spider_decode_tree_workspace_size(cfg, B, T, kv->cap, V)
+ * bytes (V = 0 without the head).
+ * ------------------------------------------------------------------------ */
+size_t spider_decode_tree_workspace_size(const spider_decoder_cfg* cfg, int B, int T, int cap, int V);
+
+spider_status spider_decode_tree(const spider_decoder_cfg* cfg, const spider_layer_weights* layers, int B, int T,
+                                 const int32_t* lens, const int32_t* pos, const int32_t* parents, const void* x,
+                                 const spider_kv_cache* kv, const float* final_norm, const void* w_unembed, int V,
+                                 float* h_out, float* logits_out, int32_t* next_out, float* weights,
+                                 void* workspace, size_t workspace_bytes, spider_stream stream);
+
+/* ------------------------------------------------------------------------
  * spider_cache_select - the slots a cache keeps, by accumulated attention
  * weight.  For every layer l, sample b and head group (each kv head its own
  * choice, or with shared = 1 one for all of them, on the weights added over

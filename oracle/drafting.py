@@ -9,6 +9,9 @@ from __future__ import annotations
 
 import numpy as np
 
+from .bf16 import round_bf16
+from .decoder import rmsnorm, rope, silu
+
 
 def tree_mask(parents):
     """parents [B, T] -> (sees [B, T, T] bool, depth [B, T])."""
@@ -154,3 +157,36 @@ def adjust_logits(logits, history=None, n_history=None, n_prompt=None, node_toke
             z = np.where(np.isnan(y), -np.inf, y)
             best[b, t] = -1 if z.max() == -np.inf else int(np.argmax(z))
     return out, best
+
+
+def decode_tree(x, weights, k, v, lens, pos, parents, cfg, recipe="bf16", attn_weights=None):
+    """One step over the nodes x [B, T, d] of a tree on explicit caches k, v [L, B, cap, d]
+    (updated in place, as are attn_weights [L, B, H, cap] if given) -> states [B, T, d]."""
+    rnd = round_bf16 if recipe == "bf16" else (lambda t: t)
+    get = weights if callable(weights) else (lambda l: weights[l])
+    f = lambda a: np.asarray(a, np.float64)  # noqa: E731
+    B, T, d = x.shape
+    H, dh = cfg.H, cfg.d // cfg.H
+    sees, depth = tree_mask(parents)
+    live = [int((np.asarray(parents[b]) > -2).sum()) for b in range(B)]
+    at = (np.asarray(pos)[:, None] + depth).reshape(-1)
+    h = f(x).reshape(B * T, d).copy()
+    for l in range(k.shape[0]):
+        w = get(l)
+        xn = f(rnd(rmsnorm(h, f(w["attn_norm"]), cfg.eps)))
+        q, kk, vv = ((xn @ f(w[m]).T).reshape(B * T, H, dh) for m in ("wq", "wk", "wv"))
+        q, kk, vv = f(rnd(rope(q, at, cfg.theta))), f(rnd(rope(kk, at, cfg.theta))), f(rnd(vv))
+        for b in range(B):
+            rows = slice(b * T, b * T + live[b])
+            k[l, b, lens[b]:lens[b] + live[b]] = kk[rows].reshape(live[b], d)
+            v[l, b, lens[b]:lens[b] + live[b]] = vv[rows].reshape(live[b], d)
+        shape = k.shape[1:3] + (H, dh)
+        o, aw = tree_attention(q.reshape(B, T, H, dh), k[l].reshape(shape), v[l].reshape(shape), lens, sees, live,
+                               weights_in=None if attn_weights is None else attn_weights[l])
+        if attn_weights is not None:
+            attn_weights[l] = np.where(np.isnan(aw), attn_weights[l], aw)
+        o = f(rnd(np.nan_to_num(o).reshape(B * T, d)))
+        h = h + o @ f(w["wo"]).T
+        xn = f(rnd(rmsnorm(h, f(w["ffn_norm"]), cfg.eps)))
+        h = h + f(rnd(silu(xn @ f(w["wg"]).T) * (xn @ f(w["wu"]).T))) @ f(w["wd"]).T
+    return h.reshape(B, T, d)

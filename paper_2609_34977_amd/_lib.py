@@ -83,6 +83,9 @@ _SIGS = {
     "spider_tree_attention_workspace_size": ([_I, _I, _I, _I, _I, _I, _I, _I], _SZ),
     "spider_tree_attention": ([_I, _I, _I, _I, _I, _VP, _I64, _I64, _VP, _VP, _I64, _I64, _I64, _I, _VP, _VP, _VP, _I,
                                _F, _VP, _VP, _VP, _VP, _SZ, _VP], _I),
+    "spider_decode_tree_workspace_size": ([ctypes.POINTER(DecoderCfg), _I, _I, _I, _I], _SZ),
+    "spider_decode_tree": ([ctypes.POINTER(DecoderCfg), ctypes.POINTER(LayerWeights), _I, _I, _VP, _VP, _VP, _VP,
+                            ctypes.POINTER(KVCache), _VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _SZ, _VP], _I),
     "spider_cache_select": ([_I, _I, _I, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP], _I),
     "spider_cache_compact": ([_I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _VP, _VP, _I, _VP, _I, _I, _I, _VP, _VP,
                               _VP, _VP, _VP], _I),
@@ -531,6 +534,43 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torc
         _need(weights_in, "weights_in", torch.float32, (B, Hkv, cap), dev),
         _need(weights_out, "weights_out", torch.float32, (B, Hkv, cap), dev), _aligned(workspace), wsz)
     return out
+
+
+def decode_tree(cfg: DecoderCfg, weights, lens, x: torch.Tensor, kv: dict, parents=None, pos=None, final_norm=None,
+                w_unembed=None, weight_table=None, attn_weights: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None):
+    """One step over drafted nodes x [B, T, d] (kv from kv_cache()): lens [B] and pos [B] host
+    ints (pos None: lens), parents [B, T] host ints as for tree_mask (None: a chain).
+    attn_weights [L, B, H, cap] fp32 collect the attention weight of every slot.
+    Returns (h [B, T, d] fp32, logits [B, T, V] fp32 or None, arg max [B, T] int32 or None)."""
+    if x.dim() != 3 or not x.is_contiguous() or x.shape[2] != cfg.d:
+        raise ValueError("x must be a contiguous [B, T, d] tensor")
+    if _dt(x) != cfg.dtype:
+        raise ValueError("x must have the decoder's dtype")
+    B, T, d = x.shape
+    dev = x.device
+    cap = kv["desc"].cap
+    if tuple(kv["k"].shape) != (cfg.L, B, cap, d):
+        raise ValueError(f"the cache must be [{cfg.L}, {B}, cap, {d}]")
+    ln = np.ascontiguousarray(lens, dtype=np.int32)
+    ps = None if pos is None else np.ascontiguousarray(pos, dtype=np.int32)
+    pr = None if parents is None else np.ascontiguousarray(parents, dtype=np.int32)
+    if ln.shape != (B,) or (ps is not None and ps.shape != (B,)) or (pr is not None and pr.shape != (B, T)):
+        raise ValueError("lens and pos must be [B], parents [B, T]")
+    V = int(w_unembed.shape[0]) if w_unembed is not None else 0
+    h = torch.empty(B, T, d, dtype=torch.float32, device=dev)
+    logits = torch.empty(B, T, V, dtype=torch.float32, device=dev) if V else None
+    nxt = torch.empty(B, T, dtype=torch.int32, device=dev) if V else None
+    L = lib()
+    wsz = L.spider_decode_tree_workspace_size(ctypes.byref(cfg), B, T, cap, V)
+    if workspace is None or workspace.numel() < wsz + 256:
+        workspace = _ws(wsz, dev)
+    wt = weight_table if weight_table is not None else layer_weights(weights)
+    _on(dev, L.spider_decode_tree, ctypes.byref(cfg), wt, B, T, ln.ctypes.data,
+        None if ps is None else ps.ctypes.data, None if pr is None else pr.ctypes.data, x.data_ptr(),
+        ctypes.byref(kv["desc"]), _ptr(final_norm), _ptr(w_unembed), V, h.data_ptr(), _ptr(logits), _ptr(nxt),
+        _need(attn_weights, "attn_weights", torch.float32, (cfg.L, B, cfg.H, cap), dev), _aligned(workspace), wsz)
+    return h, logits, nxt
 
 
 def cache_select(weights: torch.Tensor, lens: torch.Tensor, keep: int, *, n_first: int = 0, n_last: int = 0,

@@ -404,6 +404,50 @@ __global__ void __launch_bounds__(256) decode_qkv_kernel(const float* __restrict
   }
 }
 
+// RoPE table rows of a tree step: row r of tab for position pos[r].
+__global__ void __launch_bounds__(256) tree_rope_kernel(float2* __restrict__ tab, const int32_t* __restrict__ pos,
+                                                        int rows, int half, int dh, double log2_theta) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= rows * half) return;
+  const int r = t / half, i = t - r * half;
+  const double ang = (double)pos[r] * exp2(-(2.0 * i / dh) * log2_theta);
+  tab[t] = make_float2((float)cos(ang), (float)sin(ang));
+}
+
+// Tree step, grid (B * T, 3): as decode_qkv_kernel for node row r, whose RoPE comes from
+// row r of the table and whose key and value go to slot[r] of sample r / T (none where
+// slot[r] is negative: an absent node).
+template <typename AT>
+__global__ void __launch_bounds__(256) tree_qkv_kernel(const float* __restrict__ Pq, const float* __restrict__ Pk,
+                                                       const float* __restrict__ Pv, int split, int64_t pstride, int T,
+                                                       int d, int dh, const int32_t* __restrict__ slot,
+                                                       const float2* __restrict__ rope, AT* __restrict__ Q,
+                                                       AT* __restrict__ ck, AT* __restrict__ cv, int64_t layer_off,
+                                                       int cap) {
+  const int r = blockIdx.x, kind = blockIdx.y, s0 = slot[r];
+  if (kind > 0 && s0 < 0) return;
+  const float* src = (kind == 0 ? Pq : (kind == 1 ? Pk : Pv)) + (int64_t)r * d;
+  AT* dst = kind == 0 ? Q + (int64_t)r * d : (kind == 1 ? ck : cv) + layer_off + ((int64_t)(r / T) * cap + s0) * d;
+  const int half = dh / 2;
+  for (int t = threadIdx.x; t < d / 2; t += 256) {
+    const int head = t / half, i = t - head * half;
+    const int c0 = head * dh + i, c1 = c0 + half;
+    float x0 = 0.f, x1 = 0.f;
+    for (int s = 0; s < split; ++s) {
+      x0 += src[s * pstride + c0];
+      x1 += src[s * pstride + c1];
+    }
+    if (kind < 2) {
+      const float2 cs = rope[(int64_t)r * half + i];
+      const float2 y = rope_rotate(x0, x1, cs.x, cs.y);
+      x0 = y.x;
+      x1 = y.y;
+    }
+    Act<AT>::store(dst + c0, x0);
+    Act<AT>::store(dst + c1, x1);
+  }
+}
+
 constexpr int kDecodeMaxKeys = 8192;
 constexpr int kDecodeMaxDh = 256;
 
@@ -1788,6 +1832,129 @@ spider_status run_decode(const spider_decoder_cfg& c, const spider_layer_weights
   return SPIDER_OK;
 }
 
+// ------------------------------------------------------------------ tree step
+struct TreeStepWs {
+  PrefillWs p;     // activations and partials for B * T rows
+  float2* rope;    // [B * T][dh/2]
+  int32_t* tab;    // identity [R], positions [R], slots [R], lengths [B], live nodes [B]; tree mask [B][T][W]
+  float* Plog;     // LM head partials [head_split][R][V]
+  void* attn;      // workspace of the attention
+  size_t attn_bytes, bytes;
+};
+
+// Split-K of the LM head: many nodes fill the chip without it.
+int tree_head_split(int R) { return std::max(1, std::min(kHeadSplit, 32 / R)); }
+
+size_t tree_tab_ints(int B, int T) { return (((size_t)3 * B * T + 2 * B + 1) & ~(size_t)1) + 2 * (size_t)B * T * ((T + 63) / 64); }
+
+TreeStepWs tree_step_layout(const spider_decoder_cfg& c, int B, int T, int cap, int V, char* base) {
+  Carver cv{base};
+  TreeStepWs w{};
+  const int R = B * T;
+  w.p = prefill_layout(c, R, cv);
+  w.rope = reinterpret_cast<float2*>(cv.take((size_t)R * (c.d / c.H / 2) * sizeof(float2)));
+  w.tab = reinterpret_cast<int32_t*>(cv.take(tree_tab_ints(B, T) * sizeof(int32_t)));
+  w.Plog = V > 0 ? reinterpret_cast<float*>(cv.take((size_t)tree_head_split(R) * R * V * sizeof(float))) : nullptr;
+  w.attn_bytes = spider_tree_attention_workspace_size(B, T, c.H, c.H, c.d / c.H, cap, c.dtype, 1);
+  w.attn = cv.take(w.attn_bytes);
+  w.bytes = cv.off;
+  return w;
+}
+
+// One step over the nodes of every sample's tree: a decode step whose rows share a
+// cache, attend by the tree mask and sit at their depth behind the context.
+template <typename AT>
+spider_status run_decode_tree(const spider_decoder_cfg& c, const spider_layer_weights* W, int B, int T,
+                              const std::vector<int32_t>& tab, const void* x, const spider_kv_cache& kv,
+                              const float* final_norm, const void* wu, int V, float* h, float* logits, int32_t* next,
+                              float* weights, const TreeStepWs& ws, hipStream_t st) {
+  const bool bf16 = c.dtype == SPIDER_BF16;
+  const int d = c.d, dh = d / c.H, half = dh / 2, R = B * T;
+  const PrefillWs& p = ws.p;
+  SPIDER_TRY(upload_ints(tab.data(), tab.size(), ws.tab, st));
+  const int32_t *ident = ws.tab, *pos = ws.tab + R, *slot = ws.tab + 2 * R, *lens = ws.tab + 3 * R, *nodes = lens + B;
+  const uint64_t* mask = reinterpret_cast<const uint64_t*>(ws.tab + (((size_t)3 * R + 2 * B + 1) & ~(size_t)1));
+  {
+    ProfScope ps(KC_EMBED, st);
+    launch_embed<AT>(x, h, (int64_t)R * d, RopeArgs{ws.rope, nullptr, 0, half, dh, 0.0}, st);
+    SPIDER_LAUNCHED("embed");
+    tree_rope_kernel<<<(unsigned)ceil_div(R * half, 256), 256, 0, st>>>(ws.rope, pos, R, half, dh,
+                                                                        std::log2((double)c.theta));
+    SPIDER_LAUNCHED("tree_rope");
+  }
+  AT* xn = reinterpret_cast<AT*>(p.xn);
+  AT* qb = reinterpret_cast<AT*>(p.q);
+  AT* ob = reinterpret_cast<AT*>(p.o);
+  AT* act = reinterpret_cast<AT*>(p.act);
+  AT* ck = reinterpret_cast<AT*>(kv.k);
+  AT* cv = reinterpret_cast<AT*>(kv.v);
+  const int64_t ps_ = (int64_t)R * d;
+  const int sm = split_max_for_rows(R);
+  auto gemm = [&](GemmArgs& ga, const GemmGroup* g, int ngroups, int K, int epilogue, int cap, int cls,
+                  const char* what) -> spider_status {
+    ga.ngroups = ngroups;
+    ga.K = K;
+    ga.lda = K;
+    ga.epilogue = epilogue;
+    for (int i = 0; i < ngroups; ++i) ga.g[i] = g[i];
+    ProfScope ps(cls, st);
+    const int s2 = std::min(cls == KC_LM_HEAD ? tree_head_split(R) : sm, cap);
+    hipError_t e = bf16 ? launch_gemm_bf16(ga, s2, st) : launch_gemm_f32(ga, s2, st);
+    SPIDER_REQUIRE(e == hipSuccess, SPIDER_ERR_HIP, "tree step %s: %s", what, hipGetErrorString(e));
+    return SPIDER_OK;
+  };
+  auto norm = [&](const float* w, int pend, AT* out) -> spider_status {
+    ProfScope ps(out ? KC_RMSNORM : KC_RESIDUAL, st);
+    launch_norm<AT>(R, h, d, p.Pres, pend, ps_, pend ? ident : nullptr, w, c.eps, nullptr, out ? 1 : 0, out, st);
+    SPIDER_LAUNCHED("rmsnorm");
+    return SPIDER_OK;
+  };
+  const float scale = (float)(1.0 / std::sqrt((double)dh));
+  int pend = 0;
+  for (int l = 0; l < c.L; ++l) {
+    const spider_layer_weights& w = W[l];
+    const int64_t loff = (int64_t)l * B * kv.cap * d;
+    SPIDER_TRY(norm(w.attn_norm, pend, xn));
+    GemmArgs ga{};
+    const GemmGroup qkv[3] = {{xn, nullptr, R, w.wq, nullptr, d, p.Pq, d, ps_, 0, 0, 0},
+                              {xn, nullptr, R, w.wk, nullptr, d, p.Pk, d, ps_, 0, 0, 0},
+                              {xn, nullptr, R, w.wv, nullptr, d, p.Pv, d, ps_, 0, 0, 0}};
+    SPIDER_TRY(gemm(ga, qkv, 3, d, EPI_PARTIAL_F32, 2, KC_GEMM_QKV, "gemm_qkv"));
+    {
+      ProfScope ps(KC_QKV_FINALIZE, st);
+      tree_qkv_kernel<AT><<<dim3((unsigned)R, 3), 256, 0, st>>>(p.Pq, p.Pk, p.Pv, ga.split, ps_, T, d, dh, slot,
+                                                                 ws.rope, qb, ck, cv, loff, kv.cap);
+      SPIDER_LAUNCHED("tree_qkv");
+    }
+    float* wl = weights ? weights + (int64_t)l * B * c.H * kv.cap : nullptr;
+    SPIDER_TRY(spider_tree_attention(B, T, c.H, c.H, dh, qb, (int64_t)T * d, d, ck + loff, cv + loff,
+                                     (int64_t)kv.cap * d, d, dh, kv.cap, lens, nodes, mask, c.dtype, scale, ob, wl, wl,
+                                     ws.attn, ws.attn_bytes, st));
+    GemmArgs go{};
+    const GemmGroup o{ob, nullptr, R, w.wo, nullptr, d, p.Pres, d, ps_, 0, 0, 0};
+    SPIDER_TRY(gemm(go, &o, 1, d, EPI_PARTIAL_F32, 8, KC_GEMM_O, "gemm_o"));
+    SPIDER_TRY(norm(w.ffn_norm, go.split, xn));
+    GemmArgs gu{};
+    const GemmGroup up{xn, nullptr, R, w.wg, w.wu, c.d_ff, act, c.d_ff, 0, 0, 0, 0};
+    SPIDER_TRY(gemm(gu, &up, 1, d, EPI_SWIGLU, 1, KC_GEMM_GATEUP, "gemm_gateup"));
+    GemmArgs gd{};
+    const GemmGroup dn{act, nullptr, R, w.wd, nullptr, d, p.Pres, d, ps_, 0, 0, 0};
+    SPIDER_TRY(gemm(gd, &dn, 1, c.d_ff, EPI_PARTIAL_F32, 8, KC_GEMM_DOWN, "gemm_down"));
+    pend = gd.split;
+  }
+  SPIDER_TRY(norm(nullptr, pend, static_cast<AT*>(nullptr)));
+  if (wu) {
+    SPIDER_TRY(norm(final_norm, 0, xn));
+    GemmArgs gh{};
+    const GemmGroup head{xn, nullptr, R, wu, nullptr, V, ws.Plog, V, (int64_t)R * V, 0, 0, 0};
+    SPIDER_TRY(gemm(gh, &head, 1, d, EPI_PARTIAL_F32, kHeadSplit, KC_LM_HEAD, "lm head"));
+    ProfScope ps(KC_LM_HEAD, st);
+    logits_argmax_kernel<<<R, kArgmaxThreads, 0, st>>>(ws.Plog, gh.split, (int64_t)R * V, V, logits, next);
+    SPIDER_LAUNCHED("logits_argmax");
+  }
+  return SPIDER_OK;
+}
+
 }  // namespace
 }  // namespace spider
 
@@ -1997,4 +2164,83 @@ extern "C" spider_status spider_decode_step(const spider_decoder_cfg* cfg, const
                                 next_out, ws, st);
   return run_decode<float>(*cfg, layers, B, lens, x, *kv, final_norm, w_unembed, Vh, h_out, logits_out, next_out,
                            ws, st);
+}
+
+extern "C" size_t spider_decode_tree_workspace_size(const spider_decoder_cfg* cfg, int B, int T, int cap, int V) {
+  if (!cfg || cfg->L < 1 || cfg->d < 1 || cfg->H < 1 || cfg->d % cfg->H || B < 1 || T < 1 || T > 256 || cap < 1 ||
+      V < 0 || (int64_t)B * T > 65535)
+    return 0;
+  return tree_step_layout(*cfg, B, T, cap, V, nullptr).bytes;
+}
+
+extern "C" spider_status spider_decode_tree(const spider_decoder_cfg* cfg, const spider_layer_weights* layers, int B,
+                                            int T, const int32_t* lens, const int32_t* pos, const int32_t* parents,
+                                            const void* x, const spider_kv_cache* kv, const float* final_norm,
+                                            const void* w_unembed, int V, float* h_out, float* logits_out,
+                                            int32_t* next_out, float* weights, void* workspace,
+                                            size_t workspace_bytes, spider_stream stream) {
+  clear_error();
+  SPIDER_TRY(validate_cfg(cfg));
+  SPIDER_REQUIRE(B >= 1 && T >= 1 && layers && lens, SPIDER_ERR_INVALID_ARG,
+                 "spider_decode_tree: B >= 1, T >= 1, layers and lens required");
+  SPIDER_REQUIRE(T <= 256 && (int64_t)B * T <= 65535, SPIDER_ERR_UNSUPPORTED,
+                 "spider_decode_tree: T <= 256 and B * T <= 65535");
+  SPIDER_REQUIRE(kv && kv->k && kv->v && kv->cap >= 1, SPIDER_ERR_INVALID_ARG,
+                 "spider_decode_tree: kv cache with k, v and cap >= 1 required");
+  SPIDER_REQUIRE(cfg->d / cfg->H <= kDecodeMaxDh && (cfg->d / cfg->H) % (cfg->dtype == SPIDER_BF16 ? 8 : 4) == 0,
+                 SPIDER_ERR_UNSUPPORTED, "spider_decode_tree: dh must be a multiple of 16 bytes and at most 256");
+  SPIDER_REQUIRE(((uintptr_t)kv->k % 16) == 0 && ((uintptr_t)kv->v % 16) == 0, SPIDER_ERR_UNSUPPORTED,
+                 "spider_decode_tree: cache must be 16-byte aligned");
+  // the mask and the depths come first: they check the parents
+  const int W = (T + 63) / 64, R = B * T;
+  std::vector<int32_t> chain;
+  if (!parents) {
+    chain.resize(R);
+    for (int r = 0; r < R; ++r) chain[r] = r % T - 1;
+    parents = chain.data();
+  }
+  std::vector<uint64_t> mask((size_t)R * W);
+  std::vector<int32_t> depth(R), tab(tree_tab_ints(B, T), 0);
+  SPIDER_TRY(spider_tree_mask(B, T, parents, mask.data(), depth.data()));
+  for (int b = 0; b < B; ++b) {
+    int live = 0;
+    while (live < T && parents[b * T + live] != -2) ++live;
+    SPIDER_REQUIRE(lens[b] >= 0 && lens[b] <= kv->cap - live, SPIDER_ERR_SHAPE,
+                   "spider_decode_tree: lens[%d] = %d and %d nodes do not fit %d slots", b, lens[b], live, kv->cap);
+    const int p0 = pos ? pos[b] : lens[b];
+    SPIDER_REQUIRE(p0 >= 0 && p0 <= 0x7fffffff - 256, SPIDER_ERR_SHAPE, "spider_decode_tree: pos[%d] = %d", b, p0);
+    for (int t = 0; t < T; ++t) {
+      const int r = b * T + t;
+      tab[r] = r;
+      tab[R + r] = p0 + depth[r];
+      tab[2 * R + r] = t < live ? lens[b] + t : -1;
+    }
+    tab[3 * R + b] = lens[b];
+    tab[3 * R + B + b] = live;
+  }
+  std::memcpy(tab.data() + (((size_t)3 * R + 2 * B + 1) & ~(size_t)1), mask.data(), mask.size() * sizeof(uint64_t));
+  if (w_unembed) {
+    SPIDER_REQUIRE(V >= 1 && final_norm, SPIDER_ERR_INVALID_ARG,
+                   "spider_decode_tree: the LM head needs V >= 1 and final_norm");
+    SPIDER_REQUIRE(cfg->dtype != SPIDER_BF16 || V % 64 == 0, SPIDER_ERR_UNSUPPORTED,
+                   "spider_decode_tree: bf16 LM head needs V a multiple of 64");
+    SPIDER_REQUIRE(((uintptr_t)w_unembed % 16) == 0 && ((uintptr_t)final_norm % 16) == 0, SPIDER_ERR_UNSUPPORTED,
+                   "spider_decode_tree: w_unembed and final_norm must be 16-byte aligned");
+  }
+  SPIDER_TRY(validate_prefill_args(cfg, layers, x, h_out));
+  const int Vh = w_unembed ? V : 0;
+  const TreeStepWs need = tree_step_layout(*cfg, B, T, kv->cap, Vh, nullptr);
+  SPIDER_REQUIRE(need.attn_bytes > 0, SPIDER_ERR_UNSUPPORTED,
+                 "spider_decode_tree: sizes beyond spider_tree_attention's limits");
+  SPIDER_REQUIRE(workspace && workspace_bytes >= need.bytes, SPIDER_ERR_WORKSPACE,
+                 "spider_decode_tree: workspace of %zu bytes needed, %zu given", need.bytes, workspace_bytes);
+  SPIDER_REQUIRE(((uintptr_t)workspace % 256) == 0, SPIDER_ERR_WORKSPACE,
+                 "spider_decode_tree: workspace must be 256-byte aligned");
+  const TreeStepWs ws = tree_step_layout(*cfg, B, T, kv->cap, Vh, reinterpret_cast<char*>(workspace));
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (cfg->dtype == SPIDER_BF16)
+    return run_decode_tree<uint16_t>(*cfg, layers, B, T, tab, x, *kv, final_norm, w_unembed, Vh, h_out, logits_out,
+                                     next_out, weights, ws, st);
+  return run_decode_tree<float>(*cfg, layers, B, T, tab, x, *kv, final_norm, w_unembed, Vh, h_out, logits_out,
+                                next_out, weights, ws, st);
 }

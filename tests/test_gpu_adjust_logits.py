@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from oracle import drafting as od
-from tests.gpu_common import need_gpu
+from gpu_common import need_gpu
 
 pytestmark = pytest.mark.gpu
 
