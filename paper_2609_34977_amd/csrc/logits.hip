@@ -47,12 +47,34 @@ __device__ __forceinline__ void wave_best(float& v, int& i) {
   }
 }
 
-// One block per (piece of the vocabulary, row): the counts of the piece's tokens in
-// the row's history and the piece's biases in LDS, then one pass over the logits.
-template <typename LT>
+// VEC consecutive logits from p (aligned to VEC of them).
+template <typename LT, int VEC>
+__device__ __forceinline__ void load_logits(const LT* p, float* x) {
+  if constexpr (VEC == 1) {
+    if constexpr (sizeof(LT) == 4) x[0] = p[0];
+    else x[0] = bf16_bits_to_f32(p[0]);
+  } else if constexpr (sizeof(LT) == 4) {
+    const floatx4 v = *reinterpret_cast<const floatx4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v[i];
+  } else {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    x[0] = __uint_as_float(v.x << 16);
+    x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+    x[2] = __uint_as_float(v.y << 16);
+    x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+  }
+}
+
+// One block per (piece of the vocabulary, row): the counts of the piece's tokens in the
+// row's history and the places of its biases in LDS, then one pass over the logits, VEC
+// at a time (4 where the rows are aligned for it).  Every block reads the whole history
+// from L2, which is why the reads go eight at a time.
+template <typename LT, int VEC>
 __global__ void __launch_bounds__(kAdjThreads) adjust_kernel(AdjustArgs a) {
   __shared__ uint32_t count[kAdjPiece];
-  __shared__ float bias[kAdjPiece];
+  __shared__ int32_t entry[kAdjPiece];  // first bias entry of a token
+  __shared__ int twice;                 // some token has several
   __shared__ float bv[kAdjThreads / 64];
   __shared__ int bi[kAdjThreads / 64];
   const int row = blockIdx.y, b = row / a.T, t = row - b * a.T;
@@ -60,19 +82,28 @@ __global__ void __launch_bounds__(kAdjThreads) adjust_kernel(AdjustArgs a) {
   const int nn = a.n_nodes ? min(max(a.n_nodes[b], 0), a.T) : a.T;
   if (t >= nn) return;
   const int v0 = blockIdx.x * kAdjPiece, nv = min(kAdjPiece, a.V - v0);
-  for (int i = tid; i < nv; i += kAdjThreads) {
-    count[i] = 0;
-    bias[i] = 0.f;
+  constexpr int kNone = 0x7fffffff;
+  for (int i = tid; i < kAdjPiece / 4; i += kAdjThreads) {
+    reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+    if (a.n_bias) reinterpret_cast<int4*>(entry)[i] = make_int4(kNone, kNone, kNone, kNone);
   }
+  if (tid == 0) twice = 0;
   __syncthreads();
   if (a.history) {
     const int n = min(max(a.n_history[b], 0), (int)a.hs), np = a.n_prompt ? a.n_prompt[b] : 0;
     const int32_t* h = a.history + b * a.hs;
-    for (int i = tid; i < n; i += kAdjThreads) {
-      const uint32_t v = (uint32_t)h[i] - (uint32_t)v0;
-      if (v < (uint32_t)nv) {
-        if (i < np) atomicOr(&count[v], kSeen);
-        else atomicAdd(&count[v], 1u);
+    for (int i0 = tid; i0 < n; i0 += 8 * kAdjThreads) {
+      int32_t id[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) id[u] = h[min(i0 + u * kAdjThreads, n - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u * kAdjThreads;
+        const uint32_t v = (uint32_t)id[u] - (uint32_t)v0;
+        if (i < n && v < (uint32_t)nv) {
+          if (i < np) atomicOr(&count[v], kSeen);
+          else atomicAdd(&count[v], 1u);
+        }
       }
     }
   }
@@ -86,39 +117,63 @@ __global__ void __launch_bounds__(kAdjThreads) adjust_kernel(AdjustArgs a) {
     }
   }
   const int32_t* ids = a.bias_ids + (int64_t)b * a.n_bias;
+  const float* bias = a.bias + (int64_t)b * a.n_bias;
   for (int i = tid; i < a.n_bias; i += kAdjThreads) {
-    const int id = ids[i];
-    const uint32_t v = (uint32_t)id - (uint32_t)v0;
-    if (v >= (uint32_t)nv) continue;
-    // the first entry of an id adds up all of them, in order
-    bool first = true;
-    for (int j = 0; j < i && first; ++j) first = ids[j] != id;
-    if (!first) continue;
-    float s = 0.f;
-    for (int j = i; j < a.n_bias; ++j)
-      if (ids[j] == id) s = __fadd_rn(s, a.bias[(int64_t)b * a.n_bias + j]);
-    bias[v] = s;
+    const uint32_t v = (uint32_t)ids[i] - (uint32_t)v0;
+    if (v < (uint32_t)nv && atomicMin(&entry[v], i) != kNone) twice = 1;
   }
-  __syncthreads();
   const float rep = a.rep ? a.rep[b] : 1.f, freq = a.freq ? a.freq[b] : 0.f, pres = a.pres ? a.pres[b] : 0.f;
   const LT* x = reinterpret_cast<const LT*>(a.logits) + row * a.ls + v0;
   float* o = a.out ? a.out + row * a.os + v0 : nullptr;
   const uint32_t* m = a.mask ? a.mask + row * a.ms + (v0 >> 5) : nullptr;
   float best = -INFINITY;
   int arg = 0x7fffffff;
-  for (int i = tid; i < nv; i += kAdjThreads) {
-    float z;
-    if constexpr (sizeof(LT) == 4) z = x[i];
-    else z = bf16_bits_to_f32(x[i]);
-    const uint32_t c = count[i];
-    if (c) z = z > 0.f ? __fdiv_rn(z, rep) : __fmul_rn(z, rep);
-    if (c & ~kSeen) z = __fsub_rn(__fsub_rn(z, __fmul_rn(freq, (float)(c & ~kSeen))), pres);
-    if (a.n_bias) z = __fadd_rn(z, bias[i]);
-    if (m && !((m[i >> 5] >> (i & 31)) & 1u)) z = -INFINITY;
-    if (o) o[i] = z;
-    if (z > best) {
-      best = z;
-      arg = v0 + i;
+  __syncthreads();
+  const bool again = twice != 0;
+  constexpr int UN = VEC == 4 ? 4 : 8;  // loads in flight
+  for (int i0 = VEC * tid; i0 < nv; i0 += UN * VEC * kAdjThreads) {
+    float z[UN][VEC];
+    uint32_t word[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int i = i0 + u * VEC * kAdjThreads;
+      if (i < nv) {
+        load_logits<LT, VEC>(x + i, z[u]);
+        word[u] = m ? m[i >> 5] : ~0u;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int i = i0 + u * VEC * kAdjThreads;
+      if (i >= nv) break;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const uint32_t c = count[i + e];
+        float y = z[u][e];
+        if (c) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+        if (c & ~kSeen) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, (float)(c & ~kSeen))), pres);
+        if (a.n_bias) {
+          const int k = entry[i + e];
+          float add = 0.f;
+          if (k != kNone) {
+            add = bias[k];
+            if (again)  // the other entries of the token, in order
+              for (int j = k + 1; j < a.n_bias; ++j)
+                if (ids[j] == v0 + i + e) add = __fadd_rn(add, bias[j]);
+          }
+          y = __fadd_rn(y, add);
+        }
+        if (!((word[u] >> ((i + e) & 31)) & 1u)) y = -INFINITY;
+        z[u][e] = y;
+        if (y > best) {
+          best = y;
+          arg = v0 + i + e;
+        }
+      }
+      if (o) {
+        if constexpr (VEC == 4) *reinterpret_cast<floatx4*>(o + i) = floatx4{z[u][0], z[u][1], z[u][2], z[u][3]};
+        else o[i] = z[u][0];
+      }
     }
   }
   if (!a.next) return;
@@ -205,8 +260,17 @@ extern "C" spider_status spider_adjust_logits(
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_ADJUST_LOGITS, st);
   const dim3 grid((unsigned)a.pieces, (unsigned)(B * T));
-  if (dtype == SPIDER_BF16) adjust_kernel<uint16_t><<<grid, kAdjThreads, 0, st>>>(a);
-  else adjust_kernel<float><<<grid, kAdjThreads, 0, st>>>(a);
+  // four logits at a time where every row starts on a 16-byte (bf16: 8-byte) boundary and has a multiple of 4
+  const uintptr_t four = dtype == SPIDER_BF16 ? 7 : 15;
+  const bool vec = V % 4 == 0 && logits_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(logits) & four) == 0 &&
+                   (!out || (out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0));
+  if (dtype == SPIDER_BF16) {
+    if (vec) adjust_kernel<uint16_t, 4><<<grid, kAdjThreads, 0, st>>>(a);
+    else adjust_kernel<uint16_t, 1><<<grid, kAdjThreads, 0, st>>>(a);
+  } else {
+    if (vec) adjust_kernel<float, 4><<<grid, kAdjThreads, 0, st>>>(a);
+    else adjust_kernel<float, 1><<<grid, kAdjThreads, 0, st>>>(a);
+  }
   SPIDER_LAUNCHED("adjust_logits");
   if (next_out) {
     adjust_join_kernel<<<(unsigned)(B * T), 64, 0, st>>>(a);
