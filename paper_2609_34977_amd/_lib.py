@@ -8,6 +8,7 @@ library is missing the import of any function raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -462,23 +463,49 @@ def decode_step(cfg: DecoderCfg, weights, lens, x: torch.Tensor, kv: dict, final
 
 
 # ----------------------------------------------------------------- drafting over the cache
+# (a decode step makes these calls many times, each a few microseconds of device work: the
+# stream handle comes from torch without a Stream object around it, sizes are kept by
+# their arguments, and a workspace is one allocation, which torch aligns to 512 bytes)
 def _on(dev, fn, *args):
     """Calls fn(*args, stream) on torch's current stream of ``dev``, with ``dev`` current."""
     if dev.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev.index)))
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, torch.cuda.current_stream(dev).cuda_stream))
+            _check(fn(*args, torch._C._cuda_getCurrentRawStream(dev.index)))
 
 
 def _need(t: Optional[torch.Tensor], name: str, dtype, shape, dev):
     """Device pointer (None for None) of a contiguous tensor of that dtype and shape on dev."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != dev or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {dev}, got {t.dtype} "
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=1024)
+def _size(name: str, *args) -> int:
+    return getattr(lib(), name)(*args)
+
+
+def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev):
+    """(tensor to keep until the call, 256-byte aligned pointer) of nbytes of workspace."""
+    if workspace is not None:
+        if workspace.device != dev or workspace.numel() * workspace.element_size() < nbytes + 256:
+            raise ValueError(f"workspace must hold {nbytes + 256} bytes on {dev}")
+        return workspace, (workspace.data_ptr() + 255) // 256 * 256
+    if nbytes == 0:
+        return None, None
+    workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    return workspace, workspace.data_ptr()
+
+
+def _gpu(t: torch.Tensor):
+    if not t.is_cuda:
+        raise ValueError("the tensors must be on a GPU")
+    return t.device
 
 
 def tree_mask(parents):
@@ -509,7 +536,7 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torc
         raise ValueError("q must be [B, T, H, dh], k and v [B, cap, Hkv, dh]")
     B, T, H, dh = q.shape
     cap, Hkv = k.shape[1], k.shape[2]
-    dev = q.device
+    dev = _gpu(q)
     if k.shape[0] != B or k.shape[3] != dh or v.shape != k.shape or v.stride() != k.stride():
         raise ValueError("k and v must be [B, cap, Hkv, dh] alike, with the B and dh of q")
     if k.dtype != q.dtype or v.dtype != q.dtype or k.device != dev or v.device != dev:
@@ -520,19 +547,15 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torc
         out = torch.empty(B, T, H, dh, dtype=q.dtype, device=dev)
     dt = _dt(q)
     L = lib()
-    weighted = weights_out is not None
-    wsz = L.spider_tree_attention_workspace_size(B, T, H, Hkv, dh, cap, dt, weighted)
-    if workspace is None:
-        workspace = _ws(wsz, dev)
-    elif workspace.device != dev or workspace.numel() * workspace.element_size() < wsz + 256:
-        raise ValueError(f"workspace must hold {wsz + 256} bytes on {dev}")
+    wsz = _size("spider_tree_attention_workspace_size", B, T, H, Hkv, dh, cap, dt, weights_out is not None)
+    workspace, wptr = _scratch(workspace, wsz, dev)
     _on(dev, L.spider_tree_attention, B, T, H, Hkv, dh, q.data_ptr(), q.stride(0), q.stride(1), k.data_ptr(),
         v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), cap, _need(lens, "lens", torch.int32, (B,), dev),
         _need(n_nodes, "n_nodes", torch.int32, (B,), dev),
         _need(tree_mask, "tree_mask", torch.int64, (B, T, (T + 63) // 64), dev), dt,
         dh ** -0.5 if scale is None else scale, _need(out, "out", q.dtype, (B, T, H, dh), dev),
         _need(weights_in, "weights_in", torch.float32, (B, Hkv, cap), dev),
-        _need(weights_out, "weights_out", torch.float32, (B, Hkv, cap), dev), _aligned(workspace), wsz)
+        _need(weights_out, "weights_out", torch.float32, (B, Hkv, cap), dev), wptr, wsz)
     return out
 
 
@@ -548,7 +571,7 @@ def decode_tree(cfg: DecoderCfg, weights, lens, x: torch.Tensor, kv: dict, paren
     if _dt(x) != cfg.dtype:
         raise ValueError("x must have the decoder's dtype")
     B, T, d = x.shape
-    dev = x.device
+    dev = _gpu(x)
     cap = kv["desc"].cap
     if tuple(kv["k"].shape) != (cfg.L, B, cap, d):
         raise ValueError(f"the cache must be [{cfg.L}, {B}, cap, {d}]")
@@ -580,7 +603,7 @@ def cache_select(weights: torch.Tensor, lens: torch.Tensor, keep: int, *, n_firs
     if weights.dim() != 4:
         raise ValueError("weights must be [L, B, Hkv, cap]")
     L_, B, Hkv, cap = weights.shape
-    dev = weights.device
+    dev = _gpu(weights)
     if keep < 1:
         raise ValueError("keep must be at least 1")
     idx = torch.empty(L_, B, 1 if shared else Hkv, keep, dtype=torch.int32, device=dev)
@@ -606,7 +629,7 @@ def cache_compact(k: torch.Tensor, v: torch.Tensor, idx: torch.Tensor, count: Op
     k_out, v_out = (k, v) if k_out is None else (k_out, v_out)
     L_, B, cap, Hkv, dh = k.shape
     cap_out = k_out.shape[2] if k_out.dim() == 5 else -1
-    dev = k.device
+    dev = _gpu(k)
     if k_out.shape != (L_, B, cap_out, Hkv, dh) or v.shape != k.shape or v_out.shape != k_out.shape:
         raise ValueError("the caches must be [L, B, cap, Hkv, dh] alike but for cap")
     if v.stride() != k.stride() or v_out.stride() != k_out.stride() or k.stride(4) != 1 or k_out.stride(4) != 1:
@@ -622,7 +645,7 @@ def cache_compact(k: torch.Tensor, v: torch.Tensor, idx: torch.Tensor, count: Op
     si = (ctypes.c_int64 * 4)(*k.stride()[:4])
     so = (ctypes.c_int64 * 4)(*k_out.stride()[:4])
     _on(dev, lib().spider_cache_compact, L_, B, Hkv, dh, _dt(k), k.data_ptr(), v.data_ptr(), si, cap,
-        k_out.data_ptr(), v_out.data_ptr(), so, cap_out, _need(idx, "idx", torch.int32, tuple(idx.shape), dev),
+        k_out.data_ptr(), v_out.data_ptr(), so, cap_out, _need(idx, "idx", torch.int32, idx.shape, dev),
         idx.shape[0], idx.shape[2], idx.shape[3], _need(count, "count", torch.int32, (B,), dev),
         _need(base, "base", torch.int32, (B,), dev), _need(weights, "weights", torch.float32, (L_, B, Hkv, cap), dev),
         _need(weights_out, "weights_out", torch.float32, (L_, B, Hkv, cap_out), dev))
@@ -648,7 +671,7 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
     if x.dim() != 3 or x.stride(2) != 1 or (min(x.shape[:2]) > 1 and x.stride(0) != x.shape[1] * x.stride(1)):
         raise ValueError("logits must be [B, T, V] or [B, V] with contiguous rows at one distance")
     B, T, V = x.shape
-    dev = logits.device
+    dev = _gpu(logits)
     row = x.stride(1) if T > 1 or B == 1 else x.stride(0)
     row = max(row, V) if B * T == 1 else row
     lead = (B,) if flat else (B, T)
@@ -671,11 +694,8 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
         ms = words
         mask = mask.unsqueeze(1) if flat and mask.dim() == 2 else mask
     L = lib()
-    wsz = L.spider_adjust_logits_workspace_size(B, T, V)
-    if workspace is None:
-        workspace = _ws(wsz, dev)
-    elif workspace.device != dev or workspace.numel() * workspace.element_size() < wsz + 256:
-        raise ValueError(f"workspace must hold {wsz + 256} bytes on {dev}")
+    wsz = _size("spider_adjust_logits_workspace_size", B, T, V)
+    workspace, wptr = _scratch(workspace, wsz, dev)
     i32, f32 = torch.int32, torch.float32
     _on(dev, L.spider_adjust_logits, B, T, V, logits.data_ptr(), row, _dt(logits),
         _need(history, "history", i32, (B, n), dev), n, _need(n_history, "n_history", i32, (B,), dev),
@@ -687,7 +707,7 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
         _need(bias, "bias", f32, (B, nb), dev), nb,
         _need(mask, "mask", i32, (B, T, words) if ms else (words,), dev), ms,
         logits.data_ptr() if inplace else _need(out, "out", f32, lead + (V,), dev), row if inplace else V,
-        _need(next_ids, "next_ids", i32, lead, dev), _aligned(workspace), wsz)
+        _need(next_ids, "next_ids", i32, lead, dev), wptr, wsz)
     return out, next_ids
 
 
