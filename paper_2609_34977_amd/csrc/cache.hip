@@ -8,9 +8,6 @@
 namespace spider {
 namespace {
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelWaves = kSelThreads / 64;
-
 struct SelectArgs {
   const float* w;  // [L][B][Hkv][cap]
   const int32_t* lens;
@@ -19,28 +16,39 @@ struct SelectArgs {
   int L, B, Hkv, G, cap, keep, n_first, n_last;
 };
 
-// Order of slot j of one row of n slots: the slots that are always kept above every
-// weight, NaN like -inf, -0 like +0.
-__device__ __forceinline__ uint32_t slot_key(const SelectArgs& a, const float* w, int j, int n) {
-  if (j < a.n_first || j >= n - a.n_last) return 0xFFFFFFFFu;
-  float x;
-  if (a.G == a.Hkv) {
-    x = w[j];
-  } else {
-    double s = 0.0;  // over the heads in order
-    for (int h = 0; h < a.Hkv; ++h) s += (double)w[(int64_t)h * a.cap + j];
-    x = (float)s;
-  }
-  return float_order_key(x != x ? -INFINITY : x);
+// Weight of slot j: its own, or added over the heads in order.
+__device__ __forceinline__ float slot_weight(const SelectArgs& a, const float* w, int j) {
+  if (a.G == a.Hkv) return w[j];
+  double s = 0.0;
+  for (int h = 0; h < a.Hkv; ++h) s += (double)w[(int64_t)h * a.cap + j];
+  return (float)s;
 }
 
-// One block per (layer, sample, head group): the keep-th largest key byte by byte
-// from a histogram of the keys that share the bytes found so far, then the kept
-// slots in ascending order.
-__global__ void __launch_bounds__(kSelThreads) cache_select_kernel(SelectArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t found[2];  // byte, keys still wanted within it
-  __shared__ uint2 tot[kSelWaves];
+// Order of slot j of a row of n slots: the slots that are always kept above every
+// weight, NaN like -inf (0x007FFFFF), -0 like +0; 0 past the last slot.
+__device__ __forceinline__ uint32_t slot_key(const SelectArgs& a, float x, int j, int n) {
+  const uint32_t k = j < a.n_first || j >= n - a.n_last ? 0xFFFFFFFFu : float_order_key(x != x ? -INFINITY : x);
+  return j < n ? k : 0u;
+}
+
+constexpr int kSelBits = 11;  // of a key per pass: 32 = 11 + 11 + 10
+constexpr int kSelBuckets = 1 << kSelBits;
+
+// One block per (layer, sample, head group): the keep-th largest key by a histogram of
+// its upper bits, then of the next bits of the keys that share those, then of the rest;
+// then the kept slots in ascending order.  Wave w owns 64 * NV consecutive slots, so that
+// after one exchange of counts every wave writes its slots without a barrier.  The keys
+// stay in registers (NV > 0, up to 64 per lane: n <= THREADS * NV); longer rows are read
+// again in each pass (NV = 0).
+// Bound by the barriers and the LDS atomics of its passes (a row is read once): weights
+// crowd in few exponents, and often in one value (slots that no query looked at), hence
+// eleven bits at once, and one add per wave for the lanes that share the first lane's bucket.
+template <int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ uint32_t hist[kSelBuckets];
+  __shared__ uint32_t found[2];  // bucket, keys still wanted within it
+  __shared__ uint2 tot[WAVES];
   const int row = blockIdx.x;  // (l * B + b) * G + g
   const int g = row % a.G, lb = row / a.G, b = lb % a.B;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -49,55 +57,110 @@ __global__ void __launch_bounds__(kSelThreads) cache_select_kernel(SelectArgs a)
   int32_t* idx = a.idx + (int64_t)row * a.keep;
   if (lb == b && g == 0 && tid == 0) a.len_out[b] = min(n, a.keep);
   if (n <= a.keep) {
-    for (int i = tid; i < a.keep; i += kSelThreads) idx[i] = i < n ? i : -1;
+    for (int i = tid; i < a.keep; i += THREADS) idx[i] = i < n ? i : -1;
     return;
   }
-  uint32_t prefix = 0, want = (uint32_t)a.keep;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += kSelThreads) {
-      const uint32_t k = slot_key(a, w, j, n);
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+  const int nv = NV ? NV : (n + THREADS - 1) / THREADS;  // 64-slot pieces of a wave
+  const int j0 = wave * nv * 64 + lane;
+  uint32_t keys[NV ? NV : 1];
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int i0 = 0; i0 < NV; i0 += 16) {  // 16 loads in flight
+#pragma unroll
+      for (int i = i0; i < i0 + 16; ++i) keys[i] = __float_as_uint(slot_weight(a, w, min(j0 + 64 * i, n - 1)));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = i0; i < i0 + 16; ++i) keys[i] = slot_key(a, __uint_as_float(keys[i]), j0 + 64 * i, n);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
-    if (tid == 0) {
-      uint32_t left = want;
-      int v = 255;
-      while (hist[v] < left) left -= hist[v--];
-      found[0] = (uint32_t)v;
-      found[1] = left;
-    }
-    __syncthreads();
-    prefix = (prefix << 8) | found[0];
-    want = found[1];
-    __syncthreads();
   }
-  // all slots above the key `prefix`, and the first `want` slots that equal it
-  uint32_t above = 0, equal = 0;
-  for (int j0 = 0; j0 < n; j0 += kSelThreads) {
-    const int j = j0 + tid;
-    const uint32_t k = j < n ? slot_key(a, w, j, n) : 0u;
-    const bool gt = j < n && k > prefix, eq = j < n && k == prefix;
-    const uint64_t mg = __ballot(gt), me = __ballot(eq);
-    if (lane == 0) tot[wave] = make_uint2(__popcll(mg), __popcll(me));
-    __syncthreads();
-    uint32_t ga = above, ea = equal;
-    for (int v = 0; v < kSelWaves; ++v) {
-      const uint2 c = tot[v];
-      above += c.x;
-      equal += c.y;
-      if (v < wave) {
-        ga += c.x;
-        ea += c.y;
+  // f(key, slot) for every slot of the wave in ascending pieces
+  auto each = [&](auto&& f) {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) f(keys[i], j0 + 64 * i);
+    } else {
+      for (int i0 = 0; i0 < nv; i0 += 8) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = slot_weight(a, w, min(j0 + 64 * (i0 + i), n - 1));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i0 + i < nv) f(slot_key(a, x[i], j0 + 64 * (i0 + i), n), j0 + 64 * (i0 + i));
       }
     }
-    const uint64_t below = (1ull << lane) - 1ull;
-    ga += __popcll(mg & below);
-    ea += __popcll(me & below);
-    if (gt || (eq && ea < want)) idx[ga + min(ea, want)] = j;
+  };
+  uint32_t prefix = 0, want = (uint32_t)a.keep;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
+    for (int i = tid; i < kSelBuckets; i += THREADS) hist[i] = 0;
     __syncthreads();
+    each([&](uint32_t k, int) {
+      const bool on = pass == 0 ? k != 0 : (k >> (shift + bits)) == prefix;
+      const uint64_t active = __ballot(on);
+      if (active == 0) return;
+      const uint32_t bucket = (k >> shift) & ((1u << bits) - 1u);
+      const int leader = __ffsll((unsigned long long)active) - 1;
+      const bool same = on && bucket == (uint32_t)__builtin_amdgcn_readlane((int)bucket, leader);
+      const uint64_t group = __ballot(same);
+      if (lane == leader) atomicAdd(&hist[bucket], (uint32_t)__popcll(group));
+      else if (on && !same) atomicAdd(&hist[bucket], 1u);
+    });
+    __syncthreads();
+    if (wave == 0) {
+      // lane l: the sum of 32 buckets, highest first; then the 32 of the lane where the count is reached
+      uint32_t s = 0;
+      const int top = kSelBuckets - 1 - 32 * lane;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s += hist[top - ((i + lane) & 31)];
+      uint32_t up = s;  // inclusive prefix over the lanes
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(up, o, 64);
+        if (lane >= o) up += y;
+      }
+      const int at = __ffsll((unsigned long long)__ballot(up >= want)) - 1;
+      const uint32_t left = want - (uint32_t)__shfl((int)(up - s), at, 64);
+      const uint32_t c = lane < 32 ? hist[kSelBuckets - 1 - 32 * at - lane] : 0u;
+      uint32_t in = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up(in, o, 64);
+        if (lane >= o) in += y;
+      }
+      const int v = __ffsll((unsigned long long)__ballot(lane < 32 && in >= left)) - 1;
+      if (lane == v) {
+        found[0] = (uint32_t)(kSelBuckets - 1 - 32 * at - lane);
+        found[1] = left - (in - c);
+      }
+    }
+    __syncthreads();
+    prefix = __builtin_amdgcn_readfirstlane((prefix << bits) | found[0]);
+    want = __builtin_amdgcn_readfirstlane(found[1]);
   }
+  // all slots above the key `prefix`, and the first `want` slots that equal it
+  uint32_t gt = 0, eq = 0;
+  each([&](uint32_t k, int) {
+    gt += __popcll(__ballot(k > prefix));
+    eq += __popcll(__ballot(k == prefix));
+  });
+  asm volatile("" : "+s"(prefix));  // the comparisons below are made again, not kept in 4 * NV registers
+  if (lane == 0) tot[wave] = make_uint2(gt, eq);
+  __syncthreads();
+  gt = eq = 0;
+  for (int v = 0; v < wave; ++v) {
+    gt += tot[v].x;
+    eq += tot[v].y;
+  }
+  const uint64_t below = (1ull << lane) - 1ull;
+  each([&](uint32_t k, int j) {
+    const uint64_t mg = __ballot(k > prefix), me = __ballot(k == prefix);
+    const uint32_t ga = gt + __popcll(mg & below), ea = eq + __popcll(me & below);
+    if (k > prefix || (k == prefix && ea < want)) idx[ga + min(ea, want)] = j;
+    gt += __popcll(mg);
+    eq += __popcll(me);
+  });
 }
 
 struct CompactArgs {
@@ -199,11 +262,17 @@ extern "C" spider_status spider_cache_select(int L, int B, int Hkv, int cap, con
                  "spider_cache_select: n_first + n_last = %lld exceed keep = %d", (long long)n_first + n_last, keep);
   SPIDER_REQUIRE(keep <= cap, SPIDER_ERR_SHAPE, "spider_cache_select: keep = %d exceeds cap = %d", keep, cap);
   const int G = shared ? 1 : Hkv;
-  SPIDER_REQUIRE((int64_t)L * B * G <= 0x7fffffff, SPIDER_ERR_UNSUPPORTED, "spider_cache_select: too many rows");
+  SPIDER_REQUIRE((int64_t)L * B * G < (1 << 22), SPIDER_ERR_UNSUPPORTED,
+                 "spider_cache_select: layers * samples * head groups must be below 2^22");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_CACHE_SELECT, st);
   const SelectArgs a{weights, lens, idx_out, len_out, L, B, Hkv, G, cap, keep, n_first, n_last};
-  cache_select_kernel<<<(unsigned)(L * B * G), kSelThreads, 0, st>>>(a);
+  // the smallest block whose registers hold a row
+  const unsigned rows = (unsigned)(L * B * G);
+  if (cap <= 256 * 16) cache_select_kernel<256, 16><<<rows, 256, 0, st>>>(a);
+  else if (cap <= 1024 * 16) cache_select_kernel<1024, 16><<<rows, 1024, 0, st>>>(a);
+  else if (cap <= 1024 * 64) cache_select_kernel<1024, 64><<<rows, 1024, 0, st>>>(a);
+  else cache_select_kernel<1024, 0><<<rows, 1024, 0, st>>>(a);
   SPIDER_LAUNCHED("cache_select");
   return SPIDER_OK;
 }
