@@ -20,7 +20,14 @@ struct SelectArgs {
 __device__ __forceinline__ float slot_weight(const SelectArgs& a, const float* w, int j) {
   if (a.G == a.Hkv) return w[j];
   double s = 0.0;
-  for (int h = 0; h < a.Hkv; ++h) s += (double)w[(int64_t)h * a.cap + j];
+  for (int h0 = 0; h0 < a.Hkv; h0 += 4) {  // four loads in flight
+    float x[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) x[h] = w[(int64_t)min(h0 + h, a.Hkv - 1) * a.cap + j];
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      if (h0 + h < a.Hkv) s += (double)x[h];
+  }
   return (float)s;
 }
 
@@ -29,6 +36,17 @@ __device__ __forceinline__ float slot_weight(const SelectArgs& a, const float* w
 __device__ __forceinline__ uint32_t slot_key(const SelectArgs& a, float x, int j, int n) {
   const uint32_t k = j < a.n_first || j >= n - a.n_last ? 0xFFFFFFFFu : float_order_key(x != x ? -INFINITY : x);
   return j < n ? k : 0u;
+}
+
+// Sum over this lane and the lower ones: within rows of 16 lanes, then across them.
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);  // row_shr:1, 2, 4, 8
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1 and 3
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2 and 3
+  return v;
 }
 
 constexpr int kSelBits = 11;  // of a key per pass: 32 = 11 + 11 + 10
@@ -61,7 +79,7 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
     return;
   }
   const int nv = NV ? NV : (n + THREADS - 1) / THREADS;  // 64-slot pieces of a wave
-  const int j0 = wave * nv * 64 + lane;
+  int j0 = wave * nv * 64 + lane;
   uint32_t keys[NV ? NV : 1];
   if constexpr (NV > 0) {
 #pragma unroll
@@ -78,7 +96,9 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
   auto each = [&](auto&& f) {
     if constexpr (NV > 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) f(keys[i], j0 + 64 * i);
+      for (int i = 0; i < NV; ++i) {
+        f(keys[i], j0 + 64 * i);
+      }
     } else {
       for (int i0 = 0; i0 < nv; i0 += 8) {
         float x[8];
@@ -97,7 +117,8 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
     for (int i = tid; i < kSelBuckets; i += THREADS) hist[i] = 0;
     __syncthreads();
     each([&](uint32_t k, int) {
-      const bool on = pass == 0 ? k != 0 : (k >> (shift + bits)) == prefix;
+      // (in the first pass all, also the zeros past the last slot: no search goes down to their bucket)
+      const bool on = (k >> (shift + bits - 1)) >> 1 == prefix;
       const uint64_t active = __ballot(on);
       if (active == 0) return;
       const uint32_t bucket = (k >> shift) & ((1u << bits) - 1u);
@@ -114,21 +135,11 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
       const int top = kSelBuckets - 1 - 32 * lane;
 #pragma unroll
       for (int i = 0; i < 32; ++i) s += hist[top - ((i + lane) & 31)];
-      uint32_t up = s;  // inclusive prefix over the lanes
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(up, o, 64);
-        if (lane >= o) up += y;
-      }
+      const uint32_t up = wave_prefix(s);
       const int at = __ffsll((unsigned long long)__ballot(up >= want)) - 1;
-      const uint32_t left = want - (uint32_t)__shfl((int)(up - s), at, 64);
+      const uint32_t left = want - (uint32_t)__builtin_amdgcn_readlane((int)(up - s), at);
       const uint32_t c = lane < 32 ? hist[kSelBuckets - 1 - 32 * at - lane] : 0u;
-      uint32_t in = c;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up(in, o, 64);
-        if (lane >= o) in += y;
-      }
+      const uint32_t in = wave_prefix(c);
       const int v = __ffsll((unsigned long long)__ballot(lane < 32 && in >= left)) - 1;
       if (lane == v) {
         found[0] = (uint32_t)(kSelBuckets - 1 - 32 * at - lane);
@@ -145,7 +156,8 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
     gt += __popcll(__ballot(k > prefix));
     eq += __popcll(__ballot(k == prefix));
   });
-  asm volatile("" : "+s"(prefix));  // the comparisons below are made again, not kept in 4 * NV registers
+  // the comparisons and slots below are made again, not kept in 3 * NV registers
+  asm volatile("" : "+s"(prefix), "+v"(j0));
   if (lane == 0) tot[wave] = make_uint2(gt, eq);
   __syncthreads();
   gt = eq = 0;

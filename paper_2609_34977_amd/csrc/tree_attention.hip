@@ -367,75 +367,55 @@ __device__ __forceinline__ int tree_splits(const TreeArgs& a, int tiles) {
 // rescaled: the exponentials then stay below 2^8.
 constexpr float kLazyMax = 8.f;
 
-// grid: row groups x units (sample, kv head, split), see tree_place; 4 waves, wave w
-// takes tiles w, w + 4, .. of the block's split; their sums meet in LDS.
-template <typename AT, int DH, int RT, bool FULL>
-__global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_kernel(TreeArgs a) {
+// RT row tiles of a wave: queries, and the running maximum, sum and output of their rows.
+template <typename AT, int DH, int RT>
+struct RowTiles {
   using T = TreeTile<AT, DH>;
-  constexpr int KEYS = T::KEYS, KT = T::KT, CPL = T::CPL;
-  constexpr int ROWS = 16 * RT, LD = DH + 4;
-  __shared__ float xm[4][ROWS], xl[4][ROWS];
-  __shared__ float xo[4][ROWS][LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int m = lane & 15, g = lane >> 4;
-  // row groups of a unit lie 8 blocks apart: on the same XCD, whose L2 holds the unit's keys
-  const int slot = blockIdx.x >> 3;
-  const int unit = slot / a.groups * 8 + (blockIdx.x & 7), group = slot % a.groups;
-  if (unit >= a.B * a.Hkv * a.splits) return;
-  const int split = unit % a.splits, bh = unit / a.splits, b = bh / a.Hkv, hk = bh % a.Hkv;
-  const int G = a.H / a.Hkv;
-  const int2 ext = tree_extent(a, b);
-  const int n = ext.x + ext.y, R = ext.y * G, r0 = group * ROWS;
-  if (r0 >= R) return;
-  const int tiles = (n + KEYS - 1) / KEYS, ns = tree_splits(a, tiles);
-  if (split >= ns) return;
-  const int per = (tiles + ns - 1) / ns, t0 = split * per, t1 = min(tiles, t0 + per);
-  const AT* kb = reinterpret_cast<const AT*>(a.k) + b * a.kvb + hk * a.kvh;
-  const AT* vb = reinterpret_cast<const AT*>(a.v) + b * a.kvb + hk * a.kvh;
-  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  static constexpr int KEYS = T::KEYS, NS = 4 * T::KT, CPL = T::CPL;  // NS: scores of a lane and row tile
   typename T::Q q[RT];
   int node[RT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const int row = min(r0 + 16 * r + m, R - 1);
-    node[r] = row / G;
-    const AT* qp = reinterpret_cast<const AT*>(a.q) + b * a.qb + node[r] * a.qt + (int64_t)(hk * G + row % G) * a.dh;
-    T::template load_q<FULL>(q[r], qp, g, a.dh, a.scale < 0.f);
-  }
   floatx4 o[RT][CPL];
   float top[RT], sum[RT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    top[r] = -INFINITY;
-    sum[r] = 0.f;
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) o[r][c] = floatx4{};
-  }
-  typename T::K k;
-  typename T::V v;
-  if (t0 + wave < t1) T::template load_k<FULL>(k, kb, a.kvs, (t0 + wave) * KEYS, n, lane, a.dh);
-  auto step = [&](int t, auto tail_) {
-    constexpr bool tail = decltype(tail_)::value;  // some key is a node, or past the last one
-    const int j0 = t * KEYS;
-    T::template load_v<FULL>(v, vb, a.kvs, j0, n, lane, a.dh);
-    float p[RT][KT * 4];
+  float p[RT][NS];
+  uint32_t seen[RT];  // the lane's keys of the tile that its row sees, bit i for score i
+
+  template <bool FULL>
+  __device__ __forceinline__ void start(const TreeArgs& a, int b, int hk, int r0, int R, int lane) {
+    const int G = a.H / a.Hkv;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      floatx4 s[KT];
+      const int row = min(r0 + 16 * r + (lane & 15), R - 1);
+      node[r] = row / G;
+      const AT* qp = reinterpret_cast<const AT*>(a.q) + b * a.qb + node[r] * a.qt + (int64_t)(hk * G + row % G) * a.dh;
+      T::template load_q<FULL>(q[r], qp, lane >> 4, a.dh, a.scale < 0.f);
+      top[r] = -INFINITY;
+      sum[r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) o[r][c] = floatx4{};
+    }
+  }
+
+  __device__ __forceinline__ void scores(const typename T::K& k) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      floatx4 s[T::KT];
       T::scores(s, k, q[r]);
 #pragma unroll
-      for (int i = 0; i < KT * 4; ++i) p[r][i] = s[i / 4][i % 4];
+      for (int i = 0; i < NS; ++i) p[r][i] = s[i / 4][i % 4];
     }
-    if (t + 4 < t1) T::template load_k<FULL>(k, kb, a.kvs, j0 + 4 * KEYS, n, lane, a.dh);
-    uint32_t seen[RT];  // the lane's keys that its row sees, bit i for score i
+  }
+
+  // scores to weights, for the tile of keys from j0; tail: some key is a node, or past the last one
+  template <bool tail>
+  __device__ __forceinline__ void soften(const TreeArgs& a, int b, int j0, int2 ext, int g, float sc) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       seen[r] = ~0u;
       if constexpr (tail) {
         const uint32_t w = tree_window<KEYS>(a, b, node[r], j0, ext) >> (4 * g);
-        seen[r] = (w & 15u) | (KT == 2 ? (w >> 12) & 0xF0u : 0u);
+        seen[r] = (w & 15u) | (T::KT == 2 ? (w >> 12) & 0xF0u : 0u);
 #pragma unroll
-        for (int i = 0; i < KT * 4; ++i) p[r][i] = (seen[r] >> i) & 1u ? p[r][i] : -INFINITY;
+        for (int i = 0; i < NS; ++i) p[r][i] = (seen[r] >> i) & 1u ? p[r][i] : -INFINITY;
       }
     }
     bool grows = false;
@@ -444,7 +424,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_ker
     for (int r = 0; r < RT; ++r) {
       mx[r] = p[r][0];
 #pragma unroll
-      for (int i = 1; i < KT * 4; ++i) mx[r] = fmaxf(mx[r], p[r][i]);
+      for (int i = 1; i < NS; ++i) mx[r] = fmaxf(mx[r], p[r][i]);
       float2 x = lanes_x16(mx[r]);
       x = lanes_x32(fmaxf(x.x, x.y));
       mx[r] = fmaxf(x.x, x.y);
@@ -466,7 +446,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_ker
       const float mc = top[r] == -INFINITY ? 0.f : top[r] * sc;
       float s0 = 0.f;
 #pragma unroll
-      for (int i = 0; i < KT * 4; ++i) {
+      for (int i = 0; i < NS; ++i) {
         float e = __builtin_amdgcn_exp2f(fmaf(p[r][i], sc, -mc));
         if constexpr (tail) e = (seen[r] >> i) & 1u ? e : 0.f;
         p[r][i] = e;
@@ -474,70 +454,256 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_ker
       }
       sum[r] += s0;
     }
+  }
+
+  template <bool tail>
+  __device__ __forceinline__ void add(typename T::V& v) {
     if constexpr (tail) if (__any(T::nonfinite(v))) {
       // infinite and NaN values count for the rows that see them, and for no other (0 times
       // one of them is NaN): a product of its own for each kind, then they leave v
-      float on[RT][KT * 4];
+      float on[RT][NS];
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int i = 0; i < KT * 4; ++i) on[r][i] = (seen[r] >> i) & 1u ? 1.f : 0.f;
+        for (int i = 0; i < NS; ++i) on[r][i] = (seen[r] >> i) & 1u ? 1.f : 0.f;
 #pragma unroll 1
       for (int kind = 0; kind < 3; ++kind) T::template special<RT>(o, v, on, kind);
       T::drop_nonfinite(v);
     }
     T::template values<RT>(o, v, p);
+  }
+
+  // the row's sum, in every lane of its column
+  __device__ __forceinline__ float row_sum(int r) const {
+    float2 x = lanes_x16(sum[r]);
+    x = lanes_x32(x.x + x.y);
+    return x.x + x.y;
+  }
+};
+
+// What a block works on: a unit (sample, kv head, split of its keys) and a group of its
+// rows.  The row groups of a unit lie 8 blocks apart: on the same XCD, whose L2 then holds
+// the unit's keys and values.
+struct TreeWork {
+  int b, hk, bh, split, ns, r0, R, n, t0, t1;  // tiles [t0, t1) of the unit's keys
+  int2 ext;
+};
+template <int KEYS, int ROWS>
+__device__ __forceinline__ bool tree_work(const TreeArgs& a, TreeWork& w) {
+  const int slot = blockIdx.x >> 3;
+  const int unit = slot / a.groups * 8 + (blockIdx.x & 7);
+  if (unit >= a.B * a.Hkv * a.splits) return false;
+  w.split = unit % a.splits;
+  w.bh = unit / a.splits;
+  w.b = w.bh / a.Hkv;
+  w.hk = w.bh % a.Hkv;
+  w.ext = tree_extent(a, w.b);
+  w.n = w.ext.x + w.ext.y;
+  w.R = w.ext.y * (a.H / a.Hkv);
+  w.r0 = slot % a.groups * ROWS;
+  if (w.r0 >= w.R) return false;
+  const int tiles = (w.n + KEYS - 1) / KEYS;
+  w.ns = tree_splits(a, tiles);
+  if (w.split >= w.ns) return false;
+  const int per = (tiles + w.ns - 1) / w.ns;
+  w.t0 = w.split * per;
+  w.t1 = min(tiles, w.t0 + per);
+  return true;
+}
+
+// Few rows: bound by the reads of keys and values, which go straight from memory to the
+// registers of the wave that uses them, the next tile's keys on their way during the
+// softmax.  4 waves, wave w takes tiles w, w + 4, .. of the block's split; their sums meet
+// in LDS.
+template <typename AT, int DH, int RT, bool FULL>
+__global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_kernel(TreeArgs a) {
+  using Rows = RowTiles<AT, DH, RT>;
+  using T = typename Rows::T;
+  constexpr int KEYS = T::KEYS, CPL = T::CPL;
+  constexpr int ROWS = 16 * RT, LD = DH + 4;
+  __shared__ float xm[4][ROWS], xl[4][ROWS];
+  __shared__ float xo[4][ROWS][LD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int m = lane & 15, g = lane >> 4;
+  TreeWork w;
+  if (!tree_work<KEYS, ROWS>(a, w)) return;
+  const int b = w.b, n = w.n, G = a.H / a.Hkv;
+  const AT* kb = reinterpret_cast<const AT*>(a.k) + b * a.kvb + w.hk * a.kvh;
+  const AT* vb = reinterpret_cast<const AT*>(a.v) + b * a.kvb + w.hk * a.kvh;
+  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  Rows rows;
+  typename T::K k;
+  typename T::V v;
+  if (w.t0 + wave < w.t1) T::template load_k<FULL>(k, kb, a.kvs, (w.t0 + wave) * KEYS, n, lane, a.dh);
+  rows.template start<FULL>(a, b, w.hk, w.r0, w.R, lane);
+  auto step = [&](int t, auto tail_) {
+    constexpr bool tail = decltype(tail_)::value;
+    const int j0 = t * KEYS;
+    T::template load_v<FULL>(v, vb, a.kvs, j0, n, lane, a.dh);
+    rows.scores(k);
+    if (t + 4 < w.t1) T::template load_k<FULL>(k, kb, a.kvs, j0 + 4 * KEYS, n, lane, a.dh);
+    rows.template soften<tail>(a, b, j0, w.ext, g, sc);
+    rows.template add<tail>(v);
   };
-  int t = t0 + wave;
-  for (; t < min(t1, ext.x / KEYS); t += 4) step(t, std::false_type{});
-  for (; t < t1; t += 4) step(t, std::true_type{});
+  int t = w.t0 + wave;
+  for (; t < min(w.t1, w.ext.x / KEYS); t += 4) step(t, std::false_type{});
+  for (; t < w.t1; t += 4) step(t, std::true_type{});
 
   // the waves' sums onto their common maximum, in wave order
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    float2 x = lanes_x16(sum[r]);
-    x = lanes_x32(x.x + x.y);
+    const float l = rows.row_sum(r);
     if (g == 0) {
-      xm[wave][16 * r + m] = top[r];
-      xl[wave][16 * r + m] = x.x + x.y;
+      xm[wave][16 * r + m] = rows.top[r];
+      xl[wave][16 * r + m] = l;
     }
 #pragma unroll
     for (int c = 0; c < CPL; ++c)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) xo[wave][16 * r + m][T::channel(c, 4 * g + i)] = o[r][c][i];
+      for (int i = 0; i < 4; ++i) xo[wave][16 * r + m][T::channel(c, 4 * g + i)] = rows.o[r][c][i];
   }
   __syncthreads();
   constexpr int PER = 256 / ROWS >= 4 ? 256 / ROWS : 4;  // threads of a row
   const int c0 = 4 * (tid % PER);
-  for (int row = tid / PER; row < min(ROWS, R - r0); row += 256 / PER) {
+  for (int row = tid / PER; row < min(ROWS, w.R - w.r0); row += 256 / PER) {
     float mx = -INFINITY, l = 0.f, f[4];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, xm[w][row]);
+    for (int u = 0; u < 4; ++u) mx = fmaxf(mx, xm[u][row]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      f[w] = xm[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm[w][row] - mx) * sc);
+    for (int u = 0; u < 4; ++u) {
+      f[u] = xm[u][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm[u][row] - mx) * sc);
       // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
-      l += xm[w][row] == -INFINITY ? xl[w][row] : xl[w][row] * f[w];
+      l += xm[u][row] == -INFINITY ? xl[u][row] : xl[u][row] * f[u];
     }
-    const int rr = r0 + row, node_ = rr / G, h = hk * G + rr % G;
-    const int64_t out_row = ((int64_t)b * a.T + node_) * a.H + h;
-    const int64_t part_row = ((int64_t)bh * a.T * G + rr) * a.splits + split;
+    const int rr = w.r0 + row;
+    const int64_t out_row = ((int64_t)b * a.T + rr / G) * a.H + w.hk * G + rr % G;
+    const int64_t part_row = ((int64_t)w.bh * a.T * G + rr) * a.splits + w.split;
     if (tid % PER == 0) {
-      if (ns > 1) a.part_ml[part_row] = make_float2(mx, l);
+      if (w.ns > 1) a.part_ml[part_row] = make_float2(mx, l);
       else if (a.stat) a.stat[out_row] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
     }
     for (int c = c0; c < a.dh; c += 4 * PER) {
       floatx4 x = floatx4{};
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] += xo[w][row][c + i] * f[w];
-      if (ns > 1) {
+        for (int i = 0; i < 4; ++i) x[i] += xo[u][row][c + i] * f[u];
+      if (w.ns > 1) {
         *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + c) = x;
       } else {
         tree_store<AT>(a.out, out_row * a.dh + c, x, l);
       }
     }
+  }
+}
+
+// Many rows (bf16): NW waves of 32 (dh <= 128) or 16 rows each share the keys and values,
+// which come through LDS by DMA, two tiles ahead.  A tile is 32 rows of DH channels for
+// keys and as many for values; 16-byte piece c of key j lies at piece c ^ (j % 16 or less),
+// so that both the reads of one piece of 16 keys and those of all pieces of a key spread
+// over the banks.  Two waves per SIMD: one's softmax runs beside the other's products.
+template <int DH, int NW, bool FULL>
+__global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
+  constexpr int RT = DH == 256 ? 1 : 2;
+  using Rows = RowTiles<uint16_t, DH, RT>;
+  using T = typename Rows::T;
+  constexpr int CPL = T::CPL, ROWS = 16 * RT * NW;
+  constexpr int PIECES = DH / 8, SWZ = PIECES < 16 ? PIECES - 1 : 15;  // 16-byte pieces of a row
+  constexpr int TILE = 32 * DH, STAGES = 3;                             // elements of a key or value tile
+  __shared__ __align__(16) uint16_t buf[STAGES][2][TILE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int m = lane & 15, g = lane >> 4;
+  TreeWork w;
+  if (!tree_work<32, ROWS>(a, w)) return;
+  const int b = w.b, n = w.n, G = a.H / a.Hkv;
+  const uint16_t* kb = reinterpret_cast<const uint16_t*>(a.k) + b * a.kvb + w.hk * a.kvh;
+  const uint16_t* vb = reinterpret_cast<const uint16_t*>(a.v) + b * a.kvb + w.hk * a.kvh;
+  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  const uint32_t lds0 = lds_offset(&buf[0][0][0]);
+  // a tile is 2 * TILE * 2 bytes in pieces of 1 KB per wave and DMA
+  constexpr int DMAS = 4 * TILE / 1024 / NW;
+  static_assert(DMAS >= 1 && DMAS * NW * 1024 == 4 * TILE, "the waves share a tile evenly");
+  const int last_piece = a.dh / 8 - 1;
+  auto fetch = [&](int t, int stage) {
+#pragma unroll
+    for (int i = 0; i < DMAS; ++i) {
+      const int slot = (i * NW + wave) * 64 + lane;  // 16-byte slot of the stage: keys, then values
+      const int kv = slot / (TILE / 8), j = slot % (TILE / 8) / PIECES, c = (slot % PIECES) ^ (j & SWZ);
+      const uint16_t* src = (kv ? vb : kb) + (int64_t)min(32 * t + j, n - 1) * a.kvs + 8 * (FULL ? c : min(c, last_piece));
+      dma16(src, lds0 + (uint32_t)(stage * 4 * TILE + (i * NW + wave) * 1024));
+    }
+  };
+  Rows rows;
+  rows.template start<FULL>(a, b, w.hk, w.r0 + 16 * RT * wave, w.R, lane);
+  // the queries have arrived: from here on only the DMAs count as loads in flight
+  dma_wait_all();
+  fetch(w.t0, 0);
+  if (w.t0 + 1 < w.t1) fetch(w.t0 + 1, 1);
+  auto step = [&](int t, auto tail_) {
+    constexpr bool tail = decltype(tail_)::value;
+    const int stage = (t - w.t0) % STAGES;
+    // tile t has landed, and every wave is done with tile t - 1, whose place tile t + 2 takes
+    if (t + 1 < w.t1) dma_wait_barrier<DMAS>();
+    else dma_wait_barrier<0>();
+    if (t + 2 < w.t1) fetch(t + 2, (stage + 2) % STAGES);
+    const uint16_t* ks = buf[stage][0];
+    const uint16_t* vs = buf[stage][1];
+    typename T::K k;
+#pragma unroll
+    for (int u = 0; u < T::KT; ++u)
+#pragma unroll
+      for (int i = 0; i < T::NK; ++i) {
+        const int c = 4 * i + g;
+        u32x4 x = *reinterpret_cast<const u32x4*>(ks + (16 * u + m) * DH + 8 * (c ^ (m & SWZ)));
+        if (!FULL && c > last_piece) x = u32x4{0, 0, 0, 0};
+        k.f[u][i] = __builtin_bit_cast(bf16x8, x);
+      }
+    rows.scores(k);
+    rows.template soften<tail>(a, b, 32 * t, w.ext, g, sc);
+    typename T::V v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = T::value_key(e, g);
+      if constexpr (DH == 64) {
+        const uint2 x = *reinterpret_cast<const uint2*>(vs + j * DH + 8 * ((m / 2) ^ (j & SWZ)) + 4 * (m % 2));
+        v.w[e][0] = x.x;
+        v.w[e][1] = x.y;
+      } else {
+#pragma unroll
+        for (int q = 0; q < DH / 128; ++q) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(vs + j * DH + 8 * ((16 * q + m) ^ (j & SWZ)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v.w[e][4 * q + i] = x[i];
+        }
+      }
+    }
+    rows.template add<tail>(v);
+  };
+  int t = w.t0;
+  for (; t < min(w.t1, w.ext.x / 32); ++t) step(t, std::false_type{});
+  for (; t < w.t1; ++t) step(t, std::true_type{});
+
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const float l = rows.row_sum(r), top = rows.top[r];
+    const int rr = w.r0 + 16 * (RT * wave + r) + m;
+    if (rr >= w.R) continue;
+    const int64_t out_row = ((int64_t)b * a.T + rr / G) * a.H + w.hk * G + rr % G;
+    const int64_t part_row = ((int64_t)w.bh * a.T * G + rr) * a.splits + w.split;
+    if (g == 0) {
+      if (w.ns > 1) a.part_ml[part_row] = make_float2(top, l);
+      else if (a.stat) a.stat[out_row] = make_float2(top == -INFINITY ? 0.f : top * sc, l == 0.f ? 0.f : 1.f / l);
+    }
+#pragma unroll
+    for (int c = 0; c < CPL; c += 4)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = T::channel(c, 4 * g + i);  // four consecutive channels
+        if (!FULL && ch >= a.dh) continue;
+        const floatx4 x = {rows.o[r][c][i], rows.o[r][c + 1][i], rows.o[r][c + 2][i], rows.o[r][c + 3][i]};
+        if (w.ns > 1) *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + ch) = x;
+        else tree_store<uint16_t>(a.out, out_row * a.dh + ch, x, l);
+      }
   }
 }
 
@@ -620,7 +786,8 @@ __global__ void __launch_bounds__(256) tree_weights_kernel(TreeArgs a) {
 // Tiles, row groups and splits of a call, and its workspace.
 struct TreePlan {
   int dhp;     // kernel width: 64, 128 or 256
-  int rt;      // row tiles of a wave
+  int rt;      // row tiles of a wave of tree_attention_kernel, or 0:
+  int nw;      // waves of tree_rows_kernel
   int groups;  // row groups of a unit
   int splits, min_tiles;
   size_t ml_off, o_off, bytes;
@@ -631,29 +798,46 @@ TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype d
   const bool bf16 = dtype == SPIDER_BF16;
   const int R = T * (H / Hkv), keys = bf16 ? 32 : 16;
   p.dhp = dh <= 64 ? 64 : (dh <= 128 ? 128 : 256);
-  p.rt = R <= 16 ? 1 : (R <= 32 || !bf16 || p.dhp == 256 ? 2 : 4);
-  p.groups = ceil_div(R, 16 * p.rt);
+  const int wave_rows = p.dhp == 256 ? 16 : 32;
+  int rows, target;
+  if (!bf16 || R <= wave_rows) {
+    p.rt = R <= 16 ? 1 : 2;
+    rows = 16 * p.rt;
+    target = 768;
+  } else {
+    p.nw = R <= 2 * wave_rows ? 2 : (R <= 4 * wave_rows ? 4 : 8);
+    rows = wave_rows * p.nw;
+    target = 256 * 8 / p.nw;
+  }
+  p.groups = ceil_div(R, rows);
   p.min_tiles = 8;
   const int64_t units = (int64_t)B * Hkv * p.groups;
   const int tiles = ceil_div(cap, keys);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((768 + units - 1) / units, tiles / p.min_tiles));
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((target + units - 1) / units, tiles / p.min_tiles));
   size_t off = weights ? align_up((size_t)B * T * H * sizeof(float2), 256) : 0;
   p.ml_off = off;
   if (p.splits > 1) {
-    const size_t rows = (size_t)B * T * H * p.splits;
-    off = align_up(off + rows * sizeof(float2), 256);
+    const size_t rows_ = (size_t)B * T * H * p.splits;
+    off = align_up(off + rows_ * sizeof(float2), 256);
     p.o_off = off;
-    off = align_up(off + rows * dh * sizeof(float), 256);
+    off = align_up(off + rows_ * dh * sizeof(float), 256);
   }
   p.bytes = off;
   return p;
 }
 
+unsigned tree_blocks(const TreeArgs& a) { return (unsigned)((a.B * a.Hkv * a.splits + 7) / 8 * 8 * a.groups); }
+
 template <typename AT, int DH, int RT>
 void launch_tree(const TreeArgs& a, hipStream_t st) {
-  const int units = (a.B * a.Hkv * a.splits + 7) / 8 * 8;
-  if (a.dh == DH) tree_attention_kernel<AT, DH, RT, true><<<(unsigned)(units * a.groups), 256, 0, st>>>(a);
-  else tree_attention_kernel<AT, DH, RT, false><<<(unsigned)(units * a.groups), 256, 0, st>>>(a);
+  if (a.dh == DH) tree_attention_kernel<AT, DH, RT, true><<<tree_blocks(a), 256, 0, st>>>(a);
+  else tree_attention_kernel<AT, DH, RT, false><<<tree_blocks(a), 256, 0, st>>>(a);
+}
+
+template <int DH, int NW>
+void launch_tree_rows(const TreeArgs& a, hipStream_t st) {
+  if (a.dh == DH) tree_rows_kernel<DH, NW, true><<<tree_blocks(a), 64 * NW, 0, st>>>(a);
+  else tree_rows_kernel<DH, NW, false><<<tree_blocks(a), 64 * NW, 0, st>>>(a);
 }
 
 template <typename AT, int DH>
@@ -668,8 +852,11 @@ spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   {
     ProfScope ps(KC_TREE_ATTN, st);
     if (p.rt == 1) launch_tree<AT, DH, 1>(a, st);
-    else if (p.rt == 2) launch_tree<AT, DH, 2>(a, st);
-    else if constexpr (sizeof(AT) == 2 && DH <= 128) launch_tree<AT, DH, 4>(a, st);
+    else if constexpr (sizeof(AT) == 4) launch_tree<AT, DH, 2>(a, st);
+    else if (p.nw == 2) launch_tree_rows<DH, 2>(a, st);
+    else if (p.nw == 4) launch_tree_rows<DH, 4>(a, st);
+    else if (p.nw == 8) launch_tree_rows<DH, 8>(a, st);
+    else if constexpr (DH <= 128) launch_tree<AT, DH, 2>(a, st);
     SPIDER_LAUNCHED("tree_attention");
     if (a.splits > 1) {
       tree_join_kernel<AT><<<dim3((unsigned)(a.T * a.H), (unsigned)a.B), 64, 0, st>>>(a);
