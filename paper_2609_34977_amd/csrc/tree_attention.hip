@@ -14,6 +14,7 @@ namespace {
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr int kTreeMaxNodes = 256;
 constexpr int kTreeMaxDh = 256;
@@ -148,57 +149,42 @@ struct TreeTile<uint16_t, DH> {
       for (int i = 0; i < NK; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.f[t][i], q.f[i], s[t], 0, 0, 0);
     }
   }
-  // whether a value of the lane's keys is infinite or NaN
-  __device__ static __forceinline__ bool nonfinite(const V& v) {
-    bool bad = false;
+  // the value operands: channel n of the lane's eight keys
+  struct Ops {
+    u32x4 f[CPL];
+  };
+  __device__ static __forceinline__ Ops turn(const V& v) {
+    Ops x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int n = 0; n < CPL; ++n)
 #pragma unroll
-      for (int i = 0; i < VW; ++i)
-        bad = bad || (v.w[e][i] & 0x7F80u) == 0x7F80u || (v.w[e][i] & 0x7F800000u) == 0x7F800000u;
-    return bad;
+      for (int e = 0; e < 4; ++e)
+        x.f[n][e] = __builtin_amdgcn_perm(v.w[2 * e + 1][n / 2], v.w[2 * e][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
+    return x;
   }
-  __device__ static __forceinline__ void drop_nonfinite(V& v) {
+  // infinite and NaN values become 0; whether there was one
+  __device__ static __forceinline__ bool drop_nonfinite(Ops& v) {
+    uint32_t bad = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int i = 0; i < VW; ++i) {
-        const uint32_t x = v.w[e][i];
-        v.w[e][i] = ((x & 0x7F80u) == 0x7F80u ? 0u : x & 0xFFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : x & 0xFFFF0000u);
-      }
-  }
-  // adds inf (kind 0), -inf (1) or NaN (2) to every output whose row sees such a value
-  template <int RT>
-  __device__ static __forceinline__ void special(floatx4 (*o)[CPL], const V& v, const float (*on)[KT * 4], int kind) {
-    uint32_t bits = kind == 2 ? 0x7FFFu : 0xFFFFu, lo = kind == 0 ? 0x7F80u : (kind == 1 ? 0xFF80u : 0x7F81u);
-    uint32_t span = kind == 2 ? 0x7Eu : 0u;
-    asm volatile("" : "+s"(bits), "+s"(lo), "+s"(span));  // not three sets of comparisons, kept ahead of time
-    auto is = [=](uint32_t h) { return (h & bits) - lo <= span ? 0x3F80u : 0u; };
-    const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
-#pragma unroll
-    for (int n = 0; n < CPL; ++n) {
-      u32x4 x;
+    for (int n = 0; n < CPL; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t sh = 16 * (n % 2);
-        x[e] = is(v.w[2 * e][n / 2] >> sh & 0xFFFFu) | is(v.w[2 * e + 1][n / 2] >> sh & 0xFFFFu) << 16;
+        const uint32_t x = v.f[n][e];
+        const uint32_t drop = ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+        bad |= drop;
+        v.f[n][e] = x & ~drop;
       }
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        u32x4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          y[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{on[r][2 * e], on[r][2 * e + 1]}, bf16x2v));
-        const floatx4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
-                                                                  __builtin_bit_cast(bf16x8, y), floatx4{}, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[r][n][i] += c[i] > 0.f ? add : 0.f;
-      }
-    }
+    return bad != 0;
   }
-  // O^T += V^T P^T; the fp32 weights enter as bf16 high and low parts
-  template <int RT>
-  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const V& v, const float (*p)[KT * 4]) {
+  __device__ static __forceinline__ uint32_t pack(float a0, float a1) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
+  }
+  __device__ static __forceinline__ float value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
+  // O^T += V^T P^T.  TWO: the fp32 weights enter as bf16 high and low parts; else rounded
+  // to bf16 once, and l += the sums of the rounded weights, by a product with ones, so that
+  // the weights of a row still add up to one.
+  template <int RT, bool TWO>
+  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], floatx4* l, const Ops& v, const float (*p)[KT * 4]) {
     bf16x8 hi[RT], lo[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -206,26 +192,24 @@ struct TreeTile<uint16_t, DH> {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float a0 = p[r][2 * e], a1 = p[r][2 * e + 1];
-        const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
-        const float2v rest{a0 - __uint_as_float(h << 16), a1 - __uint_as_float(h & 0xFFFF0000u)};
-        wh[e] = h;
-        wl[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
+        wh[e] = pack(a0, a1);
+        if constexpr (TWO) wl[e] = pack(a0 - __uint_as_float(wh[e] << 16), a1 - __uint_as_float(wh[e] & 0xFFFF0000u));
       }
       hi[r] = __builtin_bit_cast(bf16x8, wh);
-      lo[r] = __builtin_bit_cast(bf16x8, wl);
+      if constexpr (TWO) lo[r] = __builtin_bit_cast(bf16x8, wl);
+    }
+    if constexpr (!TWO) {
+      const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+#pragma unroll
+      for (int r = 0; r < RT; ++r) l[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, hi[r], l[r], 0, 0, 0);
     }
 #pragma unroll
     for (int n = 0; n < CPL; ++n) {
-      // channel n of the lane's eight keys
-      u32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        x[e] = __builtin_amdgcn_perm(v.w[2 * e + 1][n / 2], v.w[2 * e][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
-      const bf16x8 a = __builtin_bit_cast(bf16x8, x);
+      const bf16x8 a = __builtin_bit_cast(bf16x8, v.f[n]);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[r], o[r][n], 0, 0, 0);
-        o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[r], o[r][n], 0, 0, 0);
+        if constexpr (TWO) o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[r], o[r][n], 0, 0, 0);
       }
     }
   }
@@ -246,6 +230,8 @@ struct TreeTile<float, DH> {
   struct V {
     floatx4 f[4][DH / 64];
   };
+  using Ops = V;
+  __device__ static __forceinline__ Ops turn(const V& v) { return v; }
   __device__ static __forceinline__ int channel(int n, int m) { return 64 * (n / 4) + 4 * m + n % 4; }
   __device__ static __forceinline__ int value_key(int e, int g) { return 4 * g + e; }
 
@@ -286,44 +272,21 @@ struct TreeTile<float, DH> {
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[i][c], q.f[i][c], s[0], 0, 0, 0);
   }
-  __device__ static __forceinline__ bool nonfinite(const V& v) {
+  __device__ static __forceinline__ bool drop_nonfinite(V& v) {
     bool bad = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int n = 0; n < CPL; ++n)
-        bad = bad || (__float_as_uint(v.f[e][n / 4][n % 4]) & 0x7F800000u) == 0x7F800000u;
+      for (int n = 0; n < CPL; ++n) {
+        const bool drop = (__float_as_uint(v.f[e][n / 4][n % 4]) & 0x7F800000u) == 0x7F800000u;
+        bad = bad || drop;
+        if (drop) v.f[e][n / 4][n % 4] = 0.f;
+      }
     return bad;
   }
-  __device__ static __forceinline__ void drop_nonfinite(V& v) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int n = 0; n < CPL; ++n)
-        if ((__float_as_uint(v.f[e][n / 4][n % 4]) & 0x7F800000u) == 0x7F800000u) v.f[e][n / 4][n % 4] = 0.f;
-  }
-  template <int RT>
-  __device__ static __forceinline__ void special(floatx4 (*o)[CPL], const V& v, const float (*on)[4], int kind) {
-    uint32_t bits = kind == 2 ? 0x7FFFFFFFu : ~0u, span = kind == 2 ? 0x7FFFFEu : 0u;
-    uint32_t lo = kind == 0 ? 0x7F800000u : (kind == 1 ? 0xFF800000u : 0x7F800001u);
-    asm volatile("" : "+s"(bits), "+s"(lo), "+s"(span));  // not three sets of comparisons, kept ahead of time
-    const float add = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
-#pragma unroll
-    for (int n = 0; n < CPL; ++n)
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        floatx4 c = floatx4{};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t x = __float_as_uint(v.f[e][n / 4][n % 4]);
-          c = __builtin_amdgcn_mfma_f32_16x16x4f32((x & bits) - lo <= span ? 1.f : 0.f, on[r][e], c, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[r][n][i] += c[i] > 0.f ? add : 0.f;
-      }
-  }
-  template <int RT>
-  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const V& v, const float (*p)[4]) {
+  __device__ static __forceinline__ float value(const float* p) { return *p; }
+  template <int RT, bool TWO>
+  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], floatx4*, const V& v, const float (*p)[4]) {
 #pragma unroll
     for (int n = 0; n < CPL; ++n)
 #pragma unroll
@@ -368,16 +331,18 @@ __device__ __forceinline__ int tree_splits(const TreeArgs& a, int tiles) {
 constexpr float kLazyMax = 8.f;
 
 // RT row tiles of a wave: queries, and the running maximum, sum and output of their rows.
-template <typename AT, int DH, int RT>
+// TWO: see TreeTile::values; the sum then is the fp32 weights', a part of it in each lane.
+template <typename AT, int DH, int RT, bool TWO>
 struct RowTiles {
   using T = TreeTile<AT, DH>;
   static constexpr int KEYS = T::KEYS, NS = 4 * T::KT, CPL = T::CPL;  // NS: scores of a lane and row tile
   typename T::Q q[RT];
   int node[RT];
-  floatx4 o[RT][CPL];
+  floatx4 o[RT][CPL], l[RT];
   float top[RT], sum[RT];
   float p[RT][NS];
   uint32_t seen[RT];  // the lane's keys of the tile that its row sees, bit i for score i
+  bool nonfinite = false;  // add() left out a value
 
   template <bool FULL>
   __device__ __forceinline__ void start(const TreeArgs& a, int b, int hk, int r0, int R, int lane) {
@@ -390,6 +355,7 @@ struct RowTiles {
       T::template load_q<FULL>(q[r], qp, lane >> 4, a.dh, a.scale < 0.f);
       top[r] = -INFINITY;
       sum[r] = 0.f;
+      l[r] = floatx4{};
 #pragma unroll
       for (int c = 0; c < CPL; ++c) o[r][c] = floatx4{};
     }
@@ -436,7 +402,8 @@ struct RowTiles {
         const float nt = fmaxf(top[r], mx[r]);
         const float f = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top[r] - nt) * sc);
         top[r] = nt;
-        sum[r] *= f;
+        if constexpr (TWO) sum[r] *= f;
+        else l[r] *= f;
 #pragma unroll
         for (int c = 0; c < CPL; ++c) o[r][c] *= f;
       }
@@ -450,31 +417,45 @@ struct RowTiles {
         float e = __builtin_amdgcn_exp2f(fmaf(p[r][i], sc, -mc));
         if constexpr (tail) e = (seen[r] >> i) & 1u ? e : 0.f;
         p[r][i] = e;
-        s0 += e;
+        if constexpr (TWO) s0 += e;
       }
-      sum[r] += s0;
+      if constexpr (TWO) sum[r] += s0;
     }
   }
 
+  // the tile's values into the outputs.  Infinite and NaN values count for the rows that
+  // see them and for no other, but 0 times one of them is NaN: they leave the product, and
+  // add_nonfinite puts them back.
   template <bool tail>
-  __device__ __forceinline__ void add(typename T::V& v) {
-    if constexpr (tail) if (__any(T::nonfinite(v))) {
-      // infinite and NaN values count for the rows that see them, and for no other (0 times
-      // one of them is NaN): a product of its own for each kind, then they leave v
-      float on[RT][NS];
+  __device__ __forceinline__ void add(typename T::Ops& v) {
+    if constexpr (tail) nonfinite = nonfinite || __any(T::drop_nonfinite(v));
+    T::template values<RT, TWO>(o, l, v, p);
+  }
+
+  // the infinite and NaN values of the keys [j0, j1) into the outputs of the rows that see
+  // them; channel(c, i): of output o[.][c][i]
+  template <typename F>
+  __device__ __forceinline__ void add_nonfinite(const TreeArgs& a, int b, const AT* vb, int j0, int j1, int2 ext,
+                                                F&& channel) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) on[r][i] = (seen[r] >> i) & 1u ? 1.f : 0.f;
+      for (int c = 0; c < CPL; ++c)
 #pragma unroll 1
-      for (int kind = 0; kind < 3; ++kind) T::template special<RT>(o, v, on, kind);
-      T::drop_nonfinite(v);
-    }
-    T::template values<RT>(o, v, p);
+        for (int j = j0; j < j1; ++j) {
+          if (!(tree_window<KEYS>(a, b, node[r], j, ext) & 1u)) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int ch = channel(c, i);
+            const float x = ch < a.dh ? T::value(vb + (int64_t)j * a.kvs + ch) : 0.f;
+            if ((__float_as_uint(x) & 0x7F800000u) == 0x7F800000u) o[r][c][i] += x;
+          }
+        }
   }
 
   // the row's sum, in every lane of its column
   __device__ __forceinline__ float row_sum(int r) const {
+    if constexpr (!TWO) return l[r][0];
     float2 x = lanes_x16(sum[r]);
     x = lanes_x32(x.x + x.y);
     return x.x + x.y;
@@ -516,8 +497,8 @@ __device__ __forceinline__ bool tree_work(const TreeArgs& a, TreeWork& w) {
 // softmax.  4 waves, wave w takes tiles w, w + 4, .. of the block's split; their sums meet
 // in LDS.
 template <typename AT, int DH, int RT, bool FULL>
-__global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_kernel(TreeArgs a) {
-  using Rows = RowTiles<AT, DH, RT>;
+__global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_kernel(TreeArgs a) {
+  using Rows = RowTiles<AT, DH, RT, true>;
   using T = typename Rows::T;
   constexpr int KEYS = T::KEYS, CPL = T::CPL;
   constexpr int ROWS = 16 * RT, LD = DH + 4;
@@ -543,11 +524,17 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_ker
     rows.scores(k);
     if (t + 4 < w.t1) T::template load_k<FULL>(k, kb, a.kvs, j0 + 4 * KEYS, n, lane, a.dh);
     rows.template soften<tail>(a, b, j0, w.ext, g, sc);
-    rows.template add<tail>(v);
+    auto ops = T::turn(v);
+    rows.template add<tail>(ops);
   };
   int t = w.t0 + wave;
   for (; t < min(w.t1, w.ext.x / KEYS); t += 4) step(t, std::false_type{});
+  const int tail0 = t;
   for (; t < w.t1; t += 4) step(t, std::true_type{});
+  if (rows.nonfinite)
+    for (t = tail0; t < w.t1; t += 4)
+      rows.add_nonfinite(a, b, vb, t * KEYS, min(n, (t + 1) * KEYS), w.ext,
+                         [&](int c, int i) { return T::channel(c, 4 * g + i); });
 
   // the waves' sums onto their common maximum, in wave order
 #pragma unroll
@@ -601,17 +588,17 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 2 : 1) tree_attention_ker
 // which come through LDS by DMA, two tiles ahead.  A tile is 32 rows of DH channels for
 // keys and as many for values; 16-byte piece c of key j lies at piece c ^ (j % 16 or less),
 // so that both the reads of one piece of 16 keys and those of all pieces of a key spread
-// over the banks.  Two waves per SIMD: one's softmax runs beside the other's products.
+// over the banks.
 template <int DH, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
   constexpr int RT = DH == 256 ? 1 : 2;
-  using Rows = RowTiles<uint16_t, DH, RT>;
+  using Rows = RowTiles<uint16_t, DH, RT, false>;
   using T = typename Rows::T;
   constexpr int CPL = T::CPL, ROWS = 16 * RT * NW;
   constexpr int PIECES = DH / 8, SWZ = PIECES < 16 ? PIECES - 1 : 15;  // 16-byte pieces of a row
   constexpr int TILE = 32 * DH, STAGES = 3;                             // elements of a key or value tile
   __shared__ __align__(16) uint16_t buf[STAGES][2][TILE];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, g = lane >> 4;
   TreeWork w;
   if (!tree_work<32, ROWS>(a, w)) return;
@@ -620,34 +607,39 @@ __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
   const uint16_t* vb = reinterpret_cast<const uint16_t*>(a.v) + b * a.kvb + w.hk * a.kvh;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
   const uint32_t lds0 = lds_offset(&buf[0][0][0]);
-  // a tile is 2 * TILE * 2 bytes in pieces of 1 KB per wave and DMA
-  constexpr int DMAS = 4 * TILE / 1024 / NW;
-  static_assert(DMAS >= 1 && DMAS * NW * 1024 == 4 * TILE, "the waves share a tile evenly");
+  // A DMA of a wave fills 1 KB, 64 / PIECES rows.  Every wave fetches the same rows of keys
+  // and values, KD pieces of each (width 64 in 8 waves: one piece, of keys or of values).
+  constexpr int KD = DH / 16 / NW, DMAS = KD ? 2 * KD : 1;
   const int last_piece = a.dh / 8 - 1;
-  auto fetch = [&](int t, int stage) {
+  auto fetch = [&](int t) {
+    const uint32_t to = lds0 + (uint32_t)((t - w.t0) % STAGES * 4 * TILE);
+    if constexpr (KD > 0) {
 #pragma unroll
-    for (int i = 0; i < DMAS; ++i) {
-      const int slot = (i * NW + wave) * 64 + lane;  // 16-byte slot of the stage: keys, then values
-      const int kv = slot / (TILE / 8), j = slot % (TILE / 8) / PIECES, c = (slot % PIECES) ^ (j & SWZ);
-      const uint16_t* src = (kv ? vb : kb) + (int64_t)min(32 * t + j, n - 1) * a.kvs + 8 * (FULL ? c : min(c, last_piece));
-      dma16(src, lds0 + (uint32_t)(stage * 4 * TILE + (i * NW + wave) * 1024));
+      for (int i = 0; i < KD; ++i) {
+        const int part = i * NW + wave, j = part * (64 / PIECES) + lane / PIECES, c = (lane % PIECES) ^ (j & SWZ);
+        const int64_t off = (int64_t)min(32 * t + j, n - 1) * a.kvs + 8 * (FULL ? c : min(c, last_piece));
+        dma16(kb + off, to + part * 1024);
+        dma16(vb + off, to + 2 * TILE + part * 1024);
+      }
+    } else {
+      const int part = wave % (NW / 2), j = part * (64 / PIECES) + lane / PIECES, c = (lane % PIECES) ^ (j & SWZ);
+      const int64_t off = (int64_t)min(32 * t + j, n - 1) * a.kvs + 8 * (FULL ? c : min(c, last_piece));
+      dma16((wave < NW / 2 ? kb : vb) + off, to + (wave < NW / 2 ? 0 : 2 * TILE) + part * 1024);
     }
   };
   Rows rows;
   rows.template start<FULL>(a, b, w.hk, w.r0 + 16 * RT * wave, w.R, lane);
-  // the queries have arrived: from here on only the DMAs count as loads in flight
-  dma_wait_all();
-  fetch(w.t0, 0);
-  if (w.t0 + 1 < w.t1) fetch(w.t0 + 1, 1);
+  dma_wait_all();  // the queries are here: from now on only the DMAs count as loads in flight
+  fetch(w.t0);
+  if (w.t0 + 1 < w.t1) fetch(w.t0 + 1);
   auto step = [&](int t, auto tail_) {
     constexpr bool tail = decltype(tail_)::value;
-    const int stage = (t - w.t0) % STAGES;
     // tile t has landed, and every wave is done with tile t - 1, whose place tile t + 2 takes
     if (t + 1 < w.t1) dma_wait_barrier<DMAS>();
     else dma_wait_barrier<0>();
-    if (t + 2 < w.t1) fetch(t + 2, (stage + 2) % STAGES);
-    const uint16_t* ks = buf[stage][0];
-    const uint16_t* vs = buf[stage][1];
+    if (t + 2 < w.t1) fetch(t + 2);
+    const uint16_t* ks = buf[(t - w.t0) % STAGES][0];
+    const uint16_t* vs = buf[(t - w.t0) % STAGES][1];
     typename T::K k;
 #pragma unroll
     for (int u = 0; u < T::KT; ++u)
@@ -659,29 +651,32 @@ __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
         k.f[u][i] = __builtin_bit_cast(bf16x8, x);
       }
     rows.scores(k);
-    rows.template soften<tail>(a, b, 32 * t, w.ext, g, sc);
-    typename T::V v;
+    // the value operands by transposing reads: 16 lanes read four keys of 16 channels, a lane
+    // gets the four keys of channel 16 n + lane % 16
+    typename T::Ops v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = T::value_key(e, g);
-      if constexpr (DH == 64) {
-        const uint2 x = *reinterpret_cast<const uint2*>(vs + j * DH + 8 * ((m / 2) ^ (j & SWZ)) + 4 * (m % 2));
-        v.w[e][0] = x.x;
-        v.w[e][1] = x.y;
-      } else {
+    for (int c = 0; c < CPL; ++c) {
+      u32x4 x;
 #pragma unroll
-        for (int q = 0; q < DH / 128; ++q) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(vs + j * DH + 8 * ((16 * q + m) ^ (j & SWZ)));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v.w[e][4 * q + i] = x[i];
-        }
+      for (int e = 0; e < 2; ++e) {
+        const int j = 16 * e + 4 * g + m / 4, piece = 2 * c + m % 4 / 2;
+        const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ (j & SWZ)) + 4 * (m % 2)));
+        const uint2 z = __builtin_bit_cast(uint2, y);
+        x[2 * e] = z.x;
+        x[2 * e + 1] = z.y;
       }
+      v.f[c] = x;
     }
+    rows.template soften<tail>(a, b, 32 * t, w.ext, g, sc);
     rows.template add<tail>(v);
   };
   int t = w.t0;
   for (; t < min(w.t1, w.ext.x / 32); ++t) step(t, std::false_type{});
+  const int tail0 = t;
   for (; t < w.t1; ++t) step(t, std::true_type{});
+  if (rows.nonfinite)
+    rows.add_nonfinite(a, b, vb, 32 * tail0, min(n, 32 * w.t1), w.ext, [&](int c, int i) { return 16 * c + 4 * g + i; });
 
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -695,15 +690,12 @@ __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
       else if (a.stat) a.stat[out_row] = make_float2(top == -INFINITY ? 0.f : top * sc, l == 0.f ? 0.f : 1.f / l);
     }
 #pragma unroll
-    for (int c = 0; c < CPL; c += 4)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ch = T::channel(c, 4 * g + i);  // four consecutive channels
-        if (!FULL && ch >= a.dh) continue;
-        const floatx4 x = {rows.o[r][c][i], rows.o[r][c + 1][i], rows.o[r][c + 2][i], rows.o[r][c + 3][i]};
-        if (w.ns > 1) *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + ch) = x;
-        else tree_store<uint16_t>(a.out, out_row * a.dh + ch, x, l);
-      }
+    for (int c = 0; c < CPL; ++c) {
+      const int ch = 16 * c + 4 * g;  // of four consecutive outputs
+      if (!FULL && ch >= a.dh) continue;
+      if (w.ns > 1) *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + ch) = rows.o[r][c];
+      else tree_store<uint16_t>(a.out, out_row * a.dh + ch, rows.o[r][c], l);
+    }
   }
 }
 
@@ -805,7 +797,8 @@ TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype d
     rows = 16 * p.rt;
     target = 768;
   } else {
-    p.nw = R <= 2 * wave_rows ? 2 : (R <= 4 * wave_rows ? 4 : 8);
+    // (width 256 has no registers for two waves per SIMD)
+    p.nw = R <= 2 * wave_rows ? 2 : (R <= 4 * wave_rows || p.dhp == 256 ? 4 : 8);
     rows = wave_rows * p.nw;
     target = 256 * 8 / p.nw;
   }
@@ -855,8 +848,10 @@ spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
     else if constexpr (sizeof(AT) == 4) launch_tree<AT, DH, 2>(a, st);
     else if (p.nw == 2) launch_tree_rows<DH, 2>(a, st);
     else if (p.nw == 4) launch_tree_rows<DH, 4>(a, st);
-    else if (p.nw == 8) launch_tree_rows<DH, 8>(a, st);
-    else if constexpr (DH <= 128) launch_tree<AT, DH, 2>(a, st);
+    else if constexpr (DH <= 128) {
+      if (p.nw == 8) launch_tree_rows<DH, 8>(a, st);
+      else launch_tree<AT, DH, 2>(a, st);
+    }
     SPIDER_LAUNCHED("tree_attention");
     if (a.splits > 1) {
       tree_join_kernel<AT><<<dim3((unsigned)(a.T * a.H), (unsigned)a.B), 64, 0, st>>>(a);
