@@ -33,11 +33,13 @@ struct TreeArgs {
   float2* stat;     // [B][T][H] (largest score in powers of two, 1 / sum of exponentials), with w_out
   float2* part_ml;  // [B][Hkv][T * G][splits] (largest raw score, sum) of a split
   float* part_o;    // .. [dh] its unscaled output
+  float* scores;    // [B][Hkv][tiles][T * G][keys of a tile] raw scores, -inf where not seen, or null
   int64_t qb, qt;         // strides of q, elements
   int64_t kvb, kvs, kvh;  // strides of k and v
   int B, T, H, Hkv, dh, cap;
   float scale;
   int groups, splits, min_tiles;  // of the launch, see TreePlan
+  int join_blocks;                // of tree_finish_kernel
 };
 
 // The filled slots and live nodes of sample b, clamped to the cache.
@@ -149,42 +151,49 @@ struct TreeTile<uint16_t, DH> {
       for (int i = 0; i < NK; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.f[t][i], q.f[i], s[t], 0, 0, 0);
     }
   }
-  // the value operands: channel n of the lane's eight keys
+  // the operands of the value products: channel n of the lane's eight keys, put together
+  // from the rows, or read that way
   struct Ops {
     u32x4 f[CPL];
   };
-  __device__ static __forceinline__ Ops turn(const V& v) {
-    Ops x;
+  __device__ static __forceinline__ bf16x8 operand(const V& v, int n) {
+    u32x4 x;
 #pragma unroll
-    for (int n = 0; n < CPL; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        x.f[n][e] = __builtin_amdgcn_perm(v.w[2 * e + 1][n / 2], v.w[2 * e][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
-    return x;
+    for (int e = 0; e < 4; ++e)
+      x[e] = __builtin_amdgcn_perm(v.w[2 * e + 1][n / 2], v.w[2 * e][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
+    return __builtin_bit_cast(bf16x8, x);
   }
+  __device__ static __forceinline__ bf16x8 operand(const Ops& v, int n) { return __builtin_bit_cast(bf16x8, v.f[n]); }
   // infinite and NaN values become 0; whether there was one
+  __device__ static __forceinline__ uint32_t finite(uint32_t x, bool& bad) {
+    const uint32_t drop = ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+    bad = bad || drop != 0;
+    return x & ~drop;
+  }
+  __device__ static __forceinline__ bool drop_nonfinite(V& v) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < VW; ++i) v.w[e][i] = finite(v.w[e][i], bad);
+    return bad;
+  }
   __device__ static __forceinline__ bool drop_nonfinite(Ops& v) {
-    uint32_t bad = 0;
+    bool bad = false;
 #pragma unroll
     for (int n = 0; n < CPL; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t x = v.f[n][e];
-        const uint32_t drop = ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-        bad |= drop;
-        v.f[n][e] = x & ~drop;
-      }
-    return bad != 0;
+      for (int e = 0; e < 4; ++e) v.f[n][e] = finite(v.f[n][e], bad);
+    return bad;
   }
   __device__ static __forceinline__ uint32_t pack(float a0, float a1) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
   }
   __device__ static __forceinline__ float value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
   // O^T += V^T P^T.  TWO: the fp32 weights enter as bf16 high and low parts; else rounded
-  // to bf16 once, and l += the sums of the rounded weights, by a product with ones, so that
-  // the weights of a row still add up to one.
-  template <int RT, bool TWO>
-  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], floatx4* l, const Ops& v, const float (*p)[KT * 4]) {
+  // to bf16 once.
+  template <int RT, bool TWO, typename S>
+  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const S& v, const float (*p)[KT * 4]) {
     bf16x8 hi[RT], lo[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -198,14 +207,9 @@ struct TreeTile<uint16_t, DH> {
       hi[r] = __builtin_bit_cast(bf16x8, wh);
       if constexpr (TWO) lo[r] = __builtin_bit_cast(bf16x8, wl);
     }
-    if constexpr (!TWO) {
-      const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
-#pragma unroll
-      for (int r = 0; r < RT; ++r) l[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, hi[r], l[r], 0, 0, 0);
-    }
 #pragma unroll
     for (int n = 0; n < CPL; ++n) {
-      const bf16x8 a = __builtin_bit_cast(bf16x8, v.f[n]);
+      const bf16x8 a = operand(v, n);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[r], o[r][n], 0, 0, 0);
@@ -230,8 +234,6 @@ struct TreeTile<float, DH> {
   struct V {
     floatx4 f[4][DH / 64];
   };
-  using Ops = V;
-  __device__ static __forceinline__ Ops turn(const V& v) { return v; }
   __device__ static __forceinline__ int channel(int n, int m) { return 64 * (n / 4) + 4 * m + n % 4; }
   __device__ static __forceinline__ int value_key(int e, int g) { return 4 * g + e; }
 
@@ -285,8 +287,8 @@ struct TreeTile<float, DH> {
     return bad;
   }
   __device__ static __forceinline__ float value(const float* p) { return *p; }
-  template <int RT, bool TWO>
-  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], floatx4*, const V& v, const float (*p)[4]) {
+  template <int RT, bool TWO, typename S>
+  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const S& v, const float (*p)[4]) {
 #pragma unroll
     for (int n = 0; n < CPL; ++n)
 #pragma unroll
@@ -331,14 +333,14 @@ __device__ __forceinline__ int tree_splits(const TreeArgs& a, int tiles) {
 constexpr float kLazyMax = 8.f;
 
 // RT row tiles of a wave: queries, and the running maximum, sum and output of their rows.
-// TWO: see TreeTile::values; the sum then is the fp32 weights', a part of it in each lane.
+// TWO: see TreeTile::values.
 template <typename AT, int DH, int RT, bool TWO>
 struct RowTiles {
   using T = TreeTile<AT, DH>;
   static constexpr int KEYS = T::KEYS, NS = 4 * T::KT, CPL = T::CPL;  // NS: scores of a lane and row tile
   typename T::Q q[RT];
   int node[RT];
-  floatx4 o[RT][CPL], l[RT];
+  floatx4 o[RT][CPL];
   float top[RT], sum[RT];
   float p[RT][NS];
   uint32_t seen[RT];  // the lane's keys of the tile that its row sees, bit i for score i
@@ -355,7 +357,6 @@ struct RowTiles {
       T::template load_q<FULL>(q[r], qp, lane >> 4, a.dh, a.scale < 0.f);
       top[r] = -INFINITY;
       sum[r] = 0.f;
-      l[r] = floatx4{};
 #pragma unroll
       for (int c = 0; c < CPL; ++c) o[r][c] = floatx4{};
     }
@@ -371,9 +372,11 @@ struct RowTiles {
     }
   }
 
-  // scores to weights, for the tile of keys from j0; tail: some key is a node, or past the last one
+  // scores to weights, for the tile of keys from j0; tail: some key is a node, or past the
+  // last one; keep (or null): where the tile's scores of the lane's row go (row tile 0)
   template <bool tail>
-  __device__ __forceinline__ void soften(const TreeArgs& a, int b, int j0, int2 ext, int g, float sc) {
+  __device__ __forceinline__ void soften(const TreeArgs& a, int b, int j0, int2 ext, int g, float sc,
+                                         float* keep = nullptr) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       seen[r] = ~0u;
@@ -383,6 +386,11 @@ struct RowTiles {
 #pragma unroll
         for (int i = 0; i < NS; ++i) p[r][i] = (seen[r] >> i) & 1u ? p[r][i] : -INFINITY;
       }
+    }
+    if (keep) {
+#pragma unroll
+      for (int i = 0; i < NS; i += 4)
+        *reinterpret_cast<floatx4*>(keep + 4 * i + 4 * g) = floatx4{p[0][i], p[0][i + 1], p[0][i + 2], p[0][i + 3]};
     }
     bool grows = false;
     float mx[RT];
@@ -402,8 +410,7 @@ struct RowTiles {
         const float nt = fmaxf(top[r], mx[r]);
         const float f = top[r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top[r] - nt) * sc);
         top[r] = nt;
-        if constexpr (TWO) sum[r] *= f;
-        else l[r] *= f;
+        sum[r] *= f;
 #pragma unroll
         for (int c = 0; c < CPL; ++c) o[r][c] *= f;
       }
@@ -417,19 +424,19 @@ struct RowTiles {
         float e = __builtin_amdgcn_exp2f(fmaf(p[r][i], sc, -mc));
         if constexpr (tail) e = (seen[r] >> i) & 1u ? e : 0.f;
         p[r][i] = e;
-        if constexpr (TWO) s0 += e;
+        s0 += e;
       }
-      if constexpr (TWO) sum[r] += s0;
+      sum[r] += s0;
     }
   }
 
   // the tile's values into the outputs.  Infinite and NaN values count for the rows that
   // see them and for no other, but 0 times one of them is NaN: they leave the product, and
   // add_nonfinite puts them back.
-  template <bool tail>
-  __device__ __forceinline__ void add(typename T::Ops& v) {
+  template <bool tail, typename S>
+  __device__ __forceinline__ void add(S& v) {
     if constexpr (tail) nonfinite = nonfinite || __any(T::drop_nonfinite(v));
-    T::template values<RT, TWO>(o, l, v, p);
+    T::template values<RT, TWO, S>(o, v, p);
   }
 
   // the infinite and NaN values of the keys [j0, j1) into the outputs of the rows that see
@@ -455,7 +462,6 @@ struct RowTiles {
 
   // the row's sum, in every lane of its column
   __device__ __forceinline__ float row_sum(int r) const {
-    if constexpr (!TWO) return l[r][0];
     float2 x = lanes_x16(sum[r]);
     x = lanes_x32(x.x + x.y);
     return x.x + x.y;
@@ -517,15 +523,18 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_ker
   typename T::V v;
   if (w.t0 + wave < w.t1) T::template load_k<FULL>(k, kb, a.kvs, (w.t0 + wave) * KEYS, n, lane, a.dh);
   rows.template start<FULL>(a, b, w.hk, w.r0, w.R, lane);
+  const int64_t tile_scores = (int64_t)a.T * G * KEYS;
+  float* kept = RT == 1 && a.scores && m < w.R
+                    ? a.scores + (int64_t)w.bh * ((a.cap + KEYS - 1) / KEYS) * tile_scores + m * KEYS : nullptr;
   auto step = [&](int t, auto tail_) {
     constexpr bool tail = decltype(tail_)::value;
     const int j0 = t * KEYS;
     T::template load_v<FULL>(v, vb, a.kvs, j0, n, lane, a.dh);
     rows.scores(k);
     if (t + 4 < w.t1) T::template load_k<FULL>(k, kb, a.kvs, j0 + 4 * KEYS, n, lane, a.dh);
-    rows.template soften<tail>(a, b, j0, w.ext, g, sc);
-    auto ops = T::turn(v);
-    rows.template add<tail>(ops);
+    if constexpr (RT == 1) rows.template soften<tail>(a, b, j0, w.ext, g, sc, kept ? kept + t * tile_scores : nullptr);
+    else rows.template soften<tail>(a, b, j0, w.ext, g, sc);
+    rows.template add<tail>(v);
   };
   int t = w.t0 + wave;
   for (; t < min(w.t1, w.ext.x / KEYS); t += 4) step(t, std::false_type{});
@@ -699,33 +708,146 @@ __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
   }
 }
 
-// The splits of one row joined: grid (rows of T * H, B), a thread per four channels.
-template <typename AT>
-__global__ void __launch_bounds__(64) tree_join_kernel(TreeArgs a) {
-  const int t = blockIdx.x / a.H, h = blockIdx.x % a.H, b = blockIdx.y;
+// One launch after the attention: blocks below a.join_blocks join the splits of the rows (a
+// wave per row with few splits, else a block), the others add up the weights from the kept
+// scores.
+// Neither waits for the other: a weights block joins its rows' statistics itself.
+// Join: groups of dh / 4 threads, a thread per four channels, take every ng-th split, their
+// sums meet in LDS in group order.  Weights: a thread per four slots, all live rows of the
+// head group in order.
+constexpr int kWaveJoin = 8;  // splits that a wave joins
+template <typename AT, int THREADS>
+__device__ __forceinline__ void tree_join(const TreeArgs& a, float sc) {
+  __shared__ float red[4];
+  __shared__ floatx4 xs_[256];
+  __shared__ float ls_[256];
+  constexpr int TEAMS = 256 / THREADS;
+  const int team = threadIdx.x / THREADS, tid = threadIdx.x % THREADS;
+  floatx4* xs = xs_ + team * THREADS;
+  float* ls = ls_ + team * THREADS;
+  auto sync = [] {
+    if constexpr (THREADS == 64) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    else __syncthreads();
+  };
+  const int r = blockIdx.x * TEAMS + team, h = r % a.H, t = r / a.H % a.T, b = r / a.H / a.T;
+  if (b >= a.B) return;
   const int2 ext = tree_extent(a, b);
   if (t >= ext.y) return;
-  constexpr int KEYS = sizeof(AT) == 2 ? 32 : 16;
+  constexpr int KEYS = TreeTile<AT, 64>::KEYS;
   const int ns = tree_splits(a, (ext.x + ext.y + KEYS - 1) / KEYS);
   if (ns == 1) return;
   const int G = a.H / a.Hkv, hk = h / G;
   const int64_t part = (((int64_t)b * a.Hkv + hk) * a.T * G + (int64_t)t * G + h % G) * a.splits;
-  const float sc = fabsf(a.scale) * 1.4426950408889634f;
   float mx = -INFINITY;
-  for (int s = 0; s < ns; ++s) mx = fmaxf(mx, a.part_ml[part + s].x);
-  const int64_t row = ((int64_t)b * a.T + t) * a.H + h;
-  const int c = 4 * threadIdx.x;
+  for (int s = tid; s < ns; s += THREADS) mx = fmaxf(mx, a.part_ml[part + s].x);
+  mx = wave_max(mx);
+  if constexpr (THREADS == 256) {
+    if ((tid & 63) == 0) red[tid >> 6] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  }
+  const int per = a.dh / 4, ng = THREADS / per, grp = tid / per, c = 4 * (tid % per);
   float l = 0.f;
   floatx4 x = floatx4{};
-  for (int s = 0; s < ns; ++s) {
-    const float2 ml = a.part_ml[part + s];
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mx) * sc);
-    l += ml.x == -INFINITY ? ml.y : ml.y * f;
-    if (c < a.dh) x += *reinterpret_cast<const floatx4*>(a.part_o + (part + s) * a.dh + c) * f;
+  if (grp < ng) {
+    for (int s0 = grp; s0 < ns; s0 += 4 * ng) {
+      float2 ml[4];
+      floatx4 o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int s = min(s0 + u * ng, ns - 1);
+        ml[u] = a.part_ml[part + s];
+        o[u] = *reinterpret_cast<const floatx4*>(a.part_o + (part + s) * a.dh + c);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (s0 + u * ng >= ns) break;
+        const float f = ml[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[u].x - mx) * sc);
+        // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
+        l += ml[u].x == -INFINITY ? ml[u].y : ml[u].y * f;
+        x += o[u] * f;
+      }
+    }
   }
-  if (c < a.dh) tree_store<AT>(a.out, row * a.dh + c, x, l);
-  if (a.stat && threadIdx.x == 0)
-    a.stat[row] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
+  xs[tid] = x;
+  ls[tid] = l;
+  sync();
+  if (grp > 0) return;
+  for (int i = 1; i < ng; ++i) {
+    x += xs[i * per + tid];
+    l += ls[i * per + tid];
+  }
+  const int64_t row = ((int64_t)b * a.T + t) * a.H + h;
+  tree_store<AT>(a.out, row * a.dh + c, x, l);
+  if (a.stat && tid == 0) a.stat[row] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
+}
+
+template <typename AT>
+__global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
+  constexpr int KEYS = TreeTile<AT, 64>::KEYS;
+  __shared__ float2 st[16];
+  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  if ((int)blockIdx.x < a.join_blocks) {
+    if (a.splits <= kWaveJoin) tree_join<AT, 64>(a, sc);
+    else tree_join<AT, 256>(a, sc);
+    return;
+  }
+  const int blk = blockIdx.x - a.join_blocks, tid = threadIdx.x;
+  const int blocks = (a.cap + 1023) / 1024, bh = blk / blocks, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int G = a.H / a.Hkv;
+  const int2 ext = tree_extent(a, b);
+  const int n = ext.x + ext.y, R = ext.y * G;
+  const int j = (blk % blocks * 256 + tid) * 4;
+  if (blk % blocks * 1024 >= n) return;
+  // (the first rows' scores on their way before their statistics)
+  const float* s = a.scores + ((int64_t)bh * ((a.cap + KEYS - 1) / KEYS) + j / KEYS) * a.T * G * KEYS + j % KEYS;
+  floatx4 x[8];
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (j < n && u < R) x[u] = *reinterpret_cast<const floatx4*>(s + u * KEYS);
+  const int ns = tree_splits(a, (n + KEYS - 1) / KEYS);
+  if (ns == 1) {
+    if (tid < R) st[tid] = a.stat[((int64_t)b * a.T + tid / G) * a.H + hk * G + tid % G];
+  } else {
+    // 16 lanes per row, every 16th split each
+    const int r = tid / 16, k = tid % 16;
+    const float2* ml = a.part_ml + ((int64_t)bh * a.T * G + min(r, R - 1)) * a.splits;
+    float mx = -INFINITY, l = 0.f;
+    for (int i = k; i < ns; i += 16) mx = fmaxf(mx, ml[i].x);
+    mx = fmaxf(mx, lane_dpp<kDppRor8>(mx));
+    mx = fmaxf(mx, lane_dpp<kDppRor4>(mx));
+    mx = fmaxf(mx, lane_dpp<kDppX2>(mx));
+    mx = fmaxf(mx, lane_dpp<kDppX1>(mx));
+    for (int i = k; i < ns; i += 16) {
+      const float2 v = ml[i];
+      l += v.x == -INFINITY ? v.y : v.y * __builtin_amdgcn_exp2f((v.x - mx) * sc);
+    }
+    l = row16_sum(l);
+    if (k == 0) st[r] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
+  }
+  __syncthreads();
+  if (j >= n) return;
+  floatx4 sum = floatx4{};
+  for (int r0 = 0; r0 < R; r0 += 8) {
+    if (r0 > 0) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (r0 + u < R) x[u] = *reinterpret_cast<const floatx4*>(s + (r0 + u) * KEYS);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (r0 + u >= R) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[u][i], sc, -st[r0 + u].x)) * st[r0 + u].y;
+        sum[i] += x[u][i] == -INFINITY ? 0.f : e;
+      }
+    }
+  }
+  const int64_t at = (int64_t)bh * a.cap + j;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (j + i < n) a.w_out[at + i] = (j + i < ext.x && a.w_in ? a.w_in[at + i] : 0.f) + sum[i];
 }
 
 // The weight of every slot: a wave per KEYS keys of one kv head, all live rows of the
@@ -782,7 +904,8 @@ struct TreePlan {
   int nw;      // waves of tree_rows_kernel
   int groups;  // row groups of a unit
   int splits, min_tiles;
-  size_t ml_off, o_off, bytes;
+  bool kept;  // the weights come from kept scores
+  size_t ml_off, o_off, score_off, bytes;
 };
 
 TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype dtype, bool weights) {
@@ -814,6 +937,14 @@ TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype d
     off = align_up(off + rows_ * sizeof(float2), 256);
     p.o_off = off;
     off = align_up(off + rows_ * dh * sizeof(float), 256);
+  }
+  // The weights of up to 16 rows come from the scores, kept in fp32 (8 bytes a row and key,
+  // written and read), those of more rows from a second pass over the keys (2 dh bytes a
+  // key, and the products again).  Measured: WEIGHTS_MEASURED
+  p.score_off = off;
+  if (weights && p.rt == 1) {
+    p.kept = true;
+    off = align_up(off + (size_t)B * Hkv * R * tiles * keys * sizeof(float), 256);
   }
   p.bytes = off;
   return p;
@@ -853,12 +984,14 @@ spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
       else launch_tree<AT, DH, 2>(a, st);
     }
     SPIDER_LAUNCHED("tree_attention");
-    if (a.splits > 1) {
-      tree_join_kernel<AT><<<dim3((unsigned)(a.T * a.H), (unsigned)a.B), 64, 0, st>>>(a);
-      SPIDER_LAUNCHED("tree_join");
-    }
   }
-  if (a.w_out) {
+  const unsigned weight_blocks = a.scores ? (unsigned)ceil_div(a.cap, 1024) * (unsigned)(a.B * a.Hkv) : 0u;
+  if (a.join_blocks + weight_blocks > 0) {
+    ProfScope ps(a.scores ? KC_TREE_WEIGHTS : KC_TREE_ATTN, st);
+    tree_finish_kernel<AT><<<a.join_blocks + weight_blocks, 256, 0, st>>>(a);
+    SPIDER_LAUNCHED("tree_finish");
+  }
+  if (a.w_out && !a.scores) {
     ProfScope ps(KC_TREE_WEIGHTS, st);
     launch_tree_weights<AT, DH>(a, st);
     SPIDER_LAUNCHED("tree_weights");
@@ -927,13 +1060,15 @@ extern "C" spider_status spider_tree_attention(int B, int T, int H, int Hkv, int
                  "spider_tree_attention: workspace must be 256-byte aligned");
   char* ws = reinterpret_cast<char*>(workspace);
   TreeArgs a{q, k, v, out, lens, n_nodes, tree_mask, weights_in, weights_out, nullptr, nullptr, nullptr,
-             q_stride_b, q_stride_t, kv_stride_b, kv_stride_s, kv_stride_h, B, T, H, Hkv, dh, cap, scale,
-             p.groups, p.splits, p.min_tiles};
+             nullptr, q_stride_b, q_stride_t, kv_stride_b, kv_stride_s, kv_stride_h, B, T, H, Hkv, dh, cap, scale,
+             p.groups, p.splits, p.min_tiles,
+             p.splits == 1 ? 0 : (p.splits <= kWaveJoin ? ceil_div(B * T * H, 4) : B * T * H)};
   if (weights_out) a.stat = reinterpret_cast<float2*>(ws);
   if (p.splits > 1) {
     a.part_ml = reinterpret_cast<float2*>(ws + p.ml_off);
     a.part_o = reinterpret_cast<float*>(ws + p.o_off);
   }
+  if (p.kept) a.scores = reinterpret_cast<float*>(ws + p.score_off);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   return dtype == SPIDER_BF16 ? run_tree<uint16_t>(a, p, st) : run_tree<float>(a, p, st);
 }
