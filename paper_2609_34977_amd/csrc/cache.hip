@@ -221,37 +221,50 @@ __global__ void __launch_bounds__(256) cache_copy_kernel(CompactArgs a) {
   if (a.w_out && c == 0) a.w_out[(int64_t)lbh * a.cap_out + dst] = a.w_in[(int64_t)lbh * a.cap_in + src];
 }
 
-// In place: one block per (layer, sample, head, kind) walks its entries in ascending
-// order.  An entry never comes from below the slot it goes to, so no later entry reads
-// what an earlier piece has written; within a piece every read precedes every write.
-__global__ void __launch_bounds__(256) cache_move_kernel(CompactArgs a) {
+// In place: blocks of a (layer, sample, head) each own cw 16-byte columns of the keys or of
+// the values (kind 0, 1), or the weights (2), and walk the entries in ascending order, kMove
+// per thread at a time.  An entry never comes from below the slot it goes to, so what a
+// piece of entries writes lies below all that later pieces read; within a piece every read
+// has returned before the first write, hence the wait and the barrier between them.
+constexpr int kMove = 8;
+__global__ void __launch_bounds__(256) cache_move_kernel(CompactArgs a, int cw) {
   const int lbh = blockIdx.x, h = lbh % a.Hkv, b = lbh / a.Hkv % a.B, l = lbh / a.Hkv / a.B;
-  const int kind = blockIdx.y;
+  const int columns = (a.nv + cw - 1) / cw, kind = blockIdx.y / columns;
   const CompactRow r = compact_row(a, l, b, h);
+  int src[kMove], dst[kMove];
+  bool on[kMove];
   if (kind == 2) {
+    if (blockIdx.y % columns != 0) return;
     const float* in = a.w_in + (int64_t)lbh * a.cap_in;
     float* out = a.w_out + (int64_t)lbh * a.cap_out;
-    for (int i0 = 0; i0 < r.n; i0 += 256) {
-      int src, dst;
-      const bool on = compact_entry(a, r, i0 + threadIdx.x, src, dst) && src != dst;
-      const float x = on ? in[src] : 0.f;
-      __syncthreads();
-      if (on) out[dst] = x;
-      __syncthreads();
+    for (int i0 = 0; i0 < r.n; i0 += 256 * kMove) {
+      float x[kMove];
+#pragma unroll
+      for (int u = 0; u < kMove; ++u) {
+        on[u] = compact_entry(a, r, i0 + 256 * u + threadIdx.x, src[u], dst[u]) && src[u] != dst[u];
+        x[u] = on[u] ? in[src[u]] : 0.f;
+      }
+      dma_wait_barrier<0>();
+#pragma unroll
+      for (int u = 0; u < kMove; ++u)
+        if (on[u]) out[dst[u]] = x[u];
     }
     return;
   }
-  const int per = 256 / a.nv, c = threadIdx.x % a.nv, e = threadIdx.x / a.nv;
+  const int per = 256 / cw, e = threadIdx.x / cw, c = blockIdx.y % columns * cw + threadIdx.x % cw;
   const char* in = a.in[kind] + l * a.il + b * a.ib + h * a.ih + 16 * c;
   char* out = a.out[kind] + l * a.ol + b * a.ob + h * a.oh + 16 * c;
-  for (int i0 = 0; i0 < r.n; i0 += per) {
-    int src, dst;
-    const bool on = e < per && compact_entry(a, r, i0 + e, src, dst) && src != dst;
-    u32x4 x = {0, 0, 0, 0};
-    if (on) x = *reinterpret_cast<const u32x4*>(in + src * a.is);
-    __syncthreads();
-    if (on) *reinterpret_cast<u32x4*>(out + dst * a.os) = x;
-    __syncthreads();
+  for (int i0 = 0; i0 < r.n; i0 += per * kMove) {
+    u32x4 x[kMove];
+#pragma unroll
+    for (int u = 0; u < kMove; ++u) {
+      on[u] = c < a.nv && compact_entry(a, r, i0 + per * u + e, src[u], dst[u]) && src[u] != dst[u];
+      x[u] = on[u] ? *reinterpret_cast<const u32x4*>(in + src[u] * a.is) : u32x4{0, 0, 0, 0};
+    }
+    dma_wait_barrier<0>();
+#pragma unroll
+    for (int u = 0; u < kMove; ++u)
+      if (on[u]) *reinterpret_cast<u32x4*>(out + dst[u] * a.os) = x[u];
   }
 }
 
@@ -345,8 +358,12 @@ extern "C" spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spi
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_CACHE_COMPACT, st);
   const unsigned rows = (unsigned)(L * B * Hkv);
+  // Columns of 128 bytes, or of 32 where there are few streams to walk.  Measured, columns
+  // of 32 / 64 / 128 / 256 bytes: 64 streams of 16384 entries of 256 bytes 350 / 365 / 503 /
+  // 863 us; 256 streams of 600, 128 / 256 bytes 27 / 31 us; 1024 streams of 576 136 / 132 us.
+  const int cw = (int64_t)L * B * Hkv >= 256 ? 8 : 2;
   if (inplace)
-    cache_move_kernel<<<dim3(rows, weights_in ? 3 : 2), 256, 0, st>>>(a);
+    cache_move_kernel<<<dim3(rows, (unsigned)(ceil_div(a.nv, cw) * (weights_in ? 3 : 2))), 256, 0, st>>>(a, cw);
   else
     cache_copy_kernel<<<dim3((unsigned)ceil_div(n_max, 256 / a.nv), rows), 256, 0, st>>>(a);
   SPIDER_LAUNCHED("cache_compact");

@@ -7,8 +7,6 @@
 namespace spider {
 namespace {
 
-constexpr int kAdjThreads = 256;
-constexpr int kAdjPiece = 4096;          // vocabulary entries per block
 constexpr uint32_t kSeen = 0x80000000u;  // count word: the token stands in the prompt
 
 struct AdjustArgs {
@@ -66,39 +64,59 @@ __device__ __forceinline__ void load_logits(const LT* p, float* x) {
   }
 }
 
+// A logit under the penalties: c is the count word of its token.
+__device__ __forceinline__ float penalised(float y, uint32_t c, float rep, float freq, float pres) {
+  if (c) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+  if (c & ~kSeen) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, (float)(c & ~kSeen))), pres);
+  return y;
+}
+
 // One block per (piece of the vocabulary, row): the counts of the piece's tokens in the
-// row's history and the places of its biases in LDS, then one pass over the logits, VEC
-// at a time (4 where the rows are aligned for it).  Every block reads the whole history
-// from L2, which is why the reads go eight at a time.
-template <typename LT, int VEC>
-__global__ void __launch_bounds__(kAdjThreads) adjust_kernel(AdjustArgs a) {
-  __shared__ uint32_t count[kAdjPiece];
-  __shared__ int32_t entry[kAdjPiece];  // first bias entry of a token
-  __shared__ int twice;                 // some token has several
-  __shared__ float bv[kAdjThreads / 64];
-  __shared__ int bi[kAdjThreads / 64];
+// row's history in LDS, then one pass over the logits, VEC at a time (4 where the rows are
+// aligned for it), all of a thread's on their way while the counts are made; then the few
+// tokens with a bias, which that pass leaves out (bits in LDS), each by the thread that
+// marked it.  A piece is as large as its counts fit: every block reads the whole history,
+// and a row in one piece needs no second launch for its arg max.
+template <typename LT, int VEC, int PIECE, int THREADS>
+__global__ void __launch_bounds__(THREADS) adjust_kernel(AdjustArgs a) {
+  constexpr int UN = PIECE / THREADS / VEC;
+  __shared__ uint32_t count[PIECE];
+  __shared__ uint32_t biased[PIECE / 32];
+  __shared__ int twice;  // some token has several bias entries
+  __shared__ float bv[THREADS / 64];
+  __shared__ int bi[THREADS / 64];
   const int row = blockIdx.y, b = row / a.T, t = row - b * a.T;
   const int tid = threadIdx.x;
   const int nn = a.n_nodes ? min(max(a.n_nodes[b], 0), a.T) : a.T;
   if (t >= nn) return;
-  const int v0 = blockIdx.x * kAdjPiece, nv = min(kAdjPiece, a.V - v0);
-  constexpr int kNone = 0x7fffffff;
-  for (int i = tid; i < kAdjPiece / 4; i += kAdjThreads) {
-    reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
-    if (a.n_bias) reinterpret_cast<int4*>(entry)[i] = make_int4(kNone, kNone, kNone, kNone);
+  const int v0 = blockIdx.x * PIECE, nv = min(PIECE, a.V - v0);
+  const LT* x = reinterpret_cast<const LT*>(a.logits) + row * a.ls + v0;
+  const uint32_t* m = a.mask ? a.mask + row * a.ms + (v0 >> 5) : nullptr;
+  float* o = a.out ? a.out + row * a.os + v0 : nullptr;
+  float z[UN][VEC];
+  uint32_t word[UN];
+#pragma unroll
+  for (int u = 0; u < UN; ++u) {
+    const int i = VEC * (tid + u * THREADS);
+    if (i < nv) {
+      load_logits<LT, VEC>(x + i, z[u]);
+      word[u] = m ? m[i >> 5] : ~0u;
+    }
   }
+  for (int i = tid; i < min(PIECE, (nv + 3) & ~3) / 4; i += THREADS) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+  for (int i = tid; i < PIECE / 32; i += THREADS) biased[i] = 0;
   if (tid == 0) twice = 0;
   __syncthreads();
   if (a.history) {
     const int n = min(max(a.n_history[b], 0), (int)a.hs), np = a.n_prompt ? a.n_prompt[b] : 0;
     const int32_t* h = a.history + b * a.hs;
-    for (int i0 = tid; i0 < n; i0 += 8 * kAdjThreads) {
+    for (int i0 = tid; i0 < n; i0 += 8 * THREADS) {
       int32_t id[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) id[u] = h[min(i0 + u * kAdjThreads, n - 1)];
+      for (int u = 0; u < 8; ++u) id[u] = h[min(i0 + u * THREADS, n - 1)];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int i = i0 + u * kAdjThreads;
+        const int i = i0 + u * THREADS;
         const uint32_t v = (uint32_t)id[u] - (uint32_t)v0;
         if (i < n && v < (uint32_t)nv) {
           if (i < np) atomicOr(&count[v], kSeen);
@@ -109,72 +127,68 @@ __global__ void __launch_bounds__(kAdjThreads) adjust_kernel(AdjustArgs a) {
   }
   if (a.tokens) {
     const int W = (a.T + 63) / 64;
-    const uint64_t* m = a.tree ? a.tree + (int64_t)row * W : nullptr;
-    for (int u = tid; u < nn; u += kAdjThreads) {
-      const bool sees = m ? (m[u >> 6] >> (u & 63)) & 1 : u <= t;
+    const uint64_t* tr = a.tree ? a.tree + (int64_t)row * W : nullptr;
+    for (int u = tid; u < nn; u += THREADS) {
+      const bool sees = tr ? (tr[u >> 6] >> (u & 63)) & 1 : u <= t;
       const uint32_t v = (uint32_t)a.tokens[(int64_t)b * a.T + u] - (uint32_t)v0;
       if (sees && v < (uint32_t)nv) atomicAdd(&count[v], 1u);
     }
   }
   const int32_t* ids = a.bias_ids + (int64_t)b * a.n_bias;
   const float* bias = a.bias + (int64_t)b * a.n_bias;
-  for (int i = tid; i < a.n_bias; i += kAdjThreads) {
+  uint64_t mine = 0;  // which of this thread's first 64 entries marked their token
+  for (int i = tid, k = 0; i < a.n_bias; i += THREADS, ++k) {
     const uint32_t v = (uint32_t)ids[i] - (uint32_t)v0;
-    if (v < (uint32_t)nv && atomicMin(&entry[v], i) != kNone) twice = 1;
+    if (v >= (uint32_t)nv) continue;
+    if (atomicOr(&biased[v >> 5], 1u << (v & 31)) >> (v & 31) & 1u) twice = 1;
+    else mine |= 1ull << k;
   }
   const float rep = a.rep ? a.rep[b] : 1.f, freq = a.freq ? a.freq[b] : 0.f, pres = a.pres ? a.pres[b] : 0.f;
-  const LT* x = reinterpret_cast<const LT*>(a.logits) + row * a.ls + v0;
-  float* o = a.out ? a.out + row * a.os + v0 : nullptr;
-  const uint32_t* m = a.mask ? a.mask + row * a.ms + (v0 >> 5) : nullptr;
   float best = -INFINITY;
   int arg = 0x7fffffff;
   __syncthreads();
+#pragma unroll
+  for (int u = 0; u < UN; ++u) {
+    const int i = VEC * (tid + u * THREADS);
+    if (i >= nv) break;
+    const uint32_t skip = a.n_bias ? biased[i >> 5] >> (i & 31) : 0u;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      float y = penalised(z[u][e], count[i + e], rep, freq, pres);
+      if (a.n_bias) y = __fadd_rn(y, 0.f);
+      if (!((word[u] >> ((i + e) & 31)) & 1u)) y = -INFINITY;
+      z[u][e] = y;
+      if (y > best && !((skip >> e) & 1u)) {
+        best = y;
+        arg = v0 + i + e;
+      }
+    }
+    if (o) {
+      if (VEC == 4 && (skip & 15u) == 0) {
+        *reinterpret_cast<floatx4*>(o + i) = floatx4{z[u][0], z[u][VEC > 1 ? 1 : 0], z[u][VEC > 2 ? 2 : 0], z[u][VEC > 3 ? 3 : 0]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (!((skip >> e) & 1u)) o[i + e] = z[u][e];
+      }
+    }
+  }
   const bool again = twice != 0;
-  constexpr int UN = VEC == 4 ? 4 : 8;  // loads in flight
-  for (int i0 = VEC * tid; i0 < nv; i0 += UN * VEC * kAdjThreads) {
-    float z[UN][VEC];
-    uint32_t word[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int i = i0 + u * VEC * kAdjThreads;
-      if (i < nv) {
-        load_logits<LT, VEC>(x + i, z[u]);
-        word[u] = m ? m[i >> 5] : ~0u;
-      }
+  for (int i = tid, k = 0; mine; i += THREADS, ++k, mine >>= 1) {
+    if (!(mine & 1u)) continue;
+    const int v = ids[i] - v0;
+    float add = 0.f, y[1];
+    if (!again) {
+      add = __fadd_rn(add, bias[i]);
+    } else {  // all entries of the token, in order
+      for (int j = 0; j < a.n_bias; ++j)
+        if (ids[j] == v0 + v) add = __fadd_rn(add, bias[j]);
     }
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int i = i0 + u * VEC * kAdjThreads;
-      if (i >= nv) break;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const uint32_t c = count[i + e];
-        float y = z[u][e];
-        if (c) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
-        if (c & ~kSeen) y = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, (float)(c & ~kSeen))), pres);
-        if (a.n_bias) {
-          const int k = entry[i + e];
-          float add = 0.f;
-          if (k != kNone) {
-            add = bias[k];
-            if (again)  // the other entries of the token, in order
-              for (int j = k + 1; j < a.n_bias; ++j)
-                if (ids[j] == v0 + i + e) add = __fadd_rn(add, bias[j]);
-          }
-          y = __fadd_rn(y, add);
-        }
-        if (!((word[u] >> ((i + e) & 31)) & 1u)) y = -INFINITY;
-        z[u][e] = y;
-        if (y > best) {
-          best = y;
-          arg = v0 + i + e;
-        }
-      }
-      if (o) {
-        if constexpr (VEC == 4) *reinterpret_cast<floatx4*>(o + i) = floatx4{z[u][0], z[u][1], z[u][2], z[u][3]};
-        else o[i] = z[u][0];
-      }
-    }
+    load_logits<LT, 1>(x + v, y);
+    float w = __fadd_rn(penalised(y[0], count[v], rep, freq, pres), add);
+    if (m && !((m[v >> 5] >> (v & 31)) & 1u)) w = -INFINITY;
+    if (o) o[v] = w;
+    take_best(best, arg, w, w != w || w == -INFINITY ? 0x7fffffff : v0 + v);
   }
   if (!a.next) return;
   wave_best(best, arg);
@@ -184,8 +198,9 @@ __global__ void __launch_bounds__(kAdjThreads) adjust_kernel(AdjustArgs a) {
   }
   __syncthreads();
   if (tid == 0) {
-    for (int w = 1; w < kAdjThreads / 64; ++w) take_best(best, arg, bv[w], bi[w]);
-    a.part[(int64_t)row * a.pieces + blockIdx.x] = make_float2(best, __int_as_float(arg));
+    for (int w = 1; w < THREADS / 64; ++w) take_best(best, arg, bv[w], bi[w]);
+    if (a.pieces == 1) a.next[row] = best == -INFINITY ? -1 : arg;
+    else a.part[(int64_t)row * a.pieces + blockIdx.x] = make_float2(best, __int_as_float(arg));
   }
 }
 
@@ -203,8 +218,24 @@ __global__ void __launch_bounds__(64) adjust_join_kernel(AdjustArgs a) {
   if (threadIdx.x == 0) a.next[row] = best == -INFINITY ? -1 : arg;
 }
 
+// Pieces of a row: all of it where its counts fit the LDS of a CU (a block per CU, but one
+// launch and one reading of the history), else 8192 tokens, four blocks per CU; and rows of
+// up to 8192 in such blocks too.  Measured, pieces of 8192 / 32768, us: 1 row of 32000 14.7
+// / 11.8; 248 rows of 32000 21.7 / 18.9; 64 rows of 151000 with 12000 tokens of history
+// 26.7 / 35.0 (16384: 33.2, in 1024 threads 28.3).
+constexpr int kPiece = 8192, kRow = 32768, kMaxBias = 64 * 512;
+int adjust_piece(int V) { return V > kPiece && V <= kRow ? kRow : kPiece; }
+
+template <typename LT, int VEC>
+void launch_adjust(const AdjustArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)a.pieces, (unsigned)(a.B * a.T));
+  if (adjust_piece(a.V) == kRow) adjust_kernel<LT, VEC, kRow, 1024><<<grid, 1024, 0, st>>>(a);
+  else adjust_kernel<LT, VEC, kPiece, 512><<<grid, 512, 0, st>>>(a);
+}
+
 size_t adjust_ws_bytes(int B, int T, int V) {
-  return align_up((size_t)B * T * ceil_div(V, kAdjPiece) * sizeof(float2), 256);
+  const int pieces = ceil_div(V, adjust_piece(V));
+  return pieces == 1 ? 0 : align_up((size_t)B * T * pieces * sizeof(float2), 256);
 }
 
 bool adjust_shape_ok(int B, int T, int V) {
@@ -234,8 +265,8 @@ extern "C" spider_status spider_adjust_logits(
                  "spider_adjust_logits: bad dtype");
   SPIDER_REQUIRE(B >= 1 && T >= 1 && V >= 1 && n_bias >= 0, SPIDER_ERR_INVALID_ARG,
                  "spider_adjust_logits: sizes must be positive");
-  SPIDER_REQUIRE(adjust_shape_ok(B, T, V) && n_bias <= 65536, SPIDER_ERR_UNSUPPORTED,
-                 "spider_adjust_logits: T <= 256, B * T <= 65535, V <= 2^28, n_bias <= 65536");
+  SPIDER_REQUIRE(adjust_shape_ok(B, T, V) && n_bias <= kMaxBias, SPIDER_ERR_UNSUPPORTED,
+                 "spider_adjust_logits: T <= 256, B * T <= 65535, V <= 2^28, n_bias <= 32768");
   SPIDER_REQUIRE(!history || (n_history && history_stride >= 0 && history_stride <= 0x7fffffff),
                  SPIDER_ERR_INVALID_ARG, "spider_adjust_logits: a history needs n_history and a stride below 2^31");
   SPIDER_REQUIRE(n_bias == 0 || (bias_ids && bias), SPIDER_ERR_INVALID_ARG,
@@ -256,23 +287,22 @@ extern "C" spider_status spider_adjust_logits(
                  "spider_adjust_logits: workspace must be 256-byte aligned");
   const AdjustArgs a{logits, out, next_out, reinterpret_cast<float2*>(workspace), history, n_history, n_prompt,
                      n_nodes, node_tokens, tree_mask, repetition, frequency, presence, bias_ids, bias, mask,
-                     logits_stride, out_stride, history_stride, mask_stride, B, T, V, n_bias, ceil_div(V, kAdjPiece)};
+                     logits_stride, out_stride, history_stride, mask_stride, B, T, V, n_bias, ceil_div(V, adjust_piece(V))};
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_ADJUST_LOGITS, st);
-  const dim3 grid((unsigned)a.pieces, (unsigned)(B * T));
   // four logits at a time where every row starts on a 16-byte (bf16: 8-byte) boundary and has a multiple of 4
   const uintptr_t four = dtype == SPIDER_BF16 ? 7 : 15;
   const bool vec = V % 4 == 0 && logits_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(logits) & four) == 0 &&
                    (!out || (out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0));
   if (dtype == SPIDER_BF16) {
-    if (vec) adjust_kernel<uint16_t, 4><<<grid, kAdjThreads, 0, st>>>(a);
-    else adjust_kernel<uint16_t, 1><<<grid, kAdjThreads, 0, st>>>(a);
+    if (vec) launch_adjust<uint16_t, 4>(a, st);
+    else launch_adjust<uint16_t, 1>(a, st);
   } else {
-    if (vec) adjust_kernel<float, 4><<<grid, kAdjThreads, 0, st>>>(a);
-    else adjust_kernel<float, 1><<<grid, kAdjThreads, 0, st>>>(a);
+    if (vec) launch_adjust<float, 4>(a, st);
+    else launch_adjust<float, 1>(a, st);
   }
   SPIDER_LAUNCHED("adjust_logits");
-  if (next_out) {
+  if (next_out && a.pieces > 1) {
     adjust_join_kernel<<<(unsigned)(B * T), 64, 0, st>>>(a);
     SPIDER_LAUNCHED("adjust_join");
   }

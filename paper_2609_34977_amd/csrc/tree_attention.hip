@@ -940,7 +940,8 @@ TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype d
   }
   // The weights of up to 16 rows come from the scores, kept in fp32 (8 bytes a row and key,
   // written and read), those of more rows from a second pass over the keys (2 dh bytes a
-  // key, and the products again).  Measured: WEIGHTS_MEASURED
+  // key, and the products again).  Measured, 4 rows of 128 over 16 x 8 x 32768 keys: 468 us
+  // with kept scores, 605 us with the second pass (352 us without weights).
   p.score_off = off;
   if (weights && p.rt == 1) {
     p.kept = true;

@@ -110,11 +110,12 @@ def test_cache_compact_refusals(L, kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(x=None), INVALID), (dict(out=None, nxt=None), INVALID), (dict(dt=5), INVALID), (dict(B=0), INVALID),
     (dict(V=0), INVALID), (dict(nb=-1), INVALID), (dict(T=257), UNSUPPORTED), (dict(B=65536), UNSUPPORTED),
-    (dict(V=1 << 29), UNSUPPORTED), (dict(nb=65537, bi=P, bv=P), UNSUPPORTED), (dict(h=P), INVALID),
+    (dict(V=1 << 29), UNSUPPORTED), (dict(nb=32769, bi=P, bv=P), UNSUPPORTED), (dict(h=P), INVALID),
     (dict(h=P, nh=P, hs=-1), INVALID), (dict(h=P, nh=P, hs=1 << 31), INVALID), (dict(nb=3), INVALID),
     (dict(nb=3, bi=P), INVALID), (dict(xs=99), SHAPE), (dict(os=99), SHAPE), (dict(m=P, ms=3), SHAPE),
     (dict(m=P, ms=-4), SHAPE), (dict(out=P, os=120), INVALID), (dict(out=P, dt=1), INVALID), (dict(x=P + 2), INVALID),
-    (dict(out=2 * P + 2), INVALID), (dict(wsb=8), WORKSPACE), (dict(ws=None), WORKSPACE), (dict(ws=P + 8), INVALID)])
+    (dict(out=2 * P + 2), INVALID), (dict(V=40000, xs=40000, os=40000, wsb=8), WORKSPACE),
+    (dict(V=40000, xs=40000, os=40000, ws=None), WORKSPACE), (dict(V=40000, xs=40000, os=40000, ws=P + 8), INVALID)])
 def test_adjust_logits_refusals(L, kw, status):
     a = dict(B=2, T=2, V=100, x=P, xs=100, dt=0, h=None, hs=0, nh=None, np=None, nn=None, tok=None, tree=None, rep=None,
              freq=None, pres=None, bi=None, bv=None, nb=0, m=None, ms=0, out=2 * P, os=100, nxt=P, ws=P, wsb=1 << 20)
@@ -125,6 +126,6 @@ def test_adjust_logits_refusals(L, kw, status):
 
 def test_adjust_logits_workspace_of_bad_sizes_is_zero(L):
     f = L.spider_adjust_logits_workspace_size
-    assert f(2, 2, 100) > 0
+    assert f(2, 2, 40000) > 0 and f(2, 2, 32768) == 0
     for bad in ((0, 1, 1), (1, 257, 1), (65536, 1, 1), (1, 1, 0), (1, 1, 1 << 29)):
         assert f(*bad) == 0

@@ -56,6 +56,12 @@ CASES = [
     (4, 1, 32000, 700, "f32", 8, "rows"),
     (2, 3, 32064, 1500, "bf16", 300, "rows"),
     (1, 1, 151001, 9000, "f32", 20, "one"),
+    (2, 2, 32768, 100, "f32", 600, "rows"),
+    (1, 2, 32769, 100, "bf16", 3, "rows"),
+    (1, 1, 65540, 3000, "f32", 1500, None),
+    (2, 1, 70001, 50, "bf16", 0, None),
+    (1, 3, 4096, 20, "bf16", 2500, "rows"),
+    (1, 2, 40004, 20, "f32", 7, "rows"),
     (1, 256, 130, 40, "f32", 2, None),
 ]
 
@@ -213,7 +219,7 @@ def test_refusals_of_the_binding():
         lambda: lib.adjust_logits(x, mask=torch.ones(2, 3, 3, dtype=torch.int32).cuda()),
         lambda: lib.adjust_logits(x, tree_mask=torch.ones(2, 3, 2, dtype=torch.int64).cuda()),
         lambda: lib.adjust_logits(x.bfloat16(), out=torch.zeros(2, 3, 99).cuda()),
-        lambda: lib.adjust_logits(x, workspace=torch.empty(8, dtype=torch.uint8).cuda()),
+        lambda: lib.adjust_logits(torch.zeros(2, 40000).cuda(), workspace=torch.empty(8, dtype=torch.uint8).cuda()),
     ]
     for f in bad:
         with pytest.raises((ValueError, TypeError, lib.SpiderError)):

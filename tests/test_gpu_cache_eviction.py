@@ -199,3 +199,20 @@ def test_refusals_of_the_binding():
     for f in bad:
         with pytest.raises((ValueError, TypeError, lib.SpiderError)):
             f()
+
+
+@pytest.mark.parametrize("L,B,cap,Hkv,dh,keep", [(2, 2, 3000, 4, 128, 2500), (1, 1, 9000, 2, 64, 8900)])
+def test_in_place_over_many_pieces(L, B, cap, Hkv, dh, keep):
+    """Thousands of entries that move a little: every piece's reads come before its writes."""
+    lib = need_gpu()
+    k, v = caches(L, B, cap, Hkv, dh, "bf16", False, 12)
+    w = torch.rand(L, B, Hkv, cap).cuda()
+    lens = torch.full((B,), cap, dtype=torch.int32).cuda()
+    idx, new = lib.cache_select(w, lens, keep)
+    at = idx.long().transpose(2, 3)
+    want = [torch.gather(x, 2, at[..., None].expand(-1, -1, -1, -1, dh)) for x in (k, v)]
+    ww = torch.gather(w, 3, idx.long())
+    tail = k[:, :, keep:].clone()
+    lib.cache_compact(k, v, idx, new, weights=w)
+    assert torch.equal(k[:, :, :keep], want[0]) and torch.equal(v[:, :, :keep], want[1])
+    assert torch.equal(w[..., :keep], ww) and torch.equal(k[:, :, keep:], tail)
