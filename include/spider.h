@@ -583,12 +583,16 @@ spider_status spider_decode_tree(const spider_decoder_cfg* cfg, const spider_lay
  * weights device fp32 [L][B][Hkv][cap]; idx_out device int32
  * [L][B][shared ? 1 : Hkv][keep]: the kept slots ascending, then -1; len_out
  * device int32 [B] = min(n, keep).  Requires n_first + n_last <= keep <= cap and
- * fewer than 2^22 rows (L * B * groups).
- * No workspace.
+ * fewer than 2^22 rows (L * B * groups).  Workspace:
+ * spider_cache_select_workspace_size(...) bytes (0 for short or many rows),
+ * 256-byte aligned.
  * ------------------------------------------------------------------------ */
+size_t spider_cache_select_workspace_size(int L, int B, int Hkv, int cap, int shared);
+
 spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* weights, const int32_t* lens,
                                   int keep, int n_first, int n_last, int shared, int32_t* idx_out,
-                                  int32_t* len_out, spider_stream stream);
+                                  int32_t* len_out, void* workspace, size_t workspace_bytes,
+                                  spider_stream stream);
 
 /* ------------------------------------------------------------------------
  * spider_cache_compact - moves the chosen slots of a cache to the front, or

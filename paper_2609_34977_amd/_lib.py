@@ -87,7 +87,8 @@ _SIGS = {
     "spider_decode_tree_workspace_size": ([ctypes.POINTER(DecoderCfg), _I, _I, _I, _I], _SZ),
     "spider_decode_tree": ([ctypes.POINTER(DecoderCfg), ctypes.POINTER(LayerWeights), _I, _I, _VP, _VP, _VP, _VP,
                             ctypes.POINTER(KVCache), _VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _SZ, _VP], _I),
-    "spider_cache_select": ([_I, _I, _I, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP], _I),
+    "spider_cache_select_workspace_size": ([_I, _I, _I, _I, _I], _SZ),
+    "spider_cache_select": ([_I, _I, _I, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP, _SZ, _VP], _I),
     "spider_cache_compact": ([_I, _I, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _VP, _VP, _I, _VP, _I, _I, _I, _VP, _VP,
                               _VP, _VP, _VP], _I),
     "spider_adjust_logits_workspace_size": ([_I, _I, _I], _SZ),
@@ -597,7 +598,7 @@ def decode_tree(cfg: DecoderCfg, weights, lens, x: torch.Tensor, kv: dict, paren
 
 
 def cache_select(weights: torch.Tensor, lens: torch.Tensor, keep: int, *, n_first: int = 0, n_last: int = 0,
-                 shared: bool = False):
+                 shared: bool = False, workspace: Optional[torch.Tensor] = None):
     """The slots to keep by accumulated weight: weights [L, B, Hkv, cap] fp32, lens [B] int32
     -> (idx [L, B, 1 if shared else Hkv, keep] int32 ascending then -1, new lens [B] int32)."""
     if weights.dim() != 4:
@@ -608,9 +609,11 @@ def cache_select(weights: torch.Tensor, lens: torch.Tensor, keep: int, *, n_firs
         raise ValueError("keep must be at least 1")
     idx = torch.empty(L_, B, 1 if shared else Hkv, keep, dtype=torch.int32, device=dev)
     new = torch.empty(B, dtype=torch.int32, device=dev)
+    wsz = _size("spider_cache_select_workspace_size", L_, B, Hkv, cap, int(bool(shared)))
+    workspace, wptr = _scratch(workspace, wsz, dev)
     _on(dev, lib().spider_cache_select, L_, B, Hkv, cap,
         _need(weights, "weights", torch.float32, (L_, B, Hkv, cap), dev), _need(lens, "lens", torch.int32, (B,), dev),
-        keep, n_first, n_last, int(bool(shared)), idx.data_ptr(), new.data_ptr())
+        keep, n_first, n_last, int(bool(shared)), idx.data_ptr(), new.data_ptr(), wptr, wsz)
     return idx, new
 
 

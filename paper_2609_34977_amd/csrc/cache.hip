@@ -52,15 +52,46 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
 constexpr int kSelBits = 11;  // of a key per pass: 32 = 11 + 11 + 10
 constexpr int kSelBuckets = 1 << kSelBits;
 
+// The bucket of the want-th largest key and its place within the bucket: lane l sums 32
+// buckets, the highest first, then 32 lanes look at those of the lane where the count is
+// reached.  One wave; found = (bucket, keys still wanted within it).
+__device__ __forceinline__ void find_bucket(const uint32_t* hist, uint32_t want, uint32_t* found) {
+  const int lane = threadIdx.x & 63;
+  uint32_t s = 0;
+  const int top = kSelBuckets - 1 - 32 * lane;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) s += hist[top - ((i + lane) & 31)];
+  const uint32_t up = wave_prefix(s);
+  const int at = __ffsll((unsigned long long)__ballot(up >= want)) - 1;
+  const uint32_t left = want - (uint32_t)__builtin_amdgcn_readlane((int)(up - s), at);
+  const uint32_t c = lane < 32 ? hist[kSelBuckets - 1 - 32 * at - lane] : 0u;
+  const uint32_t in = wave_prefix(c);
+  const int v = __ffsll((unsigned long long)__ballot(lane < 32 && in >= left)) - 1;
+  if (lane == v) {
+    found[0] = (uint32_t)(kSelBuckets - 1 - 32 * at - lane);
+    found[1] = left - (in - c);
+  }
+}
+
+// Counts a key's bucket (on: of the lanes that count): one add for the lanes that share the
+// first lane's bucket, since weights crowd in few exponents and often in one value.
+__device__ __forceinline__ void count_bucket(uint32_t* hist, uint32_t bucket, bool on) {
+  const uint64_t active = __ballot(on);
+  if (active == 0) return;
+  const int lane = threadIdx.x & 63, leader = __ffsll((unsigned long long)active) - 1;
+  const bool same = on && bucket == (uint32_t)__builtin_amdgcn_readlane((int)bucket, leader);
+  const uint64_t group = __ballot(same);
+  if (lane == leader) atomicAdd(&hist[bucket], (uint32_t)__popcll(group));
+  else if (on && !same) atomicAdd(&hist[bucket], 1u);
+}
+
 // One block per (layer, sample, head group): the keep-th largest key by a histogram of
 // its upper bits, then of the next bits of the keys that share those, then of the rest;
 // then the kept slots in ascending order.  Wave w owns 64 * NV consecutive slots, so that
 // after one exchange of counts every wave writes its slots without a barrier.  The keys
 // stay in registers (NV > 0, up to 64 per lane: n <= THREADS * NV); longer rows are read
 // again in each pass (NV = 0).
-// Bound by the barriers and the LDS atomics of its passes (a row is read once): weights
-// crowd in few exponents, and often in one value (slots that no query looked at), hence
-// eleven bits at once, and one add per wave for the lanes that share the first lane's bucket.
+// Bound by the barriers and the LDS atomics of its passes (a row is read once).
 template <int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
   constexpr int WAVES = THREADS / 64;
@@ -119,33 +150,10 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
     each([&](uint32_t k, int) {
       // (in the first pass all, also the zeros past the last slot: no search goes down to their bucket)
       const bool on = (k >> (shift + bits - 1)) >> 1 == prefix;
-      const uint64_t active = __ballot(on);
-      if (active == 0) return;
-      const uint32_t bucket = (k >> shift) & ((1u << bits) - 1u);
-      const int leader = __ffsll((unsigned long long)active) - 1;
-      const bool same = on && bucket == (uint32_t)__builtin_amdgcn_readlane((int)bucket, leader);
-      const uint64_t group = __ballot(same);
-      if (lane == leader) atomicAdd(&hist[bucket], (uint32_t)__popcll(group));
-      else if (on && !same) atomicAdd(&hist[bucket], 1u);
+      count_bucket(hist, (k >> shift) & ((1u << bits) - 1u), on);
     });
     __syncthreads();
-    if (wave == 0) {
-      // lane l: the sum of 32 buckets, highest first; then the 32 of the lane where the count is reached
-      uint32_t s = 0;
-      const int top = kSelBuckets - 1 - 32 * lane;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) s += hist[top - ((i + lane) & 31)];
-      const uint32_t up = wave_prefix(s);
-      const int at = __ffsll((unsigned long long)__ballot(up >= want)) - 1;
-      const uint32_t left = want - (uint32_t)__builtin_amdgcn_readlane((int)(up - s), at);
-      const uint32_t c = lane < 32 ? hist[kSelBuckets - 1 - 32 * at - lane] : 0u;
-      const uint32_t in = wave_prefix(c);
-      const int v = __ffsll((unsigned long long)__ballot(lane < 32 && in >= left)) - 1;
-      if (lane == v) {
-        found[0] = (uint32_t)(kSelBuckets - 1 - 32 * at - lane);
-        found[1] = left - (in - c);
-      }
-    }
+    if (wave == 0) find_bucket(hist, want, found);
     __syncthreads();
     prefix = __builtin_amdgcn_readfirstlane((prefix << bits) | found[0]);
     want = __builtin_amdgcn_readfirstlane(found[1]);
@@ -173,6 +181,189 @@ __global__ void __launch_bounds__(THREADS) cache_select_kernel(SelectArgs a) {
     gt += __popcll(mg);
     eq += __popcll(me);
   });
+}
+
+// Long rows, few of them: the same selection with a block per chunk of 8192 slots, in four
+// launches.  Every launch adds up the chunks' histograms of the one before (the same in all
+// blocks of a row), and counts its own chunk's next bits:
+//   1 keys (added over the heads here, once) and their upper 11 bits
+//   2 the bucket of the keep-th key; the next 11 bits of its keys
+//   3 again, the last 10 bits
+//   4 the key itself; where the chunk's slots go, and the slots
+constexpr int kChunk = 8192, kChunkThreads = 512, kChunkKeys = kChunk / kChunkThreads;
+struct ChunkWs {
+  uint32_t* keys;   // [rows][chunks][kChunk]
+  uint32_t* hist;   // [3][rows][chunks][kSelBuckets]
+  uint32_t* found;  // [2][rows][2] bucket and keys wanted after launches 2 and 3
+  uint32_t* above;  // [2][rows][chunks] keys of the chunk above the bucket of its launch
+};
+
+// Sum over the block, in every thread.
+__device__ __forceinline__ uint32_t block_sum(uint32_t v, uint32_t* cell) {
+  if (threadIdx.x == 0) *cell = 0;
+  __syncthreads();
+  const int x = wave_sum_int((int)v);
+  if ((threadIdx.x & 63) == 0) atomicAdd(cell, (uint32_t)x);
+  __syncthreads();
+  return *cell;
+}
+
+template <int PHASE>
+__global__ void __launch_bounds__(kChunkThreads) cache_select_chunk_kernel(SelectArgs a, ChunkWs ws, int chunks) {
+  constexpr int WAVES = kChunkThreads / 64;
+  __shared__ uint32_t hist[kSelBuckets];
+  __shared__ uint32_t found[2], cell;
+  __shared__ uint2 tot[WAVES];
+  const int rows = a.L * a.B * a.G;
+  const int row = blockIdx.x / chunks, ch = blockIdx.x % chunks;  // row = (l * B + b) * G + g
+  const int g = row % a.G, lb = row / a.G, b = lb % a.B;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = min(max(a.lens[b], 0), a.cap);
+  int32_t* idx = a.idx + (int64_t)row * a.keep;
+  if (PHASE == 1 && lb == b && g == 0 && ch == 0 && tid == 0) a.len_out[b] = min(n, a.keep);
+  if (n <= a.keep) {
+    if (PHASE == 1)
+      for (int i = ch * kChunk + tid; i < min(a.keep, (ch + 1) * kChunk); i += kChunkThreads) idx[i] = i < n ? i : -1;
+    return;
+  }
+  if (ch * kChunk >= n) return;
+  const int used = (n + kChunk - 1) / kChunk;
+  uint32_t* kp = ws.keys + ((int64_t)row * chunks + ch) * kChunk;
+  const int c0 = wave * (kChunk / WAVES) + lane;  // the wave's consecutive slots of the chunk
+  uint32_t keys[kChunkKeys];
+  if (PHASE == 1) {
+    const float* w = a.w + ((int64_t)lb * a.Hkv + g) * a.cap;
+    float x[kChunkKeys];
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) x[i] = slot_weight(a, w, min(ch * kChunk + c0 + 64 * i, n - 1));
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) keys[i] = slot_key(a, x[i], ch * kChunk + c0 + 64 * i, n);
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) kp[c0 + 64 * i] = keys[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) keys[i] = kp[c0 + 64 * i];
+  }
+  auto hist_of = [&](int level, int c) {
+    return ws.hist + (((int64_t)level * rows + row) * chunks + c) * kSelBuckets;
+  };
+  uint32_t prefix = 0, want = (uint32_t)a.keep;
+  if (PHASE > 1) {
+    uint32_t own[kSelBuckets / kChunkThreads];
+#pragma unroll
+    for (int i = 0; i < kSelBuckets / kChunkThreads; ++i) {
+      const int v = tid + i * kChunkThreads;
+      uint32_t sum = 0;
+      for (int c = 0; c < used; ++c) sum += hist_of(PHASE - 2, c)[v];
+      hist[v] = sum;
+      own[i] = hist_of(PHASE - 2, ch)[v];
+    }
+    if (PHASE > 2) {
+      prefix = ws.found[row * 2];
+      want = ws.found[row * 2 + 1];
+    }
+    if (PHASE > 3) {
+      prefix = (prefix << 11) | ws.found[(rows + row) * 2];
+      want = ws.found[(rows + row) * 2 + 1];
+    }
+    __syncthreads();
+    if (wave == 0) find_bucket(hist, want, found);
+    __syncthreads();
+    const uint32_t bucket = found[0];
+    want = found[1];
+    if (PHASE < 4) {
+      uint32_t up = 0;
+#pragma unroll
+      for (int i = 0; i < kSelBuckets / kChunkThreads; ++i) up += tid + i * kChunkThreads > (int)bucket ? own[i] : 0u;
+      up = block_sum(up, &cell);
+      if (tid == 0) ws.above[((int64_t)(PHASE - 2) * rows + row) * chunks + ch] = up;
+      if (tid == 0 && ch == 0) {
+        ws.found[((PHASE - 2) * rows + row) * 2] = bucket;
+        ws.found[((PHASE - 2) * rows + row) * 2 + 1] = want;
+      }
+    }
+    prefix = __builtin_amdgcn_readfirstlane((prefix << (PHASE == 4 ? 10 : 11)) | bucket);
+  }
+  if (PHASE < 4) {
+    constexpr int shift = PHASE == 1 ? 21 : (PHASE == 2 ? 10 : 0), bits = PHASE == 3 ? 10 : 11;
+    __syncthreads();
+    for (int i = tid; i < kSelBuckets; i += kChunkThreads) hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i)
+      count_bucket(hist, (keys[i] >> shift) & ((1u << bits) - 1u), (keys[i] >> (shift + bits - 1)) >> 1 == prefix);
+    __syncthreads();
+    uint32_t* h = hist_of(PHASE - 1, ch);
+    for (int i = tid; i < kSelBuckets; i += kChunkThreads) h[i] = hist[i];
+    return;
+  }
+  // the slots above the key and equal to it in the chunks before, then in the waves before
+  uint32_t gt = 0, eq = 0;
+  for (int c = 0; c < ch; ++c) {
+    const uint32_t* h = hist_of(2, c);
+    for (int v = tid; v < 1024; v += kChunkThreads) {
+      const uint32_t x = h[v];
+      gt += v > (int)found[0] ? x : 0u;
+      eq += v == (int)found[0] ? x : 0u;
+    }
+    if (tid < 2) gt += ws.above[((int64_t)tid * rows + row) * chunks + c];
+  }
+  gt = block_sum(gt, &cell);
+  __syncthreads();
+  eq = block_sum(eq, &cell);
+  uint32_t wg = 0, we = 0;
+#pragma unroll
+  for (int i = 0; i < kChunkKeys; ++i) {
+    wg += __popcll(__ballot(keys[i] > prefix));
+    we += __popcll(__ballot(keys[i] == prefix));
+  }
+  if (lane == 0) tot[wave] = make_uint2(wg, we);
+  __syncthreads();
+  for (int v = 0; v < wave; ++v) {
+    gt += tot[v].x;
+    eq += tot[v].y;
+  }
+  const uint64_t below = (1ull << lane) - 1ull;
+#pragma unroll
+  for (int i = 0; i < kChunkKeys; ++i) {
+    const uint32_t k = keys[i];
+    const uint64_t mg = __ballot(k > prefix), me = __ballot(k == prefix);
+    const uint32_t ga = gt + __popcll(mg & below), ea = eq + __popcll(me & below);
+    if (k > prefix || (k == prefix && ea < want)) idx[ga + min(ea, want)] = ch * kChunk + c0 + 64 * i;
+    gt += __popcll(mg);
+    eq += __popcll(me);
+  }
+}
+
+// Rows in chunks, or a block per row: chunks while they leave CUs idle, and a little longer
+// where a block per row would also add up the heads alone.  Measured with the move of the
+// slots, chunks / rows, us: 50 rows of 32329 39 / 47; 64 of 65536 270 / 263; 256 of 32000
+// 89 / 63; 8 of 9000 29 / 18; 12 rows of 29725 over 8 heads 52 / 97.
+bool select_in_chunks(int64_t rows, int cap, bool summed) {
+  return cap > (summed ? kChunk : 2 * kChunk) && rows * ceil_div(cap, kChunk) <= (summed ? 512 : 256);
+}
+
+size_t select_layout(int64_t rows, int cap, bool summed, char* base, ChunkWs* ws) {
+  if (!select_in_chunks(rows, cap, summed)) return 0;
+  const size_t chunks = ceil_div(cap, kChunk);
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    char* p = base ? base + off : nullptr;
+    off = align_up(off + n * sizeof(uint32_t), 256);
+    return reinterpret_cast<uint32_t*>(p);
+  };
+  ChunkWs w;
+  w.keys = take(rows * chunks * kChunk);
+  w.hist = take(3 * rows * chunks * kSelBuckets);
+  w.found = take(4 * rows);
+  w.above = take(2 * rows * chunks);
+  if (ws) *ws = w;
+  return off;
+}
+
+bool select_shape_ok(int L, int B, int Hkv, int cap, int shared) {
+  return L >= 1 && B >= 1 && Hkv >= 1 && cap >= 1 && (shared == 0 || shared == 1) &&
+         (int64_t)L * B * (shared ? 1 : Hkv) < (1 << 22);
 }
 
 struct CompactArgs {
@@ -273,9 +464,16 @@ __global__ void __launch_bounds__(256) cache_move_kernel(CompactArgs a, int cw) 
 
 using namespace spider;
 
+extern "C" size_t spider_cache_select_workspace_size(int L, int B, int Hkv, int cap, int shared) {
+  return select_shape_ok(L, B, Hkv, cap, shared) ? select_layout((int64_t)L * B * (shared ? 1 : Hkv), cap, shared && Hkv > 1, nullptr,
+                                                               nullptr)
+                                                 : 0;
+}
+
 extern "C" spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* weights, const int32_t* lens,
                                              int keep, int n_first, int n_last, int shared, int32_t* idx_out,
-                                             int32_t* len_out, spider_stream stream) {
+                                             int32_t* len_out, void* workspace, size_t workspace_bytes,
+                                             spider_stream stream) {
   clear_error();
   SPIDER_REQUIRE(weights && lens && idx_out && len_out, SPIDER_ERR_INVALID_ARG, "spider_cache_select: null pointer");
   SPIDER_REQUIRE(L >= 1 && B >= 1 && Hkv >= 1 && cap >= 1, SPIDER_ERR_INVALID_ARG,
@@ -289,9 +487,26 @@ extern "C" spider_status spider_cache_select(int L, int B, int Hkv, int cap, con
   const int G = shared ? 1 : Hkv;
   SPIDER_REQUIRE((int64_t)L * B * G < (1 << 22), SPIDER_ERR_UNSUPPORTED,
                  "spider_cache_select: layers * samples * head groups must be below 2^22");
+  const size_t need = select_layout((int64_t)L * B * G, cap, G != Hkv, nullptr, nullptr);
+  SPIDER_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), SPIDER_ERR_WORKSPACE,
+                 "spider_cache_select: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
+  SPIDER_REQUIRE(need == 0 || reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG,
+                 "spider_cache_select: workspace must be 256-byte aligned");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_CACHE_SELECT, st);
   const SelectArgs a{weights, lens, idx_out, len_out, L, B, Hkv, G, cap, keep, n_first, n_last};
+  if (need) {
+    ChunkWs ws;
+    select_layout((int64_t)L * B * G, cap, G != Hkv, reinterpret_cast<char*>(workspace), &ws);
+    const int chunks = ceil_div(cap, kChunk);
+    const unsigned blocks = (unsigned)(L * B * G * chunks);
+    cache_select_chunk_kernel<1><<<blocks, kChunkThreads, 0, st>>>(a, ws, chunks);
+    cache_select_chunk_kernel<2><<<blocks, kChunkThreads, 0, st>>>(a, ws, chunks);
+    cache_select_chunk_kernel<3><<<blocks, kChunkThreads, 0, st>>>(a, ws, chunks);
+    cache_select_chunk_kernel<4><<<blocks, kChunkThreads, 0, st>>>(a, ws, chunks);
+    SPIDER_LAUNCHED("cache_select_chunk");
+    return SPIDER_OK;
+  }
   // the smallest block whose registers hold a row
   const unsigned rows = (unsigned)(L * B * G);
   if (cap <= 256 * 16) cache_select_kernel<256, 16><<<rows, 256, 0, st>>>(a);

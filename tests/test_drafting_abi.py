@@ -82,12 +82,21 @@ def test_tree_attention_workspace_of_bad_sizes_is_zero(L):
     (dict(w=None), INVALID), (dict(lens=None), INVALID), (dict(idx=None), INVALID), (dict(new=None), INVALID),
     (dict(L=0), INVALID), (dict(cap=0), INVALID), (dict(keep=0), INVALID), (dict(first=-1), INVALID),
     (dict(last=-1), INVALID), (dict(shared=2), INVALID), (dict(first=6, last=5), SHAPE), (dict(keep=101), SHAPE),
-    (dict(first=2147483647, last=2147483647), SHAPE), (dict(L=65536, B=65536), UNSUPPORTED)])
+    (dict(first=2147483647, last=2147483647), SHAPE), (dict(L=65536, B=65536), UNSUPPORTED),
+    (dict(cap=20000, wsb=64), WORKSPACE), (dict(cap=20000, ws=None), WORKSPACE), (dict(cap=20000, ws=P + 64), INVALID)])
 def test_cache_select_refusals(L, kw, status):
-    a = dict(L=2, B=2, Hkv=2, cap=100, w=P, lens=P, keep=10, first=2, last=3, shared=0, idx=P, new=P)
+    a = dict(L=2, B=2, Hkv=2, cap=100, w=P, lens=P, keep=10, first=2, last=3, shared=0, idx=P, new=P,
+             ws=P, wsb=1 << 30)
     a.update(kw)
     assert L.spider_cache_select(*a.values(), None) == status
     assert b"spider_cache_select" in L.spider_last_error()
+
+
+def test_cache_select_workspace_of_bad_sizes_is_zero(L):
+    f = L.spider_cache_select_workspace_size
+    assert f(2, 2, 2, 100, 0) == 0 and f(2, 2, 2, 20000, 0) > f(2, 2, 2, 20000, 1) > 0
+    for bad in ((0, 2, 2, 20000, 0), (2, 2, 2, 0, 0), (2, 2, 2, 20000, 2), (65536, 65536, 1, 20000, 0)):
+        assert f(*bad) == 0
 
 
 @pytest.mark.parametrize("kw,status", [

@@ -40,6 +40,10 @@ def weights(kind, shape, rng):
     ((1, 1, 2, 5000), [4999], 4998, 2, 0),
     ((1, 2, 2, 9), [9, -3], 9, 0, 0),
     ((2, 1, 1, 20000), [20000], 1234, 10, 20),
+    ((1, 3, 2, 16385), [16385, 16384, 8193], 8192, 3, 5),
+    ((1, 2, 3, 8200), [8193, 8192], 8000, 0, 7999),
+    ((2, 2, 2, 24600), [24577, 40], 24576, 0, 1),
+    ((1, 1, 300, 33000), [30001], 77, 1, 1),
 ])
 def test_select(kind, shared, shape, lens, keep, first, last):
     lib = need_gpu()
