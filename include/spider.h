@@ -583,7 +583,7 @@ spider_status spider_decode_tree(const spider_decoder_cfg* cfg, const spider_lay
  * weights device fp32 [L][B][Hkv][cap]; idx_out device int32
  * [L][B][shared ? 1 : Hkv][keep]: the kept slots ascending, then -1; len_out
  * device int32 [B] = min(n, keep).  Requires n_first + n_last <= keep <= cap and
- * fewer than 2^22 rows (L * B * groups).  Workspace:
+ * fewer than 2^22 rows (L * B * groups), cap <= 2^30.  Workspace:
  * spider_cache_select_workspace_size(...) bytes (0 for short or many rows),
  * 256-byte aligned.
  * ------------------------------------------------------------------------ */
@@ -612,7 +612,7 @@ spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* w
  * Otherwise input and output must not overlap.  Slots that nothing is moved
  * to are left as they were.
  * Requires dh <= 256, dh and the strides multiples of 16 bytes, caches 16-byte
- * aligned, L * B * Hkv <= 65535.  No workspace.
+ * aligned, L * B * Hkv <= 65535, n_max <= 2^25.  No workspace.
  * ------------------------------------------------------------------------ */
 spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spider_dtype dtype, const void* k_in,
                                    const void* v_in, const int64_t in_strides[4], int cap_in, void* k_out,

@@ -362,7 +362,7 @@ size_t select_layout(int64_t rows, int cap, bool summed, char* base, ChunkWs* ws
 }
 
 bool select_shape_ok(int L, int B, int Hkv, int cap, int shared) {
-  return L >= 1 && B >= 1 && Hkv >= 1 && cap >= 1 && (shared == 0 || shared == 1) &&
+  return L >= 1 && B >= 1 && Hkv >= 1 && cap >= 1 && cap <= (1 << 30) && (shared == 0 || shared == 1) &&
          (int64_t)L * B * (shared ? 1 : Hkv) < (1 << 22);
 }
 
@@ -485,8 +485,8 @@ extern "C" spider_status spider_cache_select(int L, int B, int Hkv, int cap, con
                  "spider_cache_select: n_first + n_last = %lld exceed keep = %d", (long long)n_first + n_last, keep);
   SPIDER_REQUIRE(keep <= cap, SPIDER_ERR_SHAPE, "spider_cache_select: keep = %d exceeds cap = %d", keep, cap);
   const int G = shared ? 1 : Hkv;
-  SPIDER_REQUIRE((int64_t)L * B * G < (1 << 22), SPIDER_ERR_UNSUPPORTED,
-                 "spider_cache_select: layers * samples * head groups must be below 2^22");
+  SPIDER_REQUIRE((int64_t)L * B * G < (1 << 22) && cap <= (1 << 30), SPIDER_ERR_UNSUPPORTED,
+                 "spider_cache_select: layers * samples * head groups below 2^22, cap at most 2^30");
   const size_t need = select_layout((int64_t)L * B * G, cap, G != Hkv, nullptr, nullptr);
   SPIDER_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), SPIDER_ERR_WORKSPACE,
                  "spider_cache_select: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
@@ -553,8 +553,8 @@ extern "C" spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spi
                  SPIDER_ERR_INVALID_ARG, "spider_cache_compact: keys, values and weights all move in place or none");
   SPIDER_REQUIRE(!inplace || same, SPIDER_ERR_SHAPE,
                  "spider_cache_compact: in place, the strides and capacities of both sides must be the same");
-  SPIDER_REQUIRE((int64_t)L * B * Hkv <= 65535, SPIDER_ERR_UNSUPPORTED,
-                 "spider_cache_compact: L * B * Hkv must be at most 65535");
+  SPIDER_REQUIRE((int64_t)L * B * Hkv <= 65535 && n_max <= (1 << 25), SPIDER_ERR_UNSUPPORTED,
+                 "spider_cache_compact: L * B * Hkv at most 65535, n_max at most 2^25");
   if (n_max == 0) return SPIDER_OK;
   CompactArgs a{};
   a.in[0] = reinterpret_cast<const char*>(k_in);

@@ -811,7 +811,7 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
   } else {
     // 16 lanes per row, every 16th split each
     const int r = tid / 16, k = tid % 16;
-    const float2* ml = a.part_ml + ((int64_t)bh * a.T * G + min(r, R - 1)) * a.splits;
+    const float2* ml = a.part_ml + ((int64_t)bh * a.T * G + max(0, min(r, R - 1))) * a.splits;
     float mx = -INFINITY, l = 0.f;
     for (int i = k; i < ns; i += 16) mx = fmaxf(mx, ml[i].x);
     mx = fmaxf(mx, lane_dpp<kDppRor8>(mx));

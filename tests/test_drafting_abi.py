@@ -83,7 +83,7 @@ def test_tree_attention_workspace_of_bad_sizes_is_zero(L):
     (dict(L=0), INVALID), (dict(cap=0), INVALID), (dict(keep=0), INVALID), (dict(first=-1), INVALID),
     (dict(last=-1), INVALID), (dict(shared=2), INVALID), (dict(first=6, last=5), SHAPE), (dict(keep=101), SHAPE),
     (dict(first=2147483647, last=2147483647), SHAPE), (dict(L=65536, B=65536), UNSUPPORTED),
-    (dict(cap=20000, wsb=64), WORKSPACE), (dict(cap=20000, ws=None), WORKSPACE), (dict(cap=20000, ws=P + 64), INVALID)])
+    (dict(cap=(1 << 30) + 1), UNSUPPORTED), (dict(cap=20000, wsb=64), WORKSPACE), (dict(cap=20000, ws=None), WORKSPACE), (dict(cap=20000, ws=P + 64), INVALID)])
 def test_cache_select_refusals(L, kw, status):
     a = dict(L=2, B=2, Hkv=2, cap=100, w=P, lens=P, keep=10, first=2, last=3, shared=0, idx=P, new=P,
              ws=P, wsb=1 << 30)
@@ -105,7 +105,8 @@ def test_cache_select_workspace_of_bad_sizes_is_zero(L):
     (dict(wi=P), INVALID), (dict(wo=P), INVALID), (dict(dh=4), UNSUPPORTED), (dict(dh=264), UNSUPPORTED),
     (dict(k=P + 8), INVALID), (dict(si=(1, 2, 3, 4)), INVALID), (dict(so=(6400, 3200, 32, -16)), INVALID),
     (dict(ko=P), INVALID), (dict(ko=P, vo=2 * P, cap_out=50), SHAPE), (dict(ko=P, vo=2 * P, so=(64, 32, 32, 16)), SHAPE),
-    (dict(ko=P, vo=2 * P, wi=P, wo=2 * P), INVALID), (dict(wi=P, wo=P), INVALID), (dict(B=40000), UNSUPPORTED)])
+    (dict(ko=P, vo=2 * P, wi=P, wo=2 * P), INVALID), (dict(wi=P, wo=P), INVALID), (dict(B=40000), UNSUPPORTED),
+    (dict(n=(1 << 25) + 1), UNSUPPORTED)])
 def test_cache_compact_refusals(L, kw, status):
     a = dict(L=2, B=2, Hkv=2, dh=16, dt=1, k=P, v=2 * P, si=(6400, 3200, 32, 16), cap=100, ko=3 * P, vo=4 * P,
              so=(6400, 3200, 32, 16), cap_out=100, idx=P, il=1, ih=1, n=5, count=None, base=None, wi=None, wo=None)

@@ -236,6 +236,56 @@ def test_node_counts_outside_the_tree_are_taken_into_it():
     assert (out[0] == 2).all() and (out[2] == 2).all()
 
 
+@pytest.mark.parametrize("T", [2, 40])
+def test_samples_without_nodes_pass_their_weights_on(T):
+    """No live node, over one tile and over many splits: the context's weights go through unchanged."""
+    lib = need_gpu()
+    q, k, v = make(3, T, 4, 2, 64, 3100, "bf16", 13)
+    lens, nodes = [3000, 20, 3000], [0, 0, 1]
+    w_in, w_out = torch.rand(3, 2, 3100).cuda(), torch.full((3, 2, 3100), -2.0).cuda()
+    out = torch.full_like(q, 2.0)
+    lib.tree_attention(q, k, v, torch.tensor(lens, dtype=torch.int32).cuda(), out=out, weights_in=w_in, weights_out=w_out,
+                       n_nodes=torch.tensor(nodes, dtype=torch.int32).cuda())
+    for b in (0, 1):
+        assert torch.equal(w_out[b, :, :lens[b]], w_in[b, :, :lens[b]]) and (w_out[b, :, lens[b]:] == -2).all()
+    assert (out[:2] == 2).all()
+    ref, wref = od.tree_attention(np64(q), np64(k), np64(v), lens, n_nodes=nodes, weights_in=np64(w_in))
+    mean_abs = od.tree_attention(np64(q), np64(k), np.abs(np64(v)), lens, n_nodes=nodes)[0]
+    check(out, ref, "bf16", mean_abs)
+    assert np.abs(np64(w_out)[2, :, :3001] - wref[2, :, :3001]).max() <= 2e-5
+
+
+@pytest.mark.parametrize("dtype,T", [("bf16", 3), ("bf16", 50), ("f32", 3), ("f32", 30)])
+@pytest.mark.parametrize("scale", [-0.2, 0.0])
+def test_scales_of_any_sign(scale, dtype, T):
+    lib = need_gpu()
+    q, k, v = make(1, T, 4, 2, 64, 900, dtype, 14)
+    w = torch.zeros(1, 2, 900).cuda()
+    out = lib.tree_attention(q, k, v, torch.tensor([800], dtype=torch.int32).cuda(), scale=scale, weights_out=w)
+    ref, wref = od.tree_attention(np64(q), np64(k), np64(v), [800], scale=scale)
+    mean_abs = od.tree_attention(np64(q), np64(k), np.abs(np64(v)), [800], scale=scale)[0] if dtype == "bf16" else None
+    check(out, ref, dtype, mean_abs)
+    live = ~np.isnan(wref)
+    assert np.abs(np64(w)[live] - wref[live]).max() <= 2e-5 * wref[live].max() + 1e-6
+
+
+@pytest.mark.parametrize("T", [3, 50])
+def test_two_calls_at_once_on_two_streams(T):
+    lib = need_gpu()
+    args = [make(2, T, 8, 2, 128, 2000, "bf16", s) for s in (15, 16)]
+    ln = torch.tensor([1900, 333], dtype=torch.int32).cuda()
+    want = [lib.tree_attention(*a, ln) for a in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for s, a in zip(streams, args):
+            with torch.cuda.stream(s):
+                got.append(lib.tree_attention(*a, ln))
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_large_scores_keep_the_softmax_exact():
     """Scores in the hundreds, the largest late in the cache."""
     lib = need_gpu()
