@@ -1,6 +1,9 @@
 // Eviction from a key/value cache by accumulated attention weight:
 // spider_cache_select chooses the slots a cache keeps, spider_cache_compact
 // moves their keys, values and weights to the front.
+// Measured on one MI355X: 1024 rows of 2944 slots, 576 kept, selection 19 us, copy of
+// their keys and values (bf16 of 128) into another cache 119 us (5.1 TB/s); 64 rows of
+// 65536, 16384 kept, 58 and 209 us (5.1 TB/s).
 #include <cmath>
 
 #include "kernels.h"

@@ -57,6 +57,7 @@ CASES = [
     (2, 3, 32064, 1500, "bf16", 300, "rows"),
     (1, 1, 151001, 9000, "f32", 20, "one"),
     (2, 2, 32768, 100, "f32", 600, "rows"),
+    (1, 2, 20001, 300, "bf16", 5, "rows"),
     (1, 2, 32769, 100, "bf16", 3, "rows"),
     (1, 1, 65540, 3000, "f32", 1500, None),
     (2, 1, 70001, 50, "bf16", 0, None),

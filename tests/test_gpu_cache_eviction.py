@@ -67,6 +67,14 @@ def test_select_from_a_long_cache(keep):
     assert np.array_equal(new.cpu().numpy(), rnew) and np.array_equal(idx.cpu().numpy(), ref)
 
 
+def test_select_from_many_long_rows():
+    lib = need_gpu()
+    w = weights("ties", (1, 1, 30, 66000), np.random.default_rng(8))
+    idx, new = lib.cache_select(torch.from_numpy(w).cuda(), torch.tensor([20001], dtype=torch.int32).cuda(), 6000, n_last=50)
+    ref, rnew = od.cache_select(w, [20001], 6000, 0, 50)
+    assert np.array_equal(new.cpu().numpy(), rnew) and np.array_equal(idx.cpu().numpy(), ref)
+
+
 def caches(L, B, cap, Hkv, dh, dtype, heads_first, seed):
     g = torch.Generator().manual_seed(seed)
     shape = (L, B, Hkv, cap, dh) if heads_first else (L, B, cap, Hkv, dh)

@@ -73,6 +73,9 @@ CASES = [
     (1, 1, 8, 1, 256, [3001], "bf16", False, True),
     (1, 33, 12, 4, 40, [513], "bf16", True, False),
     (1, 60, 2, 2, 64, [700], "bf16", False, True),
+    (1, 20, 2, 2, 64, [300], "bf16", False, True),
+    (1, 5, 4, 2, 96, [300], "bf16", False, True),
+    (1, 8, 2, 2, 256, [130], "f32", False, True),
     (1, 100, 2, 2, 64, [333], "bf16", True, False),
     (2, 20, 2, 2, 128, [450, 31], "bf16", False, True),
     (1, 61, 2, 2, 128, [1999], "bf16", True, True),
