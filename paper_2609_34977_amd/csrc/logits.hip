@@ -155,11 +155,19 @@ __global__ void __launch_bounds__(THREADS) adjust_kernel(AdjustArgs a) {
     const int i = VEC * (tid + u * THREADS);
     if (i >= nv) break;
     const uint32_t skip = a.n_bias ? biased[i >> 5] >> (i & 31) : 0u;
+    uint32_t c[VEC], any = 0;  // few tokens of a vocabulary were said: one test for VEC of them
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) any |= c[e] = count[i + e];
+    if (any) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) z[u][e] = penalised(z[u][e], c[e], rep, freq, pres);
+    }
+    const uint32_t allowed = word[u] >> (i & 31);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      float y = penalised(z[u][e], count[i + e], rep, freq, pres);
+      float y = z[u][e];
       if (a.n_bias) y = __fadd_rn(y, 0.f);
-      if (!((word[u] >> ((i + e) & 31)) & 1u)) y = -INFINITY;
+      if (!((allowed >> e) & 1u)) y = -INFINITY;
       z[u][e] = y;
       if (y > best && !((skip >> e) & 1u)) {
         best = y;
