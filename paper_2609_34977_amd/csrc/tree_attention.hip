@@ -864,51 +864,75 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
     if (j + i < n) a.w_out[at + i] = (j + i < ext.x && a.w_in ? a.w_in[at + i] : 0.f) + sum[i];
 }
 
-// The weight of every slot: a wave per KEYS keys of one kv head, all live rows of the
-// head group in tiles of 16; exp2(s - max) / sum from the rows' final statistics.
-template <typename AT, int DH, bool FULL>
+// The weight of every slot, of more rows than keep their scores: a wave per NT tiles of keys
+// of one kv head, which stay in registers, all live rows of the head group in tiles of 16;
+// exp2(s - max) / sum from the rows' final statistics.  Two tiles share each reading of the
+// queries (244 rows over 8 x 8 x 16384 keys, whole call: 438 -> 355 us), where that
+// leaves enough blocks (70 rows over 2 x 8 x 500 keys, whole call: one tile 29.5, two 33.4)
+// and registers (width 256 has none).
+template <typename AT, int DH, bool FULL, int NT>
 __global__ void __launch_bounds__(256) tree_weights_kernel(TreeArgs a) {
   using T = TreeTile<AT, DH>;
-  constexpr int KEYS = T::KEYS, KT = T::KT;
+  constexpr int KEYS = T::KEYS, NS = 4 * T::KT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int m = lane & 15, g = lane >> 4;
-  const int blocks = (a.cap + 4 * KEYS - 1) / (4 * KEYS), bh = blockIdx.x / blocks;
+  const int blocks = (a.cap + 4 * NT * KEYS - 1) / (4 * NT * KEYS), bh = blockIdx.x / blocks;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const int G = a.H / a.Hkv;
   const int2 ext = tree_extent(a, b);
   const int n = ext.x + ext.y, R = ext.y * G;
-  const int j0 = (4 * (blockIdx.x % blocks) + wave) * KEYS;
+  const int j0 = (4 * (blockIdx.x % blocks) + wave) * NT * KEYS;
   if (j0 >= n) return;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
-  typename T::K k;
-  T::template load_k<FULL>(k, reinterpret_cast<const AT*>(a.k) + b * a.kvb + hk * a.kvh, a.kvs, j0, n, lane, a.dh);
-  const bool tail = j0 + KEYS > ext.x;
-  float acc[KT * 4] = {};
-  for (int r0 = 0; r0 < R; r0 += 16) {
-    const int row = min(r0 + m, R - 1), t = row / G, h = hk * G + row % G;
-    typename T::Q q;
-    T::template load_q<FULL>(q, reinterpret_cast<const AT*>(a.q) + b * a.qb + t * a.qt + (int64_t)h * a.dh, g, a.dh,
-                             a.scale < 0.f);
-    const float2 st = a.stat[((int64_t)b * a.T + t) * a.H + h];
-    floatx4 s[KT];
-    T::scores(s, k, q);
-    uint32_t w = ~0u;
-    if (tail) w = tree_window<KEYS>(a, b, t, j0, ext);
-    if (r0 + m >= R) w = 0;
-    w >>= 4 * g;
+  typename T::K k[NT];
 #pragma unroll
-    for (int i = 0; i < KT * 4; ++i) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], sc, -st.x)) * st.y;
-      acc[i] += (w >> (i / 4 * 16 + i % 4)) & 1u ? e : 0.f;
+  for (int u = 0; u < NT; ++u)
+    T::template load_k<FULL>(k[u], reinterpret_cast<const AT*>(a.k) + b * a.kvb + hk * a.kvh, a.kvs, j0 + u * KEYS, n,
+                             lane, a.dh);
+  const bool tail = j0 + NT * KEYS > ext.x;
+  float acc[NT][NS] = {};
+  const int dt = 16 / G, dg = 16 % G;
+  int t = m / G, gi = m % G;  // node and head of the group of row r0 + m
+  for (int r0 = 0; r0 < R; r0 += 16) {
+    const bool on = r0 + m < R;
+    const int node = on ? t : ext.y - 1, h = hk * G + (on ? gi : G - 1);
+    typename T::Q q;
+    T::template load_q<FULL>(q, reinterpret_cast<const AT*>(a.q) + b * a.qb + node * a.qt + (int64_t)h * a.dh, g, a.dh,
+                             a.scale < 0.f);
+    const float2 st = a.stat[((int64_t)b * a.T + node) * a.H + h];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      floatx4 s[T::KT];
+      T::scores(s, k[u], q);
+      if (tail || r0 + 16 > R) {
+        const uint32_t w = (on ? tree_window<KEYS>(a, b, node, j0 + u * KEYS, ext) : 0u) >> (4 * g);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], sc, -st.x)) * st.y;
+          acc[u][i] += (w >> (i / 4 * 16 + i % 4)) & 1u ? e : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+          acc[u][i] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], sc, -st.x)), st.y, acc[u][i]);
+      }
+    }
+    t += dt;
+    gi += dg;
+    if (gi >= G) {
+      gi -= G;
+      ++t;
     }
   }
 #pragma unroll
-  for (int i = 0; i < KT * 4; ++i) {
-    const float x = row16_sum(acc[i]);
-    const int j = j0 + 16 * (i / 4) + 4 * g + i % 4;
-    const int64_t at = (int64_t)bh * a.cap + j;
-    if (m == i && j < n) a.w_out[at] = (j < ext.x && a.w_in ? a.w_in[at] : 0.f) + x;
-  }
+  for (int u = 0; u < NT; ++u)
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const float x = row16_sum(acc[u][i]);
+      const int j = j0 + u * KEYS + 16 * (i / 4) + 4 * g + i % 4;
+      const int64_t at = (int64_t)bh * a.cap + j;
+      if (m == i && j < n) a.w_out[at] = (j < ext.x && a.w_in ? a.w_in[at] : 0.f) + x;
+    }
 }
 
 // Tiles, row groups and splits of a call, and its workspace.
@@ -937,7 +961,8 @@ TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype d
     // (width 256 has no registers for two waves per SIMD)
     p.nw = R <= 2 * wave_rows ? 2 : (R <= 4 * wave_rows || p.dhp == 256 ? 4 : 8);
     rows = wave_rows * p.nw;
-    target = 256 * 8 / p.nw;
+    // eight waves per CU; width 256 leaves LDS for one block
+    target = p.dhp == 256 ? 256 : 256 * 8 / p.nw;
   }
   p.groups = ceil_div(R, rows);
   p.min_tiles = 8;
@@ -979,11 +1004,11 @@ void launch_tree_rows(const TreeArgs& a, hipStream_t st) {
   else tree_rows_kernel<DH, NW, false><<<tree_blocks(a), 64 * NW, 0, st>>>(a);
 }
 
-template <typename AT, int DH>
+template <typename AT, int DH, int NT>
 void launch_tree_weights(const TreeArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)ceil_div(a.cap, 4 * TreeTile<AT, DH>::KEYS) * (unsigned)(a.B * a.Hkv);
-  if (a.dh == DH) tree_weights_kernel<AT, DH, true><<<grid, 256, 0, st>>>(a);
-  else tree_weights_kernel<AT, DH, false><<<grid, 256, 0, st>>>(a);
+  const unsigned grid = (unsigned)ceil_div(a.cap, 4 * NT * TreeTile<AT, DH>::KEYS) * (unsigned)(a.B * a.Hkv);
+  if (a.dh == DH) tree_weights_kernel<AT, DH, true, NT><<<grid, 256, 0, st>>>(a);
+  else tree_weights_kernel<AT, DH, false, NT><<<grid, 256, 0, st>>>(a);
 }
 
 template <typename AT, int DH>
@@ -1008,7 +1033,13 @@ spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   }
   if (a.w_out && !a.scores) {
     ProfScope ps(KC_TREE_WEIGHTS, st);
-    launch_tree_weights<AT, DH>(a, st);
+    const bool two = (int64_t)a.B * a.Hkv * ceil_div(a.cap, 8 * TreeTile<AT, DH>::KEYS) >= 512;
+    if constexpr (DH <= 128) {
+      if (two) launch_tree_weights<AT, DH, 2>(a, st);
+      else launch_tree_weights<AT, DH, 1>(a, st);
+    } else {
+      launch_tree_weights<AT, DH, 1>(a, st);
+    }
     SPIDER_LAUNCHED("tree_weights");
   }
   return SPIDER_OK;

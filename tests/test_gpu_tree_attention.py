@@ -239,6 +239,22 @@ def test_node_counts_outside_the_tree_are_taken_into_it():
     assert (out[0] == 2).all() and (out[2] == 2).all()
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 40), ("bf16", 128), ("bf16", 96), ("f32", 64), ("f32", 36),
+                                      ("f32", 128), ("f32", 100)])
+def test_weights_of_many_rows_over_many_heads(dtype, dh):
+    """Enough blocks for the weights pass that takes two tiles of keys at a time."""
+    lib = need_gpu()
+    B, T, Hkv, cap = 8, 9, 16, 1100 if dtype == "bf16" else 600
+    lens = [cap - 10 - 97 * b % 500 for b in range(B)]
+    q, k, v = make(B, T, 2 * Hkv, Hkv, dh, cap, dtype, 17, spread=1.5)
+    w_in, w_out = torch.rand(B, Hkv, cap).cuda(), torch.full((B, Hkv, cap), -7.0).cuda()
+    lib.tree_attention(q, k, v, torch.tensor(lens, dtype=torch.int32).cuda(), weights_in=w_in, weights_out=w_out)
+    _, ref = od.tree_attention(np64(q), np64(k), np64(v), lens, weights_in=np64(w_in))
+    live = ~np.isnan(ref)
+    assert (np64(w_out)[~live] == -7.0).all()
+    assert np.abs(np64(w_out)[live] - ref[live]).max() <= 2e-5 * ref[live].max() + 1e-6
+
+
 @pytest.mark.parametrize("T", [2, 40])
 def test_samples_without_nodes_pass_their_weights_on(T):
     """No live node, over one tile and over many splits: the context's weights go through unchanged."""
