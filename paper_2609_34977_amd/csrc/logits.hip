@@ -1,8 +1,8 @@
 // Rules of a sampler on logits (spider_adjust_logits): penalties for tokens that
 // were said before, biases, a grammar mask, and the arg max of what is left.
 // One reading and one writing of the logits.  Measured on one MI355X: 248 rows of 32000
-// (fp32, mask, 100 biases, 2900 tokens) 18.5 us, 3.4 TB/s; 64 rows of 151000 (bf16, 300
-// biases, 12000 tokens) 26.4 us, 2.3 TB/s; one row of 32000 11.6 us.
+// (fp32, mask, 100 biases, 2900 tokens) 18.0 us, 3.5 TB/s; 64 rows of 151000 (bf16, 300
+// biases, 12000 tokens) 25.9 us, 2.3 TB/s; one row of 32000 11.0 us.
 #include <cmath>
 
 #include "kernels.h"
