@@ -333,9 +333,16 @@ __device__ __forceinline__ uint32_t tree_window(const TreeArgs& a, int b, int t,
   return (uint32_t)x & v & (KEYS == 32 ? ~0u : (1u << KEYS) - 1u);
 }
 
-// Splits of the keys of one sample: at most a.splits, each of at least a.min_tiles tiles.
-__device__ __forceinline__ int tree_splits(const TreeArgs& a, int tiles) {
-  return max(1, min(a.splits, tiles / a.min_tiles));
+// Splits of the keys of one sample and the tiles of each: at most a.splits, each of at
+// least a.min_tiles tiles, and no more of them than have a tile (129 tiles in 16 splits of
+// 9 are 15): a block without one would end with its first fetches in flight.
+struct TreeSplits {
+  int n, tiles;
+};
+__device__ __forceinline__ TreeSplits tree_splits(const TreeArgs& a, int tiles) {
+  const int most = max(1, min(a.splits, tiles / a.min_tiles));
+  const int per = max(1, (tiles + most - 1) / most);
+  return TreeSplits{most == 1 ? 1 : (tiles + per - 1) / per, per};
 }
 
 // The maximum may lag behind by this much (in powers of two) before the sums are
@@ -500,11 +507,11 @@ __device__ __forceinline__ bool tree_work(const TreeArgs& a, TreeWork& w) {
   w.r0 = slot % a.groups * ROWS;
   if (w.r0 >= w.R) return false;
   const int tiles = (w.n + KEYS - 1) / KEYS;
-  w.ns = tree_splits(a, tiles);
+  const TreeSplits s = tree_splits(a, tiles);
+  w.ns = s.n;
   if (w.split >= w.ns) return false;
-  const int per = (tiles + w.ns - 1) / w.ns;
-  w.t0 = w.split * per;
-  w.t1 = min(tiles, w.t0 + per);
+  w.t0 = w.split * s.tiles;
+  w.t1 = min(tiles, w.t0 + s.tiles);
   return true;
 }
 
@@ -748,7 +755,7 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, float sc) {
   const int2 ext = tree_extent(a, b);
   if (t >= ext.y) return;
   constexpr int KEYS = TreeTile<AT, 64>::KEYS;
-  const int ns = tree_splits(a, (ext.x + ext.y + KEYS - 1) / KEYS);
+  const int ns = tree_splits(a, (ext.x + ext.y + KEYS - 1) / KEYS).n;
   if (ns == 1) return;
   const int G = a.H / a.Hkv, hk = h / G;
   const int64_t part = (((int64_t)b * a.Hkv + hk) * a.T * G + (int64_t)t * G + h % G) * a.splits;
@@ -819,7 +826,7 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
 #pragma unroll
   for (int u = 0; u < 8; ++u)
     if (j < n && u < R) x[u] = *reinterpret_cast<const floatx4*>(s + u * KEYS);
-  const int ns = tree_splits(a, (n + KEYS - 1) / KEYS);
+  const int ns = tree_splits(a, (n + KEYS - 1) / KEYS).n;
   if (ns == 1) {
     if (tid < R) st[tid] = a.stat[((int64_t)b * a.T + tid / G) * a.H + hk * G + tid % G];
   } else {
