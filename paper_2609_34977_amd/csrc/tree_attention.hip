@@ -174,27 +174,28 @@ struct TreeTile<uint16_t, DH> {
     return __builtin_bit_cast(bf16x8, x);
   }
   __device__ static __forceinline__ bf16x8 operand(const Ops& v, int n) { return __builtin_bit_cast(bf16x8, v.f[n]); }
-  // infinite and NaN values become 0; whether there was one
-  __device__ static __forceinline__ uint32_t finite(uint32_t x, bool& bad) {
+  // infinite and NaN values become 0; whether there was one (bits in a register: a flag per
+  // comparison would be a pair of scalar registers each)
+  __device__ static __forceinline__ uint32_t finite(uint32_t x, uint32_t& bad) {
     const uint32_t drop = ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-    bad = bad || drop != 0;
+    bad |= drop;
     return x & ~drop;
   }
   __device__ static __forceinline__ bool drop_nonfinite(V& v) {
-    bool bad = false;
+    uint32_t bad = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
       for (int i = 0; i < VW; ++i) v.w[e][i] = finite(v.w[e][i], bad);
-    return bad;
+    return bad != 0;
   }
   __device__ static __forceinline__ bool drop_nonfinite(Ops& v) {
-    bool bad = false;
+    uint32_t bad = 0;
 #pragma unroll
     for (int n = 0; n < CPL; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) v.f[n][e] = finite(v.f[n][e], bad);
-    return bad;
+    return bad != 0;
   }
   __device__ static __forceinline__ uint32_t pack(float a0, float a1) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
@@ -285,16 +286,17 @@ struct TreeTile<float, DH> {
       for (int c = 0; c < 4; ++c) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[i][c], q.f[i][c], s[0], 0, 0, 0);
   }
   __device__ static __forceinline__ bool drop_nonfinite(V& v) {
-    bool bad = false;
+    uint32_t bad = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int n = 0; n < CPL; ++n) {
-        const bool drop = (__float_as_uint(v.f[e][n / 4][n % 4]) & 0x7F800000u) == 0x7F800000u;
-        bad = bad || drop;
-        if (drop) v.f[e][n / 4][n % 4] = 0.f;
+        const uint32_t x = __float_as_uint(v.f[e][n / 4][n % 4]);
+        const uint32_t drop = (x & 0x7F800000u) == 0x7F800000u ? ~0u : 0u;
+        bad |= drop;
+        v.f[e][n / 4][n % 4] = __uint_as_float(x & ~drop);
       }
-    return bad;
+    return bad != 0;
   }
   __device__ static __forceinline__ float value(const float* p) { return *p; }
   template <int RT, bool TWO, typename S>
@@ -452,7 +454,10 @@ struct RowTiles {
   // add_nonfinite puts them back.
   template <bool tail, typename S>
   __device__ __forceinline__ void add(S& v) {
-    if constexpr (tail) nonfinite = nonfinite || __any(T::drop_nonfinite(v));
+    if constexpr (tail) {
+      const bool dropped = T::drop_nonfinite(v);  // of every tile, whatever the tiles before held
+      if (__any(dropped)) nonfinite = true;
+    }
     T::template values<RT, TWO, S>(o, v, p);
   }
 

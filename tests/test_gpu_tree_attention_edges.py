@@ -1,5 +1,5 @@
 """spider_tree_attention at its edges, against the float64 oracle: splits of the keys that a
-ceiling leaves without a tile.
+ceiling leaves without a tile, hidden infinities and NaN in many tiles.
 
 Bars as in test_gpu_tree_attention.py.
 """
@@ -29,3 +29,42 @@ def test_splits_that_the_tiles_do_not_fill(n, T, H, dh):
     ref, wref = od.tree_attention(np64(q), np64(k), np64(v), [n - T], sees)
     check(out, ref, "bf16", od.tree_attention(np64(q), np64(k), np.abs(np64(v)), [n - T], sees)[0])
     assert np.abs(np64(w)[:, :, :n] - wref[:, :, :n]).max() <= 2e-5 * wref[:, :, :n].max() + 1e-6
+
+
+def same(a, b):
+    """Equal bit for bit, NaN where NaN."""
+    return bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())
+
+
+@pytest.mark.parametrize("dtype,T,H,dh", [
+    ("bf16", 30, 2, 128), ("bf16", 110, 2, 128), ("bf16", 250, 2, 128), ("bf16", 61, 2, 128), ("bf16", 110, 2, 64),
+    ("bf16", 200, 4, 40), ("bf16", 110, 2, 256), ("bf16", 250, 1, 200), ("f32", 200, 2, 64), ("f32", 256, 1, 100),
+    ("f32", 220, 2, 256)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_hidden_slots_in_many_tiles_do_not_count(bad, dtype, T, H, dh):
+    """Bad nodes that nobody sees in every second tile of keys of the tree, one that the last row alone sees, and one
+    bad value of the context in the tile that it shares with the tree: all else keeps its bits."""
+    lib = need_gpu()
+    Hkv, n = min(H, 2), 50
+    q, k, v = make(1, T, H, Hkv, dh, n + T + 9, dtype, T + dh)
+    hidden = list(range(3, T - 2, 16))
+    sees = np.tril(np.ones((1, T, T), bool))
+    sees[0, :, hidden] = False
+    once = T - 3
+    sees[0, :, once] = False
+    sees[0, T - 1, once] = True
+    mask = torch.from_numpy(od.pack_mask(sees)).cuda()
+    ln = torch.tensor([n], dtype=torch.int32).cuda()
+    w, w2 = (torch.zeros(1, Hkv, n + T + 9).cuda() for _ in range(2))
+    clean = lib.tree_attention(q, k, v, ln, tree_mask=mask, weights_out=w).float()
+    k2, v2 = k.clone(), v.clone()
+    at = torch.tensor([n + u for u in hidden]).cuda()
+    k2[:, at], v2[:, at] = bad, bad
+    v2[:, n + once, 0, 1] = bad
+    v2[:, 40, 0, 2] = bad
+    got = lib.tree_attention(q, k2, v2, ln, tree_mask=mask, weights_out=w2).float()
+    G = H // Hkv
+    clean[:, T - 1, :G, 1] = bad
+    clean[:, :, :G, 2] = bad
+    assert same(got, clean)
+    assert torch.equal(w, w2)
