@@ -507,7 +507,9 @@ spider_status spider_tree_mask(int B, int T, const int32_t* parents, uint64_t* m
  *   s(j)  = scale * q[b,t,h] . k[b,j]   over the slots j that the node sees:
  *           j < lens[b], and j = lens[b] + u of the live nodes u of its mask
  *   out   = sum_j softmax(s)(j) v[b,j]      (0 where it sees no slot)
- * Slots that a node does not see do not enter its sums, whatever they hold.
+ * Slots that a node does not see do not enter its sums, whatever they hold; an
+ * infinite or NaN value of a slot that it sees makes its output so, however small
+ * the weight.
  * q element (b,t,h,c) at q[b*q_stride_b + t*q_stride_t + h*dh + c]; k and v
  * element (b,slot,head,c) at [b*kv_stride_b + slot*kv_stride_s +
  * head*kv_stride_h + c] (the decoder's cache of one layer: kv_stride_b = cap*d,

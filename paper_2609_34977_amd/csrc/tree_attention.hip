@@ -351,6 +351,12 @@ __device__ __forceinline__ TreeSplits tree_splits(const TreeArgs& a, int tiles) 
 // rescaled: the exponentials then stay below 2^8.
 constexpr float kLazyMax = 8.f;
 
+// x f of a sum x that goes onto another maximum: an infinite or NaN x stays what it is where
+// f has underflowed to 0.
+__device__ __forceinline__ float rescaled(float x, float f) {
+  return f == 0.f && !(fabsf(x) < INFINITY) ? x : x * f;
+}
+
 // RT row tiles of a wave: queries, and the running maximum, sum and output of their rows.
 // TWO: see TreeTile::values.
 template <typename AT, int DH, int RT, bool TWO>
@@ -363,7 +369,7 @@ struct RowTiles {
   float top[RT], sum[RT];
   float p[RT][NS];
   uint32_t seen[RT];  // the lane's keys of the tile that its row sees, bit i for score i
-  bool nonfinite = false;  // add() left out a value
+  int bad0 = 0x7fffffff, bad1 = -1;  // the first and last tile with an infinite or NaN value, as far as known
 
   template <bool FULL>
   __device__ __forceinline__ void start(const TreeArgs& a, int b, int hk, int r0, int R, int lane) {
@@ -449,37 +455,73 @@ struct RowTiles {
     }
   }
 
-  // the tile's values into the outputs.  Infinite and NaN values count for the rows that
-  // see them and for no other, but 0 times one of them is NaN: they leave the product, and
-  // add_nonfinite puts them back.
-  template <bool tail, typename S>
-  __device__ __forceinline__ void add(S& v) {
-    if constexpr (tail) {
-      const bool dropped = T::drop_nonfinite(v);  // of every tile, whatever the tiles before held
-      if (__any(dropped)) nonfinite = true;
+  // Infinite and NaN values count for the rows that see them and for no other, but 0 times
+  // one of them is NaN.  The values of a tail tile leave the product if they are not finite;
+  // those of other tiles, which all rows see, enter it, where they can give NaN for an
+  // infinite sum (a weight's low part that is 0 or negative, a weight that has underflowed).
+  // settle() puts both right after the loop.
+
+  // whether tile t holds such a value (they become 0)
+  template <typename S>
+  __device__ __forceinline__ void drop(S& v, int t) {
+    const bool dropped = T::drop_nonfinite(v);  // of every tile, whatever the tiles before held
+    if (__any(dropped)) {
+      bad0 = min(bad0, t);
+      bad1 = max(bad1, t);
     }
+  }
+
+  // the values of tile t into the outputs
+  template <bool tail, typename S>
+  __device__ __forceinline__ void add(S& v, int t) {
+    if constexpr (tail) drop(v, t);
     T::template values<RT, TWO, S>(o, v, p);
   }
 
-  // the infinite and NaN values of the keys [j0, j1) into the outputs of the rows that see
-  // them; channel(c, i): of output o[.][c][i]
-  template <typename F>
-  __device__ __forceinline__ void add_nonfinite(const TreeArgs& a, int b, const AT* vb, int j0, int j1, int2 ext,
-                                                F&& channel) {
+  // The outputs, after the tiles t0, t0 + by, .. < full without their nodes and tail tiles
+  // behind them: what a row sees of infinite and NaN values is its output.  (If there was
+  // one in a full tile, then the output is not finite; the tiles are read again to find it.)
+  // channel(c, i): of output o[.][c][i]
+  template <bool FULL, typename F>
+  __device__ __forceinline__ void settle(const TreeArgs& a, int b, const AT* vb, int t0, int by, int full, int n, int2 ext,
+                                         int lane, F&& channel) {
+    bool x = false;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int c = 0; c < CPL; ++c)
-#pragma unroll 1
-        for (int j = j0; j < j1; ++j) {
-          if (!(tree_window<KEYS>(a, b, node[r], j, ext) & 1u)) continue;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int ch = channel(c, i);
-            const float x = ch < a.dh ? T::value(vb + (int64_t)j * a.kvs + ch) : 0.f;
-            if ((__float_as_uint(x) & 0x7F800000u) == 0x7F800000u) o[r][c][i] += x;
+        for (int i = 0; i < 4; ++i) x = x || !(fabsf(o[r][c][i]) < INFINITY);
+    if (__any(x)) {
+#pragma unroll 1
+      for (int t = t0; t < full; t += by) {
+        typename T::V v;
+        T::template load_v<FULL>(v, vb, a.kvs, t * KEYS, n, lane, a.dh);
+        drop(v, t);
+      }
+    }
+    if (bad0 > bad1) return;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) {
+        floatx4 s = floatx4{};
+#pragma unroll 1
+        for (int t = bad0; t <= bad1; t += by)
+#pragma unroll 1
+          for (int j = t * KEYS; j < min(n, (t + 1) * KEYS); ++j) {
+            if (!(tree_window<KEYS>(a, b, node[r], j, ext) & 1u)) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int ch = channel(c, i);
+              const float y = ch < a.dh ? T::value(vb + (int64_t)j * a.kvs + ch) : 0.f;
+              if (!(fabsf(y) < INFINITY)) s[i] += y;
+            }
           }
-        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(fabsf(s[i]) < INFINITY)) o[r][c][i] = s[i];
+      }
   }
 
   // the row's sum, in every lane of its column
@@ -556,16 +598,13 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_ker
     if (t + 4 < w.t1) T::template load_k<FULL>(k, kb, a.kvs, j0 + 4 * KEYS, n, lane, a.dh);
     if constexpr (RT == 1) rows.template soften<tail>(a, b, j0, w.ext, g, sc, kept ? kept + t * tile_scores : nullptr);
     else rows.template soften<tail>(a, b, j0, w.ext, g, sc);
-    rows.template add<tail>(v);
+    rows.template add<tail>(v, t);
   };
   int t = w.t0 + wave;
   for (; t < min(w.t1, w.ext.x / KEYS); t += 4) step(t, std::false_type{});
-  const int tail0 = t;
   for (; t < w.t1; t += 4) step(t, std::true_type{});
-  if (rows.nonfinite)
-    for (t = tail0; t < w.t1; t += 4)
-      rows.add_nonfinite(a, b, vb, t * KEYS, min(n, (t + 1) * KEYS), w.ext,
-                         [&](int c, int i) { return T::channel(c, 4 * g + i); });
+  rows.template settle<FULL>(a, b, vb, w.t0 + wave, 4, min(w.t1, w.ext.x / KEYS), n, w.ext, lane,
+                             [&](int c, int i) { return T::channel(c, 4 * g + i); });
 
   // the waves' sums onto their common maximum, in wave order
 #pragma unroll
@@ -605,7 +644,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_ker
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] += xo[u][row][c + i] * f[u];
+        for (int i = 0; i < 4; ++i) x[i] += rescaled(xo[u][row][c + i], f[u]);
       if (w.ns > 1) {
         *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + c) = x;
       } else {
@@ -704,14 +743,13 @@ __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
       v.f[c] = x;
     }
     rows.template soften<tail>(a, b, 32 * t, w.ext, g, sc);
-    rows.template add<tail>(v);
+    rows.template add<tail>(v, t);
   };
   int t = w.t0;
   for (; t < min(w.t1, w.ext.x / 32); ++t) step(t, std::false_type{});
-  const int tail0 = t;
   for (; t < w.t1; ++t) step(t, std::true_type{});
-  if (rows.nonfinite)
-    rows.add_nonfinite(a, b, vb, 32 * tail0, min(n, 32 * w.t1), w.ext, [&](int c, int i) { return 16 * c + 4 * g + i; });
+  rows.template settle<FULL>(a, b, vb, w.t0, 1, min(w.t1, w.ext.x / 32), n, w.ext, lane,
+                             [&](int c, int i) { return 16 * c + 4 * g + i; });
 
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -791,7 +829,8 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, float sc) {
         const float f = ml[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[u].x - mx) * sc);
         // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
         l += ml[u].x == -INFINITY ? ml[u].y : ml[u].y * f;
-        x += o[u] * f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += rescaled(o[u][i], f);
       }
     }
   }

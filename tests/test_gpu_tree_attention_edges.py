@@ -1,5 +1,5 @@
 """spider_tree_attention at its edges, against the float64 oracle: splits of the keys that a
-ceiling leaves without a tile, hidden infinities and NaN in many tiles.
+ceiling leaves without a tile, hidden infinities and NaN in many tiles, infinite values that count.
 
 Bars as in test_gpu_tree_attention.py.
 """
@@ -68,3 +68,50 @@ def test_hidden_slots_in_many_tiles_do_not_count(bad, dtype, T, H, dh):
     clean[:, :, :G, 2] = bad
     assert same(got, clean)
     assert torch.equal(w, w2)
+
+
+@pytest.mark.parametrize("dtype,T,H,dh", [
+    ("bf16", 1, 2, 128), ("bf16", 5, 2, 128), ("bf16", 5, 2, 64), ("bf16", 20, 2, 96), ("bf16", 9, 2, 256),
+    ("bf16", 40, 2, 128), ("bf16", 70, 4, 128), ("bf16", 150, 2, 56), ("bf16", 40, 2, 256), ("f32", 5, 2, 64),
+    ("f32", 40, 2, 128), ("f32", 20, 2, 252)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("n", [300, 3000])
+def test_infinite_values_of_the_context(n, bad, dtype, T, H, dh):
+    """sum p v of an infinite v is infinite wherever the slot stands, and NaN of both signs; the other channels keep
+    their bits."""
+    lib = need_gpu()
+    q, k, v = make(1, T, H, 2, dh, n + T, dtype, T + dh + n)
+    ln = torch.tensor([n], dtype=torch.int32).cuda()
+    w, w2 = (torch.zeros(1, 2, n + T).cuda() for _ in range(2))
+    clean = lib.tree_attention(q, k, v, ln, weights_out=w).float()
+    v2 = v.clone()
+    v2[:, 17, 0, 3::7] = bad
+    v2[:, 150, 0, 4] = float("inf")
+    v2[:, 201, 0, 4] = -float("inf")
+    got = lib.tree_attention(q, k, v2, ln, weights_out=w2).float()
+    G = H // 2
+    clean[:, :, :G, 3::7] = bad
+    clean[:, :, :G, 4] = float("nan")
+    assert same(got, clean)
+    assert torch.equal(w, w2)
+
+
+@pytest.mark.parametrize("dtype,T,dh", [("bf16", 5, 128), ("bf16", 40, 128), ("bf16", 40, 256), ("f32", 5, 64), ("f32", 40, 128)])
+@pytest.mark.parametrize("n", [300, 3000])
+def test_infinite_values_under_weights_that_vanish(n, dtype, T, dh):
+    """exp(s - max) of the slot is below every fp32 number, not 0: its infinite value still counts."""
+    lib = need_gpu()
+    q, k, v = make(1, T, 2, 2, dh, n + T, dtype, 3)
+    q[..., 0] = 1.0
+    k[..., 0] = 0.0
+    k[:, 230:, :, 0] = 200.0   # scores of 200 and more above those before
+    k[:, 17, :, 0] = -200.0
+    ln = torch.tensor([n], dtype=torch.int32).cuda()
+    clean = lib.tree_attention(q, k, v, ln, scale=1.0).float()
+    v2 = v.clone()
+    v2[:, 17, 0, 3] = float("inf")
+    v2[:, 101, 1, 2] = -float("inf")
+    got = lib.tree_attention(q, k, v2, ln, scale=1.0).float()
+    clean[:, :, 0, 3] = float("inf")
+    clean[:, :, 1, 2] = -float("inf")
+    assert same(got, clean)
