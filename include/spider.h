@@ -525,9 +525,7 @@ spider_status spider_tree_mask(int B, int T, const int32_t* parents, uint64_t* m
  * (the same layout) may be NULL (zeros) or weights_out itself.
  * Precision: products exact, sums, maxima and exponentials fp32, out rounded
  * once.  bf16: the softmax numerators enter the product with v as bf16 high and
- * low parts (16 significant bits); with more than 32 rows per kv head (T * H /
- * Hkv; 16 for dh > 128), where the matrix products bound the time, they are
- * rounded to bf16 once (their sum is not).
+ * low parts (16 significant bits).
  * Requires H % Hkv == 0, T <= 256, dh <= 256, B and H <= 65535, B*H*T and
  * B*Hkv*ceil(cap/64) below 2^24, dh and the strides multiples of 16 bytes, q, k,
  * v, out 16-byte aligned; out overlaps no input.  Workspace:

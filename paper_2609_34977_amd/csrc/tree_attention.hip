@@ -12,8 +12,8 @@
 //   1 row of 32 kv heads over 200 slots             8.8 (host time; the kernel 8)
 //   16 rows of 32 kv heads over 705, weights       15.5
 //   4 rows of 16 x 8 kv heads over 32768            352 (6.1 TB/s), with weights 460
-//   32 rows of 8 x 8 kv heads over 16384            111 (4.8 TB/s)
-//   61 / 244 rows of 8 x 8 kv heads over 16384      129 / 184..192
+//   32 rows of 8 x 8 kv heads over 16384            111..116 (4.7 TB/s)
+//   61 / 244 rows of 8 x 8 kv heads over 16384      144 / 244..247
 #include <algorithm>
 #include <cmath>
 
@@ -201,9 +201,10 @@ struct TreeTile<uint16_t, DH> {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
   }
   __device__ static __forceinline__ float value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
-  // O^T += V^T P^T.  TWO: the fp32 weights enter as bf16 high and low parts; else rounded
-  // to bf16 once.
-  template <int RT, bool TWO, typename S>
+  // O^T += V^T P^T.  The fp32 weights enter as bf16 high and low parts, 16 significant bits,
+  // as in the prefill's attention (rounded to bf16 once, an output of 16384 slots is 2.3e-3 off
+  // the exact one instead of 1.7e-3, most of which is its own rounding).
+  template <int RT, typename S>
   __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const S& v, const float (*p)[KT * 4]) {
     bf16x8 hi[RT], lo[RT];
 #pragma unroll
@@ -213,10 +214,10 @@ struct TreeTile<uint16_t, DH> {
       for (int e = 0; e < 4; ++e) {
         const float a0 = p[r][2 * e], a1 = p[r][2 * e + 1];
         wh[e] = pack(a0, a1);
-        if constexpr (TWO) wl[e] = pack(a0 - __uint_as_float(wh[e] << 16), a1 - __uint_as_float(wh[e] & 0xFFFF0000u));
+        wl[e] = pack(a0 - __uint_as_float(wh[e] << 16), a1 - __uint_as_float(wh[e] & 0xFFFF0000u));
       }
       hi[r] = __builtin_bit_cast(bf16x8, wh);
-      if constexpr (TWO) lo[r] = __builtin_bit_cast(bf16x8, wl);
+      lo[r] = __builtin_bit_cast(bf16x8, wl);
     }
 #pragma unroll
     for (int n = 0; n < CPL; ++n) {
@@ -224,7 +225,7 @@ struct TreeTile<uint16_t, DH> {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[r], o[r][n], 0, 0, 0);
-        if constexpr (TWO) o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[r], o[r][n], 0, 0, 0);
+        o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[r], o[r][n], 0, 0, 0);
       }
     }
   }
@@ -299,7 +300,7 @@ struct TreeTile<float, DH> {
     return bad != 0;
   }
   __device__ static __forceinline__ float value(const float* p) { return *p; }
-  template <int RT, bool TWO, typename S>
+  template <int RT, typename S>
   __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const S& v, const float (*p)[4]) {
 #pragma unroll
     for (int n = 0; n < CPL; ++n)
@@ -358,8 +359,7 @@ __device__ __forceinline__ float rescaled(float x, float f) {
 }
 
 // RT row tiles of a wave: queries, and the running maximum, sum and output of their rows.
-// TWO: see TreeTile::values.
-template <typename AT, int DH, int RT, bool TWO>
+template <typename AT, int DH, int RT>
 struct RowTiles {
   using T = TreeTile<AT, DH>;
   static constexpr int KEYS = T::KEYS, NS = 4 * T::KT, CPL = T::CPL;  // NS: scores of a lane and row tile
@@ -475,7 +475,7 @@ struct RowTiles {
   template <bool tail, typename S>
   __device__ __forceinline__ void add(S& v, int t) {
     if constexpr (tail) drop(v, t);
-    T::template values<RT, TWO, S>(o, v, p);
+    T::template values<RT, S>(o, v, p);
   }
 
   // The outputs, after the tiles t0, t0 + by, .. < full without their nodes and tail tiles
@@ -568,7 +568,7 @@ __device__ __forceinline__ bool tree_work(const TreeArgs& a, TreeWork& w) {
 // in LDS.
 template <typename AT, int DH, int RT, bool FULL>
 __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_kernel(TreeArgs a) {
-  using Rows = RowTiles<AT, DH, RT, true>;
+  using Rows = RowTiles<AT, DH, RT>;
   using T = typename Rows::T;
   constexpr int KEYS = T::KEYS, CPL = T::CPL;
   constexpr int ROWS = 16 * RT, LD = DH + 4;
@@ -656,17 +656,18 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_ker
 
 // Many rows (bf16): NW waves of 32 (dh <= 128) or 16 rows each share the keys and values,
 // which come through LDS by DMA, two tiles ahead.  244 rows of 128 over 8 x 8 x 16384 keys:
-// 184 us, of which 110 the reads alone, the softmax (vector instructions, of which a lone
-// wave issues about one every 8 cycles) and the products adding to it; blocks of 4 waves
-// 187, of 2 281; half of the waves half a tile behind the others 209; each row group reading
-// for itself, as with few rows, 325.  A tile is 32 rows of DH channels for
+// 247 us, of which 110 the reads alone, the softmax (vector instructions) and the products
+// adding to it.  With the weights rounded to bf16 once, a third fewer products and less than
+// the other paths keep, it takes 190, and there blocks of 4 waves 187, of 2 281; half of the
+// waves half a tile behind the others 209; each row group reading for itself, as with few
+// rows, 325.  A tile is 32 rows of DH channels for
 // keys and as many for values; 16-byte piece c of key j lies at piece c ^ (j % 16 or less),
 // so that both the reads of one piece of 16 keys and those of all pieces of a key spread
 // over the banks.
 template <int DH, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
   constexpr int RT = DH == 256 ? 1 : 2;
-  using Rows = RowTiles<uint16_t, DH, RT, false>;
+  using Rows = RowTiles<uint16_t, DH, RT>;
   using T = typename Rows::T;
   constexpr int CPL = T::CPL, ROWS = 16 * RT * NW;
   constexpr int PIECES = DH / 8, SWZ = PIECES < 16 ? PIECES - 1 : 15;  // 16-byte pieces of a row
@@ -918,7 +919,8 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
 // The weight of every slot, of more rows than keep their scores: a wave per NT tiles of keys
 // of one kv head, which stay in registers, all live rows of the head group in tiles of 16;
 // exp2(s - max) / sum from the rows' final statistics.  Two tiles share each reading of the
-// queries (244 rows over 8 x 8 x 16384 keys, whole call: 438 -> 355 us), where that
+// queries (244 rows over 8 x 8 x 16384 keys, whole call with the attention at 190 us: 438 ->
+// 355, and 407 with the attention at 247), where that
 // leaves enough blocks (70 rows over 2 x 8 x 500 keys, whole call: one tile 29.5, two 33.4)
 // and registers (width 256 has none).
 template <typename AT, int DH, bool FULL, int NT>

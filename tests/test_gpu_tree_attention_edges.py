@@ -1,5 +1,5 @@
 """spider_tree_attention at its edges, against the float64 oracle: splits of the keys that a
-ceiling leaves without a tile, hidden infinities and NaN in many tiles, infinite values that count.
+ceiling leaves without a tile, hidden infinities and NaN in many tiles, infinite values that count, many rows.
 
 Bars as in test_gpu_tree_attention.py.
 """
@@ -115,3 +115,16 @@ def test_infinite_values_under_weights_that_vanish(n, dtype, T, dh):
     clean[:, :, 0, 3] = float("inf")
     clean[:, :, 1, 2] = -float("inf")
     assert same(got, clean)
+
+
+@pytest.mark.parametrize("T,H,dh,n", [(33, 2, 128, 700), (61, 8, 128, 4100), (150, 2, 64, 1000), (256, 2, 128, 64),
+                                      (40, 4, 72, 500), (17, 2, 256, 900), (60, 2, 200, 300)])
+def test_many_rows_are_as_exact_as_few(T, H, dh, n):
+    """The weights enter the products with 16 significant bits whatever the number of rows: the bar of few rows,
+    2^-8 |out| (the output's own rounding) + 1e-4 of the largest."""
+    lib = need_gpu()
+    q, k, v = make(1, T, H, 2, dh, n + T, "bf16", T + n, spread=1.5)
+    parents = trees(1, T, np.random.default_rng(T))
+    mask, sees = lib.tree_mask(parents)[0], od.tree_mask(parents)[0]
+    out = lib.tree_attention(q, k, v, torch.tensor([n], dtype=torch.int32).cuda(), tree_mask=torch.from_numpy(mask).cuda())
+    check(out, od.tree_attention(np64(q), np64(k), np64(v), [n], sees)[0], "bf16")
