@@ -645,8 +645,8 @@ spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spider_dtype d
  * mask_stride words (0: one row for all) or NULL.  All on the device.  Ids
  * outside [0, V) anywhere are ignored.  Rows of nodes that are not alive are left
  * as they were in out and next_out.
- * Limits: T <= 256, B*T <= 65535, V <= 2^28, n_bias <= 32768.  Workspace:
- * spider_adjust_logits_workspace_size(B, T, V) bytes (0 for V <= 32768),
+ * Limits: T <= 256, B*T <= 65535, V <= 2^28, n_bias <= 32768, history_stride <=
+ * 2^31 - 2^14.  Workspace: spider_adjust_logits_workspace_size(B, T, V) bytes (0 for V <= 32768),
  * 256-byte aligned; none without next_out.
  * ------------------------------------------------------------------------ */
 size_t spider_adjust_logits_workspace_size(int B, int T, int V);

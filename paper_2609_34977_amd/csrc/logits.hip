@@ -11,6 +11,9 @@ namespace spider {
 namespace {
 
 constexpr uint32_t kSeen = 0x80000000u;  // count word: the token stands in the prompt
+// A row's history: the kernel's index runs up to 8 * 1024 past its end, and the counts of it
+// and of 256 nodes stay below kSeen.
+constexpr int64_t kMaxHistory = (1ll << 31) - (1 << 14);
 
 struct AdjustArgs {
   const void* logits;
@@ -278,8 +281,9 @@ extern "C" spider_status spider_adjust_logits(
                  "spider_adjust_logits: sizes must be positive");
   SPIDER_REQUIRE(adjust_shape_ok(B, T, V) && n_bias <= kMaxBias, SPIDER_ERR_UNSUPPORTED,
                  "spider_adjust_logits: T <= 256, B * T <= 65535, V <= 2^28, n_bias <= 32768");
-  SPIDER_REQUIRE(!history || (n_history && history_stride >= 0 && history_stride <= 0x7fffffff),
-                 SPIDER_ERR_INVALID_ARG, "spider_adjust_logits: a history needs n_history and a stride below 2^31");
+  SPIDER_REQUIRE(!history || (n_history && history_stride >= 0 && history_stride <= kMaxHistory),
+                 SPIDER_ERR_INVALID_ARG,
+                 "spider_adjust_logits: a history needs n_history and a stride of at most 2^31 - 2^14");
   SPIDER_REQUIRE(n_bias == 0 || (bias_ids && bias), SPIDER_ERR_INVALID_ARG,
                  "spider_adjust_logits: n_bias without bias_ids and bias");
   SPIDER_REQUIRE(logits_stride >= V && (!out || out_stride >= V), SPIDER_ERR_SHAPE,

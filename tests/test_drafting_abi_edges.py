@@ -1,0 +1,25 @@
+"""Refusals of the operators for drafting over the cache at the ends of their ranges, before
+any HIP call."""
+import os
+
+import pytest
+
+lib_mod = pytest.importorskip("paper_2609_34977_amd._lib")
+OK, INVALID, SHAPE, UNSUPPORTED, WORKSPACE, HIP = 0, 1, 2, 3, 4, 5
+P = 0x100000
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(lib_mod._LIB_PATH):
+        pytest.skip("libspider.so not built")
+    return lib_mod.lib()
+
+
+@pytest.mark.parametrize("stride", [(1 << 31) - 1, (1 << 31) - (1 << 14) + 1])
+def test_adjust_logits_refuses_histories_whose_index_passes_31_bits(L, stride):
+    """The index of a history entry runs 8192 past the last one and a count must stay below its flag bit."""
+    a = dict(B=2, T=2, V=100, x=P, xs=100, dt=0, h=P, hs=stride, nh=P, np=None, nn=None, tok=None, tree=None, rep=None,
+             freq=None, pres=None, bi=None, bv=None, nb=0, m=None, ms=0, out=2 * P, os=100, nxt=P, ws=P, wsb=1 << 20)
+    assert L.spider_adjust_logits(*a.values(), None) == INVALID
+    assert b"history" in L.spider_last_error()
