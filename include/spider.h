@@ -582,8 +582,8 @@ spider_status spider_decode_tree(const spider_decoder_cfg* cfg, const spider_lay
  *   counts as -inf).
  * weights device fp32 [L][B][Hkv][cap]; idx_out device int32
  * [L][B][shared ? 1 : Hkv][keep]: the kept slots ascending, then -1; len_out
- * device int32 [B] = min(n, keep).  Requires n_first + n_last <= keep <= cap and
- * fewer than 2^22 rows (L * B * groups), cap <= 2^30.  Workspace:
+ * device int32 [B] = min(n, keep), not over lens.  Requires n_first + n_last <=
+ * keep <= cap and fewer than 2^22 rows (L * B * groups), cap <= 2^30.  Workspace:
  * spider_cache_select_workspace_size(...) bytes (0 for short or many rows),
  * 256-byte aligned.
  * ------------------------------------------------------------------------ */

@@ -495,6 +495,9 @@ extern "C" spider_status spider_cache_select(int L, int B, int Hkv, int cap, con
                  "spider_cache_select: workspace of %zu bytes needed, %zu given", need, workspace ? workspace_bytes : 0);
   SPIDER_REQUIRE(need == 0 || reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG,
                  "spider_cache_select: workspace must be 256-byte aligned");
+  // (every row reads lens while one of them writes len_out)
+  SPIDER_REQUIRE(len_out + B <= lens || lens + B <= len_out, SPIDER_ERR_INVALID_ARG,
+                 "spider_cache_select: len_out must not overlap lens");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_CACHE_SELECT, st);
   const SelectArgs a{weights, lens, idx_out, len_out, L, B, Hkv, G, cap, keep, n_first, n_last};

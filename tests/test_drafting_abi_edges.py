@@ -23,3 +23,11 @@ def test_adjust_logits_refuses_histories_whose_index_passes_31_bits(L, stride):
              freq=None, pres=None, bi=None, bv=None, nb=0, m=None, ms=0, out=2 * P, os=100, nxt=P, ws=P, wsb=1 << 20)
     assert L.spider_adjust_logits(*a.values(), None) == INVALID
     assert b"history" in L.spider_last_error()
+
+
+@pytest.mark.parametrize("new", [P, P + 4, P - 12])
+def test_cache_select_refuses_new_lengths_over_the_old_ones(L, new):
+    """Rows of a sample read its length while another one writes the new length."""
+    a = dict(L=2, B=4, Hkv=2, cap=100, w=2 * P, lens=P, keep=10, first=2, last=3, shared=0, idx=3 * P, new=new, ws=P, wsb=1 << 30)
+    assert L.spider_cache_select(*a.values(), None) == INVALID
+    assert b"overlap" in L.spider_last_error()
