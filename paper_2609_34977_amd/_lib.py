@@ -695,7 +695,7 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
     ms = 0
     if mask is not None and mask.dim() > 1:
         ms = words
-        mask = mask.unsqueeze(1) if flat and mask.dim() == 2 else mask
+        mask = mask.unsqueeze(1) if T == 1 and mask.dim() == 2 else mask
     L = lib()
     wsz = _size("spider_adjust_logits_workspace_size", B, T, V)
     workspace, wptr = _scratch(workspace, wsz, dev)

@@ -1,5 +1,5 @@
 """spider_adjust_logits: bias lists that name some tokens several times, compared bit for bit
-with the entries added one after the other in fp32."""
+with the entries added one after the other in fp32; the shapes that the binding takes."""
 import numpy as np
 import pytest
 import torch
@@ -30,3 +30,20 @@ def test_bias_entries_of_a_token_add_up_in_order(V, nb):
     out, nxt = lib.adjust_logits(torch.from_numpy(x).cuda(), bias_ids=torch.from_numpy(ids).cuda(), bias=torch.from_numpy(bias).cuda())
     assert np.array_equal(out.cpu().numpy(), want)
     assert np.array_equal(nxt.cpu().numpy(), want.argmax(1))
+
+
+def test_a_mask_row_per_sample_for_one_node():
+    """[B, W32] masks for T = 1, with logits [B, V] and [B, 1, V]."""
+    lib = need_gpu()
+    rng = np.random.default_rng(1)
+    x = torch.from_numpy(rng.normal(0, 1, (3, 100)).astype(np.float32)).cuda()
+    bits = torch.from_numpy(rng.integers(-2**31, 2**31, (3, 4)).astype(np.int32)).cuda()
+    want, ids = lib.adjust_logits(x, mask=bits)
+    got, ids1 = lib.adjust_logits(x.unsqueeze(1), mask=bits)
+    full, ids2 = lib.adjust_logits(x.unsqueeze(1), mask=bits.unsqueeze(1))
+    allowed = (bits.cpu().numpy()[:, np.arange(100) // 32] >> (np.arange(100) % 32)) & 1 == 1
+    assert np.array_equal(want.cpu().numpy(), np.where(allowed, x.cpu().numpy(), -np.inf))
+    assert torch.equal(got[:, 0], want) and torch.equal(full, got)
+    assert torch.equal(ids1[:, 0], ids) and torch.equal(ids2, ids1)
+    with pytest.raises(ValueError):
+        lib.adjust_logits(torch.zeros(3, 2, 100).cuda(), mask=bits)
