@@ -526,6 +526,7 @@ spider_status spider_tree_mask(int B, int T, const int32_t* parents, uint64_t* m
  * Precision: products exact, sums, maxima and exponentials fp32, out rounded
  * once.  bf16: the softmax numerators enter the product with v as bf16 high and
  * low parts (16 significant bits).
+ * The stride of a dimension of size 1 is not looked at.
  * Requires H % Hkv == 0, T <= 256, dh <= 256, B and H <= 65535, B*H*T and
  * B*Hkv*ceil(cap/64) below 2^24, dh and the strides multiples of 16 bytes, q, k,
  * v, out 16-byte aligned; out overlaps no input.  Workspace:
@@ -605,10 +606,11 @@ spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* w
  * (n_max each; taken into [0, n_max]); base device int32 [B] or NULL (0).  So
  * eviction takes spider_cache_select's idx and len, and the accepted nodes of
  * a tree move behind their context with base = lens, idx = their node numbers.
- * Strides: HOST [4], elements of (layer, sample, slot, head); channels
- * contiguous.  In place (k_out == k_in, v_out == v_in, the weights alike, equal
- * strides and capacities) idx must ascend strictly within a row (so idx[i] >=
- * i); a row that does not ends with unspecified contents in its own slots.
+ * Strides: HOST [4], elements of (layer, sample, slot, head), not looked at where
+ * there is one of these; channels contiguous.  In place (k_out == k_in, v_out ==
+ * v_in, the weights alike, equal strides and capacities) idx must ascend strictly
+ * within a row (so idx[i] >= i); a row that does not ends with unspecified contents
+ * in its own slots.
  * Otherwise input and output must not overlap.  Slots that nothing is moved
  * to are left as they were.
  * Requires dh <= 256, dh and the strides multiples of 16 bytes, caches 16-byte

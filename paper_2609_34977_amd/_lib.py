@@ -503,6 +503,12 @@ def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev):
     return workspace, workspace.data_ptr()
 
 
+def _alike(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether a and b have the same shape and strides, but for those of dimensions of size 1."""
+    return a.shape == b.shape and (a.stride() == b.stride() or all(
+        n == 1 or s == t for n, s, t in zip(a.shape, a.stride(), b.stride())))
+
+
 def _gpu(t: torch.Tensor):
     if not t.is_cuda:
         raise ValueError("the tensors must be on a GPU")
@@ -538,7 +544,7 @@ def tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: torc
     B, T, H, dh = q.shape
     cap, Hkv = k.shape[1], k.shape[2]
     dev = _gpu(q)
-    if k.shape[0] != B or k.shape[3] != dh or v.shape != k.shape or v.stride() != k.stride():
+    if k.shape[0] != B or k.shape[3] != dh or not _alike(k, v):
         raise ValueError("k and v must be [B, cap, Hkv, dh] alike, with the B and dh of q")
     if k.dtype != q.dtype or v.dtype != q.dtype or k.device != dev or v.device != dev:
         raise ValueError("q, k and v must share dtype and device")
@@ -635,7 +641,7 @@ def cache_compact(k: torch.Tensor, v: torch.Tensor, idx: torch.Tensor, count: Op
     dev = _gpu(k)
     if k_out.shape != (L_, B, cap_out, Hkv, dh) or v.shape != k.shape or v_out.shape != k_out.shape:
         raise ValueError("the caches must be [L, B, cap, Hkv, dh] alike but for cap")
-    if v.stride() != k.stride() or v_out.stride() != k_out.stride() or k.stride(4) != 1 or k_out.stride(4) != 1:
+    if not _alike(k, v) or not _alike(k_out, v_out) or k.stride(4) != 1 or k_out.stride(4) != 1:
         raise ValueError("keys and values must share their strides, with contiguous channels")
     if any(t.dtype != k.dtype or t.device != dev for t in (v, k_out, v_out)):
         raise ValueError("the caches must share dtype and device")

@@ -548,11 +548,14 @@ extern "C" spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spi
                          reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out);
   SPIDER_REQUIRE(bits % 16 == 0, SPIDER_ERR_INVALID_ARG, "spider_cache_compact: the caches must be 16-byte aligned");
   bool same = cap_in == cap_out;
+  const int n_in[4] = {L, B, cap_in, Hkv}, n_out[4] = {L, B, cap_out, Hkv};
+  int64_t in[4], out[4];  // bytes; the stride of a dimension of size 1 means nothing
   for (int i = 0; i < 4; ++i) {
-    SPIDER_REQUIRE(in_strides[i] >= 0 && out_strides[i] >= 0 && in_strides[i] * es % 16 == 0 &&
-                       out_strides[i] * es % 16 == 0,
-                   SPIDER_ERR_INVALID_ARG, "spider_cache_compact: strides must be multiples of 16 bytes");
-    same = same && in_strides[i] == out_strides[i];
+    in[i] = n_in[i] == 1 ? 0 : in_strides[i] * es;
+    out[i] = n_out[i] == 1 ? 0 : out_strides[i] * es;
+    SPIDER_REQUIRE(in[i] >= 0 && out[i] >= 0 && in[i] % 16 == 0 && out[i] % 16 == 0, SPIDER_ERR_INVALID_ARG,
+                   "spider_cache_compact: strides must be multiples of 16 bytes");
+    same = same && in[i] == out[i];
   }
   const bool inplace = k_in == k_out;
   SPIDER_REQUIRE(inplace == (v_in == v_out) && (!weights_in || inplace == (weights_in == weights_out)),
@@ -572,8 +575,8 @@ extern "C" spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spi
   a.idx = idx;
   a.count = count;
   a.base = base;
-  a.il = in_strides[0] * es, a.ib = in_strides[1] * es, a.is = in_strides[2] * es, a.ih = in_strides[3] * es;
-  a.ol = out_strides[0] * es, a.ob = out_strides[1] * es, a.os = out_strides[2] * es, a.oh = out_strides[3] * es;
+  a.il = in[0], a.ib = in[1], a.is = in[2], a.ih = in[3];
+  a.ol = out[0], a.ob = out[1], a.os = out[2], a.oh = out[3];
   a.L = L, a.B = B, a.Hkv = Hkv, a.nv = dh * es / 16;
   a.cap_in = cap_in, a.cap_out = cap_out, a.n_max = n_max, a.idx_layers = idx_layers, a.idx_heads = idx_heads;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);

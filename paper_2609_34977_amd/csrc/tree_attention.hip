@@ -1141,6 +1141,11 @@ extern "C" spider_status spider_tree_attention(int B, int T, int H, int Hkv, int
   // blocks of the largest launch (a grid holds 2^24 blocks of 256 threads)
   SPIDER_REQUIRE((int64_t)B * H * T < (1 << 24) && (int64_t)B * Hkv * ceil_div(cap, 64) < (1 << 24),
                  SPIDER_ERR_UNSUPPORTED, "spider_tree_attention: B * H * T or B * Hkv * cap / 64 reach 2^24");
+  // the stride of a dimension of size 1 means nothing
+  if (B == 1) q_stride_b = kv_stride_b = 0;
+  if (T == 1) q_stride_t = 0;
+  if (cap == 1) kv_stride_s = 0;
+  if (Hkv == 1) kv_stride_h = 0;
   const int64_t per16 = dtype == SPIDER_BF16 ? 8 : 4;
   SPIDER_REQUIRE(dh % per16 == 0, SPIDER_ERR_UNSUPPORTED, "spider_tree_attention: dh must be a multiple of 16 bytes");
   SPIDER_REQUIRE(q_stride_b % per16 == 0 && q_stride_t % per16 == 0 && kv_stride_b % per16 == 0 &&
