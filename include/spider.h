@@ -607,7 +607,8 @@ spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* w
  * eviction takes spider_cache_select's idx and len, and the accepted nodes of
  * a tree move behind their context with base = lens, idx = their node numbers.
  * Strides: HOST [4], elements of (layer, sample, slot, head), not looked at where
- * there is one of these; channels contiguous.  In place (k_out == k_in, v_out ==
+ * there is one of these, else positive on the output side (its slots share no
+ * memory); channels contiguous.  In place (k_out == k_in, v_out ==
  * v_in, the weights alike, equal strides and capacities) idx must ascend strictly
  * within a row (so idx[i] >= i); a row that does not ends with unspecified contents
  * in its own slots.

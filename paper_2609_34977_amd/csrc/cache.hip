@@ -555,6 +555,8 @@ extern "C" spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spi
     out[i] = n_out[i] == 1 ? 0 : out_strides[i] * es;
     SPIDER_REQUIRE(in[i] >= 0 && out[i] >= 0 && in[i] % 16 == 0 && out[i] % 16 == 0, SPIDER_ERR_INVALID_ARG,
                    "spider_cache_compact: strides must be multiples of 16 bytes");
+    SPIDER_REQUIRE(n_out[i] == 1 || out[i] > 0, SPIDER_ERR_INVALID_ARG,
+                   "spider_cache_compact: the output's slots must not share memory (a stride of 0)");
     same = same && in[i] == out[i];
   }
   const bool inplace = k_in == k_out;

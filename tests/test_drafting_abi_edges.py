@@ -1,5 +1,6 @@
 """Refusals of the operators for drafting over the cache at the ends of their ranges, before
 any HIP call."""
+import ctypes
 import os
 
 import pytest
@@ -31,3 +32,16 @@ def test_cache_select_refuses_new_lengths_over_the_old_ones(L, new):
     a = dict(L=2, B=4, Hkv=2, cap=100, w=2 * P, lens=P, keep=10, first=2, last=3, shared=0, idx=3 * P, new=new, ws=P, wsb=1 << 30)
     assert L.spider_cache_select(*a.values(), None) == INVALID
     assert b"overlap" in L.spider_last_error()
+
+
+@pytest.mark.parametrize("dim", range(4))
+@pytest.mark.parametrize("inplace", [False, True])
+def test_cache_compact_refuses_outputs_that_share_memory(L, inplace, dim):
+    """A broadcast cache: rows of other layers, samples or heads would be moved over each other."""
+    strides = [6400, 3200, 32, 16]
+    strides[dim] = 0
+    s = (ctypes.c_int64 * 4)(*strides)
+    a = dict(L=2, B=2, Hkv=2, dh=16, dt=1, k=P, v=2 * P, si=s, cap=100, ko=P if inplace else 3 * P,
+             vo=2 * P if inplace else 4 * P, so=s, cap_out=100, idx=P, il=1, ih=1, n=5, count=None, base=None, wi=None, wo=None)
+    assert L.spider_cache_compact(*a.values(), None) == INVALID
+    assert b"share" in L.spider_last_error()
