@@ -580,25 +580,26 @@ def decode_tree(cfg: DecoderCfg, weights, lens, x: torch.Tensor, kv: dict, paren
     B, T, d = x.shape
     dev = _gpu(x)
     cap = kv["desc"].cap
-    if tuple(kv["k"].shape) != (cfg.L, B, cap, d):
-        raise ValueError(f"the cache must be [{cfg.L}, {B}, cap, {d}]")
+    for name in ("k", "v"):
+        _need(kv[name], f"kv[{name!r}]", x.dtype, (cfg.L, B, cap, d), dev)
     ln = np.ascontiguousarray(lens, dtype=np.int32)
     ps = None if pos is None else np.ascontiguousarray(pos, dtype=np.int32)
     pr = None if parents is None else np.ascontiguousarray(parents, dtype=np.int32)
     if ln.shape != (B,) or (ps is not None and ps.shape != (B,)) or (pr is not None and pr.shape != (B, T)):
         raise ValueError("lens and pos must be [B], parents [B, T]")
     V = int(w_unembed.shape[0]) if w_unembed is not None else 0
+    norm, head = _need(final_norm, "final_norm", torch.float32, (d,), dev), _need(w_unembed, "w_unembed", x.dtype, (V, d), dev)
     h = torch.empty(B, T, d, dtype=torch.float32, device=dev)
     logits = torch.empty(B, T, V, dtype=torch.float32, device=dev) if V else None
     nxt = torch.empty(B, T, dtype=torch.int32, device=dev) if V else None
     L = lib()
     wsz = L.spider_decode_tree_workspace_size(ctypes.byref(cfg), B, T, cap, V)
-    if workspace is None or workspace.numel() < wsz + 256:
+    if workspace is None or workspace.device != dev or workspace.numel() * workspace.element_size() < wsz + 256:
         workspace = _ws(wsz, dev)
     wt = weight_table if weight_table is not None else layer_weights(weights)
     _on(dev, L.spider_decode_tree, ctypes.byref(cfg), wt, B, T, ln.ctypes.data,
         None if ps is None else ps.ctypes.data, None if pr is None else pr.ctypes.data, x.data_ptr(),
-        ctypes.byref(kv["desc"]), _ptr(final_norm), _ptr(w_unembed), V, h.data_ptr(), _ptr(logits), _ptr(nxt),
+        ctypes.byref(kv["desc"]), norm, head, V, h.data_ptr(), _ptr(logits), _ptr(nxt),
         _need(attn_weights, "attn_weights", torch.float32, (cfg.L, B, cfg.H, cap), dev), _aligned(workspace), wsz)
     return h, logits, nxt
 
