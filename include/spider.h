@@ -559,6 +559,7 @@ spider_status spider_tree_attention(int B, int T, int H, int Hkv, int dh, const 
  * hold unspecified values, and their slots are not written.  weights: device
  * fp32 [L][B][H][cap] or NULL: the attention weight of every slot is added up
  * in each layer, spider_tree_attention's weights_in = weights_out.
+ * Not for streams under HIP graph capture (the host values are those of one step).
  * Limits: T <= 256, B*T <= 65535, dh a multiple of 16 bytes, at most 256 (bf16:
  * 128).  Workspace: spider_decode_tree_workspace_size(cfg, B, T, kv->cap, V)
  * bytes (V = 0 without the head).

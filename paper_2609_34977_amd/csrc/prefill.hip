@@ -2238,6 +2238,12 @@ extern "C" spider_status spider_decode_tree(const spider_decoder_cfg* cfg, const
                  "spider_decode_tree: workspace must be 256-byte aligned");
   const TreeStepWs ws = tree_step_layout(*cfg, B, T, kv->cap, Vh, reinterpret_cast<char*>(workspace));
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  // The tables go through a staging buffer that later calls fill anew, or free for a larger
+  // one: a replayed copy would read what it holds by then.
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  SPIDER_HIP(hipStreamIsCapturing(st, &capture));
+  SPIDER_REQUIRE(capture == hipStreamCaptureStatusNone, SPIDER_ERR_UNSUPPORTED,
+                 "spider_decode_tree: cannot be captured into a graph (lens, pos and parents are host values of one step)");
   if (cfg->dtype == SPIDER_BF16)
     return run_decode_tree<uint16_t>(*cfg, layers, B, T, tab, x, *kv, final_norm, w_unembed, Vh, h_out, logits_out,
                                      next_out, weights, ws, st);

@@ -1,4 +1,4 @@
-"""spider_decode_tree: what the binding refuses before the library reads it."""
+"""spider_decode_tree: what is refused before anything runs."""
 import pytest
 import torch
 
@@ -24,3 +24,25 @@ def test_heads_norms_and_caches_of_another_kind_are_refused(wl):
         with pytest.raises(ValueError):
             L.decode_tree(cfg, W, [5, 0], x, **{**dict(kv=kv, final_norm=fn, w_unembed=wu), **kw})
     assert torch.equal(kv["k"], before)
+
+
+def test_capture_is_refused():
+    """Its tables come from a host buffer that the next call fills anew: a replay would read that call's."""
+    L, dec, _, cfg, W, kv = setup("tiny", 1, 1, 20)
+    x = rows(dec, (1, 3), 2).cuda()
+    want, _, _ = L.decode_tree(cfg, W, [5], x, kv)
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    table = L.layer_weights(W)
+    y = torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y.add_(1)
+        with pytest.raises(L.SpiderError) as e:
+            L.decode_tree(cfg, W, [5], x, kv, weight_table=table, workspace=ws)
+    assert "captur" in str(e.value)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert (y == 2).all()
+    again, _, _ = L.decode_tree(cfg, W, [5], x, kv)
+    assert torch.equal(again, want)
