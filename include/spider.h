@@ -558,7 +558,9 @@ spider_status spider_tree_attention(int B, int T, int H, int Hkv, int dh, const 
  * [B*T] as for spider_decode_step, row b*T + t for node t; rows of absent nodes
  * hold unspecified values, and their slots are not written.  weights: device
  * fp32 [L][B][H][cap] or NULL: the attention weight of every slot is added up
- * in each layer, spider_tree_attention's weights_in = weights_out.
+ * in each layer, spider_tree_attention's weights_in = weights_out, so over every
+ * present node, also those that are not accepted later.  (A prefill adds nothing:
+ * of slots that no node attended to, spider_cache_select keeps the lower ones.)
  * Not for streams under HIP graph capture (the host values are those of one step).
  * Limits: T <= 256, B*T <= 65535, dh a multiple of 16 bytes, at most 256 (bf16:
  * 128).  Workspace: spider_decode_tree_workspace_size(cfg, B, T, kv->cap, V)
