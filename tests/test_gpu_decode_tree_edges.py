@@ -1,8 +1,13 @@
-"""spider_decode_tree: what is refused before anything runs."""
+"""spider_decode_tree: many rows against the oracle, and what is refused before anything runs."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import decode as odec
+from oracle import drafting as od
+from synth.decoder_inputs import layer_weights
 from synth.online_inputs import unembed
+from gpu_common import log, rel_err
 from test_gpu_decode_tree import rows, setup
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +51,37 @@ def test_capture_is_refused():
     assert (y == 2).all()
     again, _, _ = L.decode_tree(cfg, W, [5], x, kv)
     assert torch.equal(again, want)
+
+
+@pytest.mark.parametrize("wl,B,T,lens,evicted", [
+    ("llava15_7b", 1, 17, [40], 0), ("llava15_7b", 1, 64, [100], 30), ("llava15_7b", 4, 64, [20, 0, 64, 33], 5),
+    ("llava15_7b", 2, 130, [70, 3], 0), ("llava15_7b", 8, 61, [5 * b for b in range(8)], 100), ("tiny", 3, 100, [50, 0, 29], 7),
+    ("tiny", 2, 256, [9, 64], 0)])
+def test_many_rows_match_the_oracle(wl, B, T, lens, evicted):
+    """Rows past 4, 16, 64 and 256, where the products take other kernels, trees of two to four mask words, and
+    positions ahead of the slots; bars as in test_gpu_decode_tree.py."""
+    cap, V = max(lens) + T + 6, 512
+    L, dec, bf16, cfg, W, kv = setup(wl, 1, B, cap)
+    rng = np.random.default_rng(T)
+    parents = np.stack([[rng.integers(max(-1, t - 9), t) for t in range(T)] for _ in range(B)])
+    parents[-1, T - 3:] = -2
+    for i, c in enumerate((kv["k"], kv["v"])):
+        c.copy_(torch.randn(c.shape, generator=torch.Generator().manual_seed(7 + i)))
+    k0, v0 = (c.double().cpu().numpy() for c in (kv["k"], kv["v"]))
+    x = rows(dec, (B, T), 3)
+    wu, fn = unembed(dec, V, seed=3), torch.rand(dec.d, generator=torch.Generator().manual_seed(5)) + 0.5
+    aw = torch.rand(1, B, dec.H, cap).cuda()
+    aw0 = aw.double().cpu().numpy()
+    pos = [n + evicted for n in lens]
+    h, logits, _ = L.decode_tree(cfg, W, lens, x.cuda(), kv, parents=parents, pos=pos, final_norm=fn.cuda(), w_unembed=wu.cuda(),
+                                 attn_weights=aw)
+    wts = lambda l: {k: v.double().numpy() for k, v in layer_weights(dec, l, 0, "cpu").items()}  # noqa: E731
+    recipe = "bf16" if bf16 else "f32"
+    ho = od.decode_tree(x.double().numpy(), wts, k0, v0, lens, pos, parents, dec, recipe, aw0)
+    lo = odec.lm_head(ho.reshape(B * T, -1), fn.numpy(), wu.double().numpy(), dec.eps, recipe).reshape(B, T, V)
+    live = parents > -2
+    tol, tol_kv = (2e-2, 1e-2) if bf16 else (1e-4, 1e-5)
+    errs = [rel_err(h.cpu().numpy()[live], ho[live]), rel_err(logits.cpu().numpy()[live], lo[live]),
+            rel_err(kv["k"].double().cpu().numpy(), k0), rel_err(kv["v"].double().cpu().numpy(), v0), rel_err(aw.double().cpu().numpy(), aw0)]
+    log(f"[tree] {wl} {B}x{T}: h, logits, k, v, weights {errs}")
+    assert max(errs[0], errs[1], errs[4]) <= tol and max(errs[2], errs[3]) <= tol_kv
