@@ -493,12 +493,14 @@ def _size(name: str, *args) -> int:
 
 def _scratch(workspace: Optional[torch.Tensor], nbytes: int, dev):
     """(tensor to keep until the call, 256-byte aligned pointer) of nbytes of workspace."""
-    if workspace is not None:
-        if workspace.device != dev or workspace.numel() * workspace.element_size() < nbytes + 256:
-            raise ValueError(f"workspace must hold {nbytes + 256} bytes on {dev}")
-        return workspace, (workspace.data_ptr() + 255) // 256 * 256
     if nbytes == 0:
         return None, None
+    if workspace is not None:
+        at = (workspace.data_ptr() + 255) // 256 * 256
+        end = workspace.data_ptr() + workspace.numel() * workspace.element_size()
+        if workspace.device != dev or not workspace.is_contiguous() or end - at < nbytes:
+            raise ValueError(f"workspace must be contiguous, on {dev}, and hold {nbytes} bytes from a multiple of 256 bytes on")
+        return workspace, at
     workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     return workspace, workspace.data_ptr()
 
@@ -697,6 +699,8 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
     n = history.shape[1] if history is not None else 0
     if (bias_ids is None) != (bias is None):
         raise ValueError("bias_ids and bias go together")
+    if bias_ids is not None and bias_ids.dim() != 2:
+        raise ValueError("bias_ids and bias must be [B, n_bias]")
     nb = bias_ids.shape[1] if bias_ids is not None else 0
     words = (V + 31) // 32
     ms = 0

@@ -47,3 +47,20 @@ def test_a_mask_row_per_sample_for_one_node():
     assert torch.equal(ids1[:, 0], ids) and torch.equal(ids2, ids1)
     with pytest.raises(ValueError):
         lib.adjust_logits(torch.zeros(3, 2, 100).cuda(), mask=bits)
+
+
+def test_a_workspace_of_the_size_that_the_library_names():
+    lib = need_gpu()
+    for V in (100, 40000):
+        x = torch.randn(3, V, device="cuda")
+        n = lib.lib().spider_adjust_logits_workspace_size(3, 1, V)
+        want, ids = lib.adjust_logits(x)
+        for ws in (torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(n + 300, dtype=torch.uint8, device="cuda")[44:]):
+            got, ids2 = lib.adjust_logits(x, workspace=ws)
+            assert torch.equal(got, want) and torch.equal(ids2, ids)
+    for ws in (torch.empty(n - 1, dtype=torch.uint8, device="cuda"), torch.empty(n + 40, dtype=torch.uint8, device="cuda")[1:],
+               torch.empty(n, dtype=torch.uint8), torch.empty(2 * n + 512, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            lib.adjust_logits(x, workspace=ws)
+    with pytest.raises(ValueError):
+        lib.adjust_logits(x, bias_ids=torch.zeros(4, dtype=torch.int32, device="cuda"), bias=torch.zeros(4, device="cuda"))
