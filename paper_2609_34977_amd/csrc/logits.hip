@@ -251,10 +251,13 @@ __global__ void __launch_bounds__(64) adjust_join_kernel(AdjustArgs a) {
 }
 
 // Pieces of a row: all of it where its counts fit the LDS of a CU (a block per CU, but one
-// launch and one reading of the history), else 8192 tokens, four blocks per CU; and rows of
-// up to 8192 in such blocks too.  Measured, pieces of 8192 / 32768, us: 1 row of 32000 14.7
-// / 11.8; 248 rows of 32000 21.7 / 18.9; 64 rows of 151000 with 12000 tokens of history
-// 26.7 / 35.0 (16384: 33.2, in 1024 threads 28.3).
+// launch, one reading of the history and no workspace), else 8192 tokens, four blocks per
+// CU; and rows of up to 8192 in such blocks too.  Measured, pieces of 8192 / 32768, us.
+// Whole calls: 1 row of 32000 14.7 / 11.8 (the host's second launch); 64 rows of 151000 with
+// 12000 tokens of history 26.7 / 35.0 (16384: 33.2, in 1024 threads 28.3).  On the device,
+// histories of 2900: 1 row of 32000 9.3 / 12.3, 64 rows 11.6 / 15.2, 248 21.6 / 19.6, 300
+// 25.7 / 32.0, 1024 64 / 74; 248 rows of 12000 14.8 / 11.4: past the 256 CUs pieces would be
+// faster, at the price of a workspace.
 constexpr int kPiece = 8192, kRow = 32768, kMaxBias = 64 * 512;
 int adjust_piece(int V) { return V > kPiece && V <= kRow ? kRow : kPiece; }
 

@@ -1018,6 +1018,12 @@ TreePlan tree_plan(int B, int T, int H, int Hkv, int dh, int cap, spider_dtype d
     target = p.dhp == 256 ? 256 : 256 * 8 / p.nw;
   }
   p.groups = ceil_div(R, rows);
+  // At least eight tiles per split.  Measured with 4 / 8 / 16, us on the device: 16 rows of
+  // 32 heads over 705 slots with weights 13.6 / 15.1 / 17.8; 32 rows of 8 heads over 2000
+  // 10.6 / 12.9 / 15.3; 4 x 1 row of 32 heads over 705 16.4 / 16.1 / 14.2; 244 rows of 8
+  // heads over 2000 29.1 / 29.4 / 37.9; fp32, 2 x 13 rows of 8 heads over 1500 with weights
+  // 13.8 / 12.8 / 14.6; 4 rows of 8 heads over 20000 24.0 / 24.0 / 24.9.  (Four would gain on
+  // short bf16 caches with idle CUs and lose in fp32.)
   p.min_tiles = 8;
   const int64_t units = (int64_t)B * Hkv * p.groups;
   const int tiles = ceil_div(cap, keys);
