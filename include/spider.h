@@ -611,10 +611,10 @@ spider_status spider_cache_select(int L, int B, int Hkv, int cap, const float* w
  * a tree move behind their context with base = lens, idx = their node numbers.
  * Strides: HOST [4], elements of (layer, sample, slot, head), not looked at where
  * there is one of these, else positive on the output side (its slots share no
- * memory); channels contiguous.  In place (k_out == k_in, v_out ==
- * v_in, the weights alike, equal strides and capacities) idx must ascend strictly
- * within a row (so idx[i] >= i); a row that does not ends with unspecified contents
- * in its own slots.
+ * memory); channels contiguous.  In place (k_out == k_in, v_out == v_in, the
+ * weights alike, equal strides and capacities) idx must ascend strictly within a
+ * row (so idx[i] >= i); a row that does not ends with unspecified contents in its
+ * own slots.
  * Otherwise input and output must not overlap.  Slots that nothing is moved
  * to are left as they were.
  * Requires dh <= 256, dh and the strides multiples of 16 bytes, caches 16-byte
@@ -652,8 +652,8 @@ spider_status spider_cache_compact(int L, int B, int Hkv, int dh, spider_dtype d
  * outside [0, V) anywhere are ignored.  Rows of nodes that are not alive are left
  * as they were in out and next_out.
  * Limits: T <= 256, B*T <= 65535, V <= 2^28, n_bias <= 32768, history_stride <=
- * 2^31 - 2^14.  Workspace: spider_adjust_logits_workspace_size(B, T, V) bytes (0 for V <= 32768),
- * 256-byte aligned; none without next_out.
+ * 2^31 - 2^14.  Workspace: spider_adjust_logits_workspace_size(B, T, V) bytes (0
+ * for V <= 32768), 256-byte aligned; none without next_out.
  * ------------------------------------------------------------------------ */
 size_t spider_adjust_logits_workspace_size(int B, int T, int V);
 
