@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "../../include/spider.h"
+#include "classes.h"
 
 namespace spider {
 
@@ -45,38 +46,6 @@ void clear_error();
   } while (0)
 
 // ----------------------------------------------------------------- profiler
-enum KernelClass {
-  KC_SCORE_PREP = 0,
-  KC_ANCHOR_TOPK,
-  KC_KMEANS,
-  KC_MAXSIM,
-  KC_SCORE_FINAL,
-  KC_SELECT,
-  KC_ASSEMBLE,
-  KC_EMBED,
-  KC_RMSNORM,
-  KC_GEMM_QKV,
-  KC_QKV_FINALIZE,
-  KC_ATTENTION,
-  KC_GEMM_O,
-  KC_GEMM_GATEUP,
-  KC_GEMM_DOWN,
-  KC_RESIDUAL,
-  KC_LENS_PREP,
-  KC_GEMM_LENS,
-  KC_LENS_ADMIT,
-  KC_COLMEAN,
-  KC_CLS_ATTN,
-  KC_PROJECTOR,
-  KC_LM_HEAD,
-  KC_TREE_ATTN,
-  KC_TREE_WEIGHTS,
-  KC_CACHE_SELECT,
-  KC_CACHE_COMPACT,
-  KC_ADJUST_LOGITS,
-  KC_COUNT
-};
-
 // Records a start event when profiling is enabled; the matching prof_end()
 // records the stop event.  Both are no-ops otherwise.
 void prof_begin(int cls, hipStream_t s);

@@ -72,7 +72,8 @@ const char* kClassNames[KC_COUNT] = {
     "select",     "assemble",    "embed",    "rmsnorm",       "gemm_qkv",
     "qkv_finalize", "attention", "gemm_o",   "gemm_gateup",   "gemm_down",
     "residual_add", "lens_prep", "gemm_lens", "lens_admit", "anchor_colmean", "cls_attention", "projector", "lm_head",
-    "tree_attention", "tree_weights", "cache_select", "cache_compact", "adjust_logits"};
+    "tree_attention", "tree_weights", "cache_select", "cache_compact", "adjust_logits",
+    "rope_append", "paged_attention", "pages_fork", "beam_select"};
 }  // namespace
 
 void prof_begin(int cls, hipStream_t s) {

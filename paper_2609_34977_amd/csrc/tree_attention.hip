@@ -17,13 +17,12 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attention_tiles.h"
 #include "kernels.h"
 
 namespace spider {
 namespace {
 
-typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
-typedef float float2v __attribute__((ext_vector_type(2)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr int kTreeMaxNodes = 256;
@@ -58,259 +57,6 @@ __device__ __forceinline__ int2 tree_extent(const TreeArgs& a, int b) {
   const int nn = a.n_nodes ? min(max(a.n_nodes[b], 0), a.T) : a.T;
   return make_int2(len, min(nn, a.cap - len));
 }
-
-// Four outputs x / l (0 where the row saw nothing) at element i, a multiple of 4.
-template <typename AT>
-__device__ __forceinline__ void tree_store(void* out, int64_t i, floatx4 x, float l) {
-  const float f = l == 0.f ? 0.f : 1.f / l;
-  x *= f;
-  if constexpr (sizeof(AT) == 4) {
-    *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(out) + i) = x;
-  } else {
-    const uint32_t w0 = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{x[0], x[1]}, bf16x2v));
-    const uint32_t w1 = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{x[2], x[3]}, bf16x2v));
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + i) = make_uint2(w0, w1);
-  }
-}
-
-// ------------------------------------------------------------------ tiles
-// A wave takes KEYS keys and RT tiles of 16 rows (queries of one kv head) at a time and
-// computes S^T = K Q^T and O^T += V^T P^T with 16x16 MFMAs, so a lane owns query
-// lane % 16 in both: the softmax runs in registers and P needs no exchange, because the
-// order of the keys within a product is free.  With g = lane / 16 the lane holds the
-// scores of keys 4g .. 4g+3 of each 16-key tile, so it also loads the values of these
-// keys: a 16-byte piece of consecutive channels each, 16 lanes a whole row.  Value
-// product n then takes channel n of every lane's piece.
-// Operands come straight from global memory: every key and value is used by one wave
-// (or by the few waves of other row groups, through L2), so LDS would only add a trip.
-template <typename AT, int DH>
-struct TreeTile;
-
-// bf16: 32 keys, v_mfma_f32_16x16x32_bf16.  k index 8g + e of the value product is key
-// 4g + e (e < 4) or 16 + 4g + e - 4.
-template <int DH>
-struct TreeTile<uint16_t, DH> {
-  static constexpr int KEYS = 32, KT = 2, NK = DH / 32, CPL = DH / 16;  // CPL: channels of a lane
-  static constexpr int VW = CPL / 2;                                     // words of a key's piece
-  struct Q {
-    bf16x8 f[NK];
-  };
-  struct K {
-    bf16x8 f[KT][NK];
-  };
-  struct V {
-    uint32_t w[8][VW];
-  };
-  // channel of accumulator n, operand row m
-  __device__ static __forceinline__ int channel(int n, int m) {
-    return DH <= 128 ? CPL * m + n : 128 * (n / 8) + 8 * m + n % 8;
-  }
-  __device__ static __forceinline__ int value_key(int e, int g) { return e < 4 ? 4 * g + e : 12 + 4 * g + e; }
-
-  template <bool FULL>
-  __device__ static __forceinline__ bf16x8 chunk(const uint16_t* p, int c, int dh) {
-    if (!FULL && c >= dh) return __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
-    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + c));
-  }
-  template <bool FULL>
-  __device__ static __forceinline__ void load_q(Q& q, const uint16_t* row, int g, int dh, bool flip) {
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      u32x4 x = __builtin_bit_cast(u32x4, chunk<FULL>(row, 32 * i + 8 * g, dh));
-      if (flip) x ^= 0x80008000u;
-      q.f[i] = __builtin_bit_cast(bf16x8, x);
-    }
-  }
-  template <bool FULL>
-  __device__ static __forceinline__ void load_k(K& k, const uint16_t* base, int64_t stride, int j0, int n, int lane,
-                                                int dh) {
-#pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      const uint16_t* row = base + (int64_t)min(j0 + 16 * t + (lane & 15), n - 1) * stride;
-#pragma unroll
-      for (int i = 0; i < NK; ++i) k.f[t][i] = chunk<FULL>(row, 32 * i + 8 * (lane >> 4), dh);
-    }
-  }
-  template <bool FULL>
-  __device__ static __forceinline__ void load_v(V& v, const uint16_t* base, int64_t stride, int j0, int n, int lane,
-                                                int dh) {
-    const int m = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint16_t* row = base + (int64_t)min(j0 + value_key(e, g), n - 1) * stride;
-      if constexpr (DH == 64) {
-        uint2 x = make_uint2(0, 0);
-        if (FULL || 4 * m < dh) x = *reinterpret_cast<const uint2*>(row + 4 * m);
-        v.w[e][0] = x.x;
-        v.w[e][1] = x.y;
-      } else {
-#pragma unroll
-        for (int q = 0; q < DH / 128; ++q) {
-          const u32x4 x = __builtin_bit_cast(u32x4, chunk<FULL>(row, 128 * q + 8 * m, dh));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v.w[e][4 * q + i] = x[i];
-        }
-      }
-    }
-  }
-  __device__ static __forceinline__ void scores(floatx4* s, const K& k, const Q& q) {
-#pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      s[t] = floatx4{};
-#pragma unroll
-      for (int i = 0; i < NK; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.f[t][i], q.f[i], s[t], 0, 0, 0);
-    }
-  }
-  // the operands of the value products: channel n of the lane's eight keys, put together
-  // from the rows, or read that way
-  struct Ops {
-    u32x4 f[CPL];
-  };
-  __device__ static __forceinline__ bf16x8 operand(const V& v, int n) {
-    u32x4 x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      x[e] = __builtin_amdgcn_perm(v.w[2 * e + 1][n / 2], v.w[2 * e][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
-    return __builtin_bit_cast(bf16x8, x);
-  }
-  __device__ static __forceinline__ bf16x8 operand(const Ops& v, int n) { return __builtin_bit_cast(bf16x8, v.f[n]); }
-  // infinite and NaN values become 0; whether there was one (bits in a register: a flag per
-  // comparison would be a pair of scalar registers each)
-  __device__ static __forceinline__ uint32_t finite(uint32_t x, uint32_t& bad) {
-    const uint32_t drop = ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-    bad |= drop;
-    return x & ~drop;
-  }
-  __device__ static __forceinline__ bool drop_nonfinite(V& v) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int i = 0; i < VW; ++i) v.w[e][i] = finite(v.w[e][i], bad);
-    return bad != 0;
-  }
-  __device__ static __forceinline__ bool drop_nonfinite(Ops& v) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int n = 0; n < CPL; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v.f[n][e] = finite(v.f[n][e], bad);
-    return bad != 0;
-  }
-  __device__ static __forceinline__ uint32_t pack(float a0, float a1) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{a0, a1}, bf16x2v));
-  }
-  __device__ static __forceinline__ float value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
-  // O^T += V^T P^T.  The fp32 weights enter as bf16 high and low parts, 16 significant bits,
-  // as in the prefill's attention (rounded to bf16 once, an output of 16384 slots is 2.3e-3 off
-  // the exact one instead of 1.7e-3, most of which is its own rounding).
-  template <int RT, typename S>
-  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const S& v, const float (*p)[KT * 4]) {
-    bf16x8 hi[RT], lo[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      u32x4 wh, wl;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float a0 = p[r][2 * e], a1 = p[r][2 * e + 1];
-        wh[e] = pack(a0, a1);
-        wl[e] = pack(a0 - __uint_as_float(wh[e] << 16), a1 - __uint_as_float(wh[e] & 0xFFFF0000u));
-      }
-      hi[r] = __builtin_bit_cast(bf16x8, wh);
-      lo[r] = __builtin_bit_cast(bf16x8, wl);
-    }
-#pragma unroll
-    for (int n = 0; n < CPL; ++n) {
-      const bf16x8 a = operand(v, n);
-#pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi[r], o[r][n], 0, 0, 0);
-        o[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo[r], o[r][n], 0, 0, 0);
-      }
-    }
-  }
-};
-
-// fp32: 16 keys, v_mfma_f32_16x16x4_f32 (exact products, fp32 sums).  Channels of the
-// score product go in the order of the lanes' 16-byte pieces; value product (i, n) takes
-// key 4g + i.
-template <int DH>
-struct TreeTile<float, DH> {
-  static constexpr int KEYS = 16, KT = 1, NK = DH / 16, CPL = DH / 16;
-  struct Q {
-    floatx4 f[NK];
-  };
-  struct K {
-    floatx4 f[NK];
-  };
-  struct V {
-    floatx4 f[4][DH / 64];
-  };
-  __device__ static __forceinline__ int channel(int n, int m) { return 64 * (n / 4) + 4 * m + n % 4; }
-  __device__ static __forceinline__ int value_key(int e, int g) { return 4 * g + e; }
-
-  template <bool FULL>
-  __device__ static __forceinline__ floatx4 chunk(const float* p, int c, int dh) {
-    if (!FULL && c >= dh) return floatx4{};
-    return *reinterpret_cast<const floatx4*>(p + c);
-  }
-  template <bool FULL>
-  __device__ static __forceinline__ void load_q(Q& q, const float* row, int g, int dh, bool flip) {
-#pragma unroll
-    for (int i = 0; i < NK; ++i) {
-      const floatx4 x = chunk<FULL>(row, 16 * i + 4 * g, dh);
-      q.f[i] = flip ? -x : x;
-    }
-  }
-  template <bool FULL>
-  __device__ static __forceinline__ void load_k(K& k, const float* base, int64_t stride, int j0, int n, int lane,
-                                                int dh) {
-    const float* row = base + (int64_t)min(j0 + (lane & 15), n - 1) * stride;
-#pragma unroll
-    for (int i = 0; i < NK; ++i) k.f[i] = chunk<FULL>(row, 16 * i + 4 * (lane >> 4), dh);
-  }
-  template <bool FULL>
-  __device__ static __forceinline__ void load_v(V& v, const float* base, int64_t stride, int j0, int n, int lane,
-                                                int dh) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float* row = base + (int64_t)min(j0 + value_key(e, lane >> 4), n - 1) * stride;
-#pragma unroll
-      for (int q = 0; q < DH / 64; ++q) v.f[e][q] = chunk<FULL>(row, 64 * q + 4 * (lane & 15), dh);
-    }
-  }
-  __device__ static __forceinline__ void scores(floatx4* s, const K& k, const Q& q) {
-    s[0] = floatx4{};
-#pragma unroll
-    for (int i = 0; i < NK; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[i][c], q.f[i][c], s[0], 0, 0, 0);
-  }
-  __device__ static __forceinline__ bool drop_nonfinite(V& v) {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int n = 0; n < CPL; ++n) {
-        const uint32_t x = __float_as_uint(v.f[e][n / 4][n % 4]);
-        const uint32_t drop = (x & 0x7F800000u) == 0x7F800000u ? ~0u : 0u;
-        bad |= drop;
-        v.f[e][n / 4][n % 4] = __uint_as_float(x & ~drop);
-      }
-    return bad != 0;
-  }
-  __device__ static __forceinline__ float value(const float* p) { return *p; }
-  template <int RT, typename S>
-  __device__ static __forceinline__ void values(floatx4 (*o)[CPL], const S& v, const float (*p)[4]) {
-#pragma unroll
-    for (int n = 0; n < CPL; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-          o[r][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.f[e][n / 4][n % 4], p[r][e], o[r][n], 0, 0, 0);
-  }
-};
 
 // Bits of the KEYS keys from j0 that node t sees: the context, then its mask.
 template <int KEYS>
@@ -348,20 +94,10 @@ __device__ __forceinline__ TreeSplits tree_splits(const TreeArgs& a, int tiles) 
   return TreeSplits{most == 1 ? 1 : (tiles + per - 1) / per, per};
 }
 
-// The maximum may lag behind by this much (in powers of two) before the sums are
-// rescaled: the exponentials then stay below 2^8.
-constexpr float kLazyMax = 8.f;
-
-// x f of a sum x that goes onto another maximum: an infinite or NaN x stays what it is where
-// f has underflowed to 0.
-__device__ __forceinline__ float rescaled(float x, float f) {
-  return f == 0.f && !(fabsf(x) < INFINITY) ? x : x * f;
-}
-
 // RT row tiles of a wave: queries, and the running maximum, sum and output of their rows.
 template <typename AT, int DH, int RT>
 struct RowTiles {
-  using T = TreeTile<AT, DH>;
+  using T = AttnTile<AT, DH>;
   static constexpr int KEYS = T::KEYS, NS = 4 * T::KT, CPL = T::CPL;  // NS: scores of a lane and row tile
   typename T::Q q[RT];
   int node[RT];
@@ -648,7 +384,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) tree_attention_ker
       if (w.ns > 1) {
         *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + c) = x;
       } else {
-        tree_store<AT>(a.out, out_row * a.dh + c, x, l);
+        attn_store<AT>(a.out, out_row * a.dh + c, x, l);
       }
     }
   }
@@ -768,7 +504,7 @@ __global__ void __launch_bounds__(64 * NW, 2) tree_rows_kernel(TreeArgs a) {
       const int ch = 16 * c + 4 * g;  // of four consecutive outputs
       if (!FULL && ch >= a.dh) continue;
       if (w.ns > 1) *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + ch) = rows.o[r][c];
-      else tree_store<uint16_t>(a.out, out_row * a.dh + ch, rows.o[r][c], l);
+      else attn_store<uint16_t>(a.out, out_row * a.dh + ch, rows.o[r][c], l);
     }
   }
 }
@@ -798,7 +534,7 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, float sc) {
   if (b >= a.B) return;
   const int2 ext = tree_extent(a, b);
   if (t >= ext.y) return;
-  constexpr int KEYS = TreeTile<AT, 64>::KEYS;
+  constexpr int KEYS = AttnTile<AT, 64>::KEYS;
   const int ns = tree_splits(a, (ext.x + ext.y + KEYS - 1) / KEYS).n;
   if (ns == 1) return;
   const int G = a.H / a.Hkv, hk = h / G;
@@ -844,13 +580,13 @@ __device__ __forceinline__ void tree_join(const TreeArgs& a, float sc) {
     l += ls[i * per + tid];
   }
   const int64_t row = ((int64_t)b * a.T + t) * a.H + h;
-  tree_store<AT>(a.out, row * a.dh + c, x, l);
+  attn_store<AT>(a.out, row * a.dh + c, x, l);
   if (a.stat && tid == 0) a.stat[row] = make_float2(mx == -INFINITY ? 0.f : mx * sc, l == 0.f ? 0.f : 1.f / l);
 }
 
 template <typename AT>
 __global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
-  constexpr int KEYS = TreeTile<AT, 64>::KEYS;
+  constexpr int KEYS = AttnTile<AT, 64>::KEYS;
   __shared__ float2 st[16];
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
   if ((int)blockIdx.x < a.join_blocks) {
@@ -925,7 +661,7 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeArgs a) {
 // and registers (width 256 has none).
 template <typename AT, int DH, bool FULL, int NT>
 __global__ void __launch_bounds__(256) tree_weights_kernel(TreeArgs a) {
-  using T = TreeTile<AT, DH>;
+  using T = AttnTile<AT, DH>;
   constexpr int KEYS = T::KEYS, NS = 4 * T::KT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int m = lane & 15, g = lane >> 4;
@@ -1065,7 +801,7 @@ void launch_tree_rows(const TreeArgs& a, hipStream_t st) {
 
 template <typename AT, int DH, int NT>
 void launch_tree_weights(const TreeArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)ceil_div(a.cap, 4 * NT * TreeTile<AT, DH>::KEYS) * (unsigned)(a.B * a.Hkv);
+  const unsigned grid = (unsigned)ceil_div(a.cap, 4 * NT * AttnTile<AT, DH>::KEYS) * (unsigned)(a.B * a.Hkv);
   if (a.dh == DH) tree_weights_kernel<AT, DH, true, NT><<<grid, 256, 0, st>>>(a);
   else tree_weights_kernel<AT, DH, false, NT><<<grid, 256, 0, st>>>(a);
 }
@@ -1092,7 +828,7 @@ spider_status run_tree(const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   }
   if (a.w_out && !a.scores) {
     ProfScope ps(KC_TREE_WEIGHTS, st);
-    const bool two = (int64_t)a.B * a.Hkv * ceil_div(a.cap, 8 * TreeTile<AT, DH>::KEYS) >= 512;
+    const bool two = (int64_t)a.B * a.Hkv * ceil_div(a.cap, 8 * AttnTile<AT, DH>::KEYS) >= 512;
     if constexpr (DH <= 128) {
       if (two) launch_tree_weights<AT, DH, 2>(a, st);
       else launch_tree_weights<AT, DH, 1>(a, st);
