@@ -666,6 +666,180 @@ spider_status spider_adjust_logits(
     spider_stream stream);
 
 /* ------------------------------------------------------------------------
+ * Beams and chunks over a paged cache.  Pages of page_size slots (a power of two
+ * from 8 to 4096) hold the keys and values of many sequences in one layer: slot j
+ * of sequence b is slot j % page_size of page table[b*table_stride + j / page_size].
+ * Element (page, slot, head, c) of k and v lies at page*stride_page +
+ * slot*stride_slot + head*stride_head + c.  A table entry outside [0, n_pages) is
+ * an absent page: its slots are neither seen nor written.
+ * The new tokens of all sequences are packed: rows cu[b] .. cu[b+1] - 1 (ascending,
+ * taken into [0, N]) are those of sequence b, and lens[b] (taken into [0,
+ * max_pages*page_size]) counts its filled slots with them, so that its last row is
+ * at position lens[b] - 1.  A row whose position is below 0 sees and stores
+ * nothing; rows before cu[0] and from cu[B] on belong to no sequence and are left
+ * as they were.
+ * table, lens and cu are device int32; k, v 16-byte aligned, the strides multiples
+ * of 16 bytes (that of a dimension of size 1 is not looked at), dh a multiple of 16
+ * bytes and at most 256, B <= 65535, max_pages * page_size <= 2^30.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t stride_page, stride_slot, stride_head;
+  int n_pages, page_size;
+  const int32_t* table;  /* [B][max_pages], row stride table_stride */
+  int64_t table_stride;
+  int max_pages;
+  const int32_t* lens;   /* [B]     */
+  const int32_t* cu;     /* [B + 1] */
+  int B;
+} spider_paged_cache;
+
+/* ------------------------------------------------------------------------
+ * spider_rope_axes - frequencies and axes of rotary positions with several axes
+ * (time, height, width, ..).  Host only.  Of rot / 2 frequencies theta^(-2i/rot)
+ * sections[a] turn by the position of axis a (their sum is rot / 2): in blocks, axis
+ * after axis, or interleaved: frequency i by axis i % n_axes while that axis has
+ * any left, else by axis 0 (sections that this cannot serve are refused).
+ * freq_out HOST double [rot / 2], axis_out HOST uint8 [rot / 2].  rot even, at most
+ * 256, n_axes <= 8.
+ * ------------------------------------------------------------------------ */
+spider_status spider_rope_axes(int rot, double theta, int n_axes, const int32_t* sections, int interleaved,
+                               double* freq_out, uint8_t* axis_out);
+
+/* ------------------------------------------------------------------------
+ * spider_rope_append - rotary positions on the queries and keys of N tokens, the
+ * keys and values stored in the pages of their sequences.  For row r, pair i <
+ * rot / 2 of a head's channels (rotate-half, as spider_prefill):
+ *   a = pos[axis[i]*pos_stride + r] * freq[i]
+ *   (x_i, x_{i+rot/2}) -> (x_i cos a - x_{i+rot/2} sin a, x_{i+rot/2} cos a + x_i sin a)
+ * channels from rot on stay as they are.  Row r of q [N][H][dh] (row stride
+ * q_stride, heads side by side) goes to q_out (row stride q_out_stride; may be q
+ * itself with the same stride), of k and v [N][Hkv][dh] (row strides k_stride,
+ * v_stride) to the row's slot of the cache.  q and q_out NULL: no queries; k, v and
+ * cache NULL: no keys, and every row is turned.
+ * pos device int32 [n_axes][N], freq device double and axis device uint8 [rot / 2]
+ * (spider_rope_axes, or any others; entries of axis at n_axes or above count as the
+ * last axis).  Angles in fp64 (|a| below 2^30), their cosines and sines rounded to
+ * fp32, the rotation in fp32, rounded once.
+ * Two rows whose slots are the same (a page that stands in the tables twice) leave
+ * either's.  q_out and the cache overlap no other input.
+ * Requires rot even, rot <= dh, n_axes <= 8, H and Hkv <= 65535, N < 2^24, q, q_out,
+ * k, v 16-byte aligned, row strides multiples of 16 bytes, no stride of the cache 0.
+ * No workspace.
+ * ------------------------------------------------------------------------ */
+spider_status spider_rope_append(int N, int H, int Hkv, int dh, int rot, int n_axes, const int32_t* pos,
+                                 int64_t pos_stride, const double* freq, const uint8_t* axis, const void* q,
+                                 int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, const spider_paged_cache* cache, spider_dtype dtype,
+                                 spider_stream stream);
+
+/* ------------------------------------------------------------------------
+ * spider_paged_attention - attention of the new tokens over the pages, for grouped
+ * heads (query head h reads kv head h / (H / Hkv)): chunks of a prompt, single
+ * decoded tokens (one row per sequence), or both in one batch.  For row r at position p, head h
+ * and its kv head:
+ *   s(j) = scale * q[r,h] . k[j]   over the slots max(0, p - window + 1) <= j <= p
+ *          (window 0: all j <= p) whose page is present
+ *   out  = sum_j softmax(s)(j) v[j]   (0 where it sees no slot)
+ * Slots that a row does not see do not enter its sums, whatever they hold; an
+ * infinite or NaN value of a slot that it sees makes its output infinite or NaN.
+ * q element (r,h,c) at q[r*q_stride + h*dh + c]; out [N][H][dh] contiguous in q's
+ * dtype, overlapping no input.
+ * Precision: products exact, sums, maxima and exponentials fp32, out rounded once.
+ * bf16: the softmax numerators enter the product with v rounded to bf16 once, and
+ * the sum that divides them is that of the rounded ones.
+ * Requires H % Hkv == 0, H <= 65535, N * H < 2^24, B * Hkv < 2^22, q and out 16-byte
+ * aligned, q_stride a multiple of 16 bytes.  Workspace:
+ * spider_paged_attention_workspace_size(N, B, H, Hkv, dh, dtype) bytes, 256-byte
+ * aligned.
+ * ------------------------------------------------------------------------ */
+size_t spider_paged_attention_workspace_size(int N, int B, int H, int Hkv, int dh, spider_dtype dtype);
+
+spider_status spider_paged_attention(int N, int H, int Hkv, int dh, const void* q, int64_t q_stride,
+                                     const spider_paged_cache* cache, spider_dtype dtype, float scale, int window,
+                                     void* out, void* workspace, size_t workspace_bytes, spider_stream stream);
+
+/* ------------------------------------------------------------------------
+ * spider_pages_fork - the page tables of the next step.  New sequence b < B_out
+ * continues old sequence parent[b] < B_in (several may continue one, some none), or
+ * starts empty (any other parent), and gets room for n_new[b] further slots (NULL:
+ * 0; negative counts as 0): n = lens_in[parent[b]] (0 if empty; taken into [0,
+ * max_pages*page_size]), lens_out[b] = min(n + n_new[b], max_pages*page_size), 0 if
+ * empty.
+ *   References: ref[p] counts the table entries (and other holders) of page p; a page is
+ *   free where ref[p] <= 0.  The old sequences give up theirs, the new ones take
+ *   one for each page they continue: pages that nobody continues are freed.
+ *   Copies: a sequence that gets new slots within a partly filled page (its last)
+ *   needs it for itself.  If others hold it too, the first of the sequences that
+ *   write into it keeps it, provided that only those hold it; each other one gives it up
+ *   for a free page, into which the filled slots are copied, in all L layers.
+ *   Room: the pages taken are the lowest free ones, in ascending order, handed out
+ *   by ascending b: its copy first, then the pages of its new slots.  Their ref is
+ *   1.  Where none is left the entries are -1, and missing_out counts them.
+ * table_in [B_in][max_pages] (entries outside [0, n_pages) are absent and hold
+ * nothing), lens_in [B_in], ref_in [n_pages], parent and n_new [B_out];
+ * table_out [B_out][max_pages] (-1 behind a sequence's pages and where a page is
+ * absent), lens_out [B_out], ref_out [n_pages], missing_out [1]: device int32,
+ * outputs overlapping neither inputs nor each other.  Thus lens_out is what
+ * spider_rope_append and spider_paged_attention want for the n_new tokens.
+ * k, v: pages of all L layers, strides HOST [4], elements of (layer, page, slot,
+ * head); positive where there is more than one, multiples of 16 bytes; 16-byte
+ * aligned; dh a multiple of 16 bytes, at most 256.
+ * Limits: B_in, B_out <= 4096, L * B_out <= 65535, page_size a power of two from 8
+ * to 4096, max_pages * page_size and page_size * Hkv * dh <= 2^30.  Workspace:
+ * spider_pages_fork_workspace_size(B_out, n_pages) bytes, 256-byte aligned.
+ * ------------------------------------------------------------------------ */
+size_t spider_pages_fork_workspace_size(int B_out, int n_pages);
+
+spider_status spider_pages_fork(int L, int Hkv, int dh, spider_dtype dtype, void* k, void* v, const int64_t strides[4],
+                                int n_pages, int page_size, int max_pages, int B_in, const int32_t* table_in,
+                                const int32_t* lens_in, const int32_t* ref_in, int B_out, const int32_t* parent,
+                                const int32_t* n_new, int32_t* table_out, int32_t* lens_out, int32_t* ref_out,
+                                int32_t* missing_out, void* workspace, size_t workspace_bytes, spider_stream stream);
+
+/* ------------------------------------------------------------------------
+ * spider_beam_select - one step of beam search for B samples of K beams (rows b*K +
+ * k of the logits): the n_out best continuations of every sample.
+ *   lse  = log sum_v exp(logits[row][v])
+ *   cand = scores[row] + (logits[row][v] - lse)   for every token v of an open beam
+ *   cand = scores[row], v = eos                    for a finished one (done[row] != 0)
+ * in descending order: between beams ties go to the lower beam; within a beam the
+ * order is that of the logits, ties to the lower token.  Logits of -inf or NaN are no
+ * candidates (and count as 0 in the sum); a beam whose score or lse is not finite
+ * has none.
+ *   scores_out[b][i] = cand, parent_out = b*K + its beam, token_out = v,
+ *   done_out = 1 if the beam was finished or v == eos, else 0
+ * and where there are fewer than n_out: -inf, -1, -1, 1.
+ * The histories follow (all four arrays, or all NULL): row b*n_out + i gets its
+ * parent's first n_history entries (taken into [0, history_cap]), then, unless the beam was
+ * finished or the row is full, its token; n_history_out is their number, 0 without a
+ * parent; later entries are left as they were.
+ * The first step of a search has K = 1 and n_out beams.  parent_out is what
+ * spider_pages_fork takes.
+ * logits fp32 or bf16, row stride logits_stride; scores fp32 [B][K]; done int32
+ * [B][K] or NULL (none is finished); eos a token, or -1 (nothing ends a beam; done
+ * must be NULL).  scores_out fp32, parent_out, token_out, done_out int32
+ * [B][n_out].  history int32 [B*K] rows of history_cap entries at history_stride,
+ * history_out [B*n_out] at history_out_stride; n_history [B*K], n_history_out
+ * [B*n_out].  All on the device; outputs overlap no input.
+ * Precision: exponentials within 2^-23 relative, their sum, the logarithm and the candidates in
+ * fp64; scores_out rounded once.
+ * Limits: K, n_out <= 64, V <= 2^19, B*K and B*n_out <= 65535, history_cap <= 2^24.
+ * Workspace: spider_beam_select_workspace_size(B, K, n_out, V) bytes, 256-byte
+ * aligned.
+ * ------------------------------------------------------------------------ */
+size_t spider_beam_select_workspace_size(int B, int K, int n_out, int V);
+
+spider_status spider_beam_select(int B, int K, int n_out, int V, const void* logits, int64_t logits_stride,
+                                 spider_dtype dtype, const float* scores, const int32_t* done, int eos,
+                                 float* scores_out, int32_t* parent_out, int32_t* token_out, int32_t* done_out,
+                                 const int32_t* history, int64_t history_stride, const int32_t* n_history,
+                                 int history_cap, int32_t* history_out, int64_t history_out_stride,
+                                 int32_t* n_history_out, void* workspace, size_t workspace_bytes,
+                                 spider_stream stream);
+
+/* ------------------------------------------------------------------------
  * Kernel-class profiler (process-global, not thread-safe; for benchmarks).
  * When enabled, every launch of the library records a pair of HIP events on
  * its stream.  spider_profile_read() synchronises on the recorded events and

@@ -42,6 +42,13 @@ class KVCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("cap", ctypes.c_int)]
 
 
+class PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int), ("lens", ctypes.c_void_p), ("cu", ctypes.c_void_p),
+                ("B", ctypes.c_int)]
+
+
 _VP, _I, _I64, _SZ, _F, _D = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t,
                               ctypes.c_float, ctypes.c_double)
 
@@ -94,6 +101,17 @@ _SIGS = {
     "spider_adjust_logits_workspace_size": ([_I, _I, _I], _SZ),
     "spider_adjust_logits": ([_I, _I, _I, _VP, _I64, _I, _VP, _I64, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
                               _I, _VP, _I64, _VP, _I64, _VP, _VP, _SZ, _VP], _I),
+    "spider_rope_axes": ([_I, _D, _I, _VP, _I, _VP, _VP], _I),
+    "spider_rope_append": ([_I, _I, _I, _I, _I, _I, _VP, _I64, _VP, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64,
+                            ctypes.POINTER(PagedCache), _I, _VP], _I),
+    "spider_paged_attention_workspace_size": ([_I, _I, _I, _I, _I, _I], _SZ),
+    "spider_paged_attention": ([_I, _I, _I, _I, _VP, _I64, ctypes.POINTER(PagedCache), _I, _F, _I, _VP, _VP, _SZ, _VP], _I),
+    "spider_pages_fork_workspace_size": ([_I, _I], _SZ),
+    "spider_pages_fork": ([_I, _I, _I, _I, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ,
+                           _VP], _I),
+    "spider_beam_select_workspace_size": ([_I, _I, _I, _I], _SZ),
+    "spider_beam_select": ([_I, _I, _I, _I, _VP, _I64, _I, _VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _I64, _VP, _I, _VP, _I64, _VP, _VP, _SZ,
+                            _VP], _I),
     "spider_profile_enable": ([_I], _I),
     "spider_profile_mask": ([ctypes.c_uint32], _I),
     "spider_profile_classes": ([], _I),
@@ -723,6 +741,183 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
         logits.data_ptr() if inplace else _need(out, "out", f32, lead + (V,), dev), row if inplace else V,
         _need(next_ids, "next_ids", i32, lead, dev), wptr, wsz)
     return out, next_ids
+
+
+# ----------------------------------------------------------------- beams and chunks over a paged cache
+def _paged(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, like: torch.Tensor):
+    """Descriptor of one layer's pages k and v [n_pages, page_size, Hkv, dh] and its batch."""
+    dev = like.device
+    if k.dim() != 4 or k.stride(3) != 1 or not _alike(k, v):
+        raise ValueError("k and v pages must be [n_pages, page_size, Hkv, dh] alike, with contiguous channels")
+    if k.dtype != like.dtype or v.dtype != like.dtype or k.device != dev or v.device != dev:
+        raise ValueError("rows and pages must share dtype and device")
+    if table.dim() != 2 or table.dtype is not torch.int32 or table.device != dev or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError(f"table must be an int32 [B, max_pages] tensor on {dev} with contiguous rows")
+    B = table.shape[0]
+    return PagedCache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.shape[0], k.shape[1], table.data_ptr(),
+                      table.stride(0), table.shape[1], _need(lens, "lens", torch.int32, (B,), dev),
+                      _need(cu, "cu_q", torch.int32, (B + 1,), dev), B)
+
+
+def _rows(t: torch.Tensor, name: str, like: torch.Tensor):
+    """Checks rows [N, heads, dh] whose heads lie side by side."""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must be [N, heads, dh] with the heads of a row side by side, of one dtype and device")
+    return t
+
+
+def rope_axes(rot: int, theta: float, sections, interleaved: bool = False):
+    """Frequencies (float64) and axes (uint8) of rot / 2 pairs of channels, NumPy arrays for the
+    host: sections[a] of the frequencies theta^(-2i/rot) for axis a, in blocks or in turn."""
+    s = np.ascontiguousarray(sections, dtype=np.int32)
+    if s.ndim != 1 or rot < 2 or rot > 256:
+        raise ValueError("sections must be a list, rot from 2 to 256")
+    freq = np.zeros(rot // 2, np.float64)
+    axis = np.zeros(rot // 2, np.uint8)
+    _check(lib().spider_rope_axes(rot, theta, len(s), s.ctypes.data, int(bool(interleaved)), freq.ctypes.data, axis.ctypes.data))
+    return freq, axis
+
+
+def rope_append(pos: torch.Tensor, freq: torch.Tensor, axis: torch.Tensor, *, q: Optional[torch.Tensor] = None,
+                q_out: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+                lens: Optional[torch.Tensor] = None, cu_q: Optional[torch.Tensor] = None):
+    """Rotary positions pos [n_axes, N] int32 on q [N, H, dh] (into q_out, a new tensor if None,
+    or q itself) and on k [N, Hkv, dh], which goes with v into the pages [n_pages, page_size,
+    Hkv, dh] of its sequences: table [B, max_pages], lens [B], cu_q [B + 1] int32.  freq float64
+    and axis uint8 [rot / 2] on the GPU (from rope_axes).  Returns q_out (None without q)."""
+    ref = q if q is not None else k
+    if ref is None:
+        raise ValueError("q or k is needed")
+    dev = _gpu(ref)
+    N, _, dh = _rows(ref, "q" if q is not None else "k", ref).shape
+    if any((t is None) != (k is None) for t in (v, k_pages, v_pages, table, lens, cu_q)):
+        raise ValueError("k, v, k_pages, v_pages, table, lens and cu_q go together")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if pos.dim() != 2 or pos.shape[1] != N or pos.dtype is not torch.int32 or pos.device != dev or (N > 1 and pos.stride(1) != 1):
+        raise ValueError(f"pos must be an int32 [n_axes, {N}] tensor on {dev} with contiguous rows")
+    if freq.dim() != 1:
+        raise ValueError("freq must be [rot / 2]")
+    half = freq.shape[0]
+    f, ax = _need(freq, "freq", torch.float64, (half,), dev), _need(axis, "axis", torch.uint8, (half,), dev)
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        elif _rows(q_out, "q_out", q).shape != q.shape:
+            raise ValueError("q_out must have the shape of q")
+    desc = None
+    if k is not None:
+        if _rows(k, "k", ref).shape != _rows(v, "v", ref).shape or k.shape[0] != N or k.shape[2] != dh:
+            raise ValueError("k and v must be [N, Hkv, dh] alike, with the N and dh of q")
+        desc = _paged(k_pages, v_pages, table, lens, cu_q, ref)
+        if k_pages.shape[2:] != k.shape[1:]:
+            raise ValueError("the pages must have the heads and channels of k")
+    _on(dev, lib().spider_rope_append, N, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, dh, 2 * half, pos.shape[0],
+        pos.data_ptr(), pos.stride(0), f, ax, None if q is None else q.data_ptr(), 0 if q is None else q.stride(0),
+        None if q is None else q_out.data_ptr(), 0 if q is None else q_out.stride(0), None if k is None else k.data_ptr(),
+        0 if k is None else k.stride(0), None if k is None else v.data_ptr(), 0 if k is None else v.stride(0),
+        None if desc is None else ctypes.byref(desc), _dt(ref))
+    return q_out
+
+
+def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                    cu_q: torch.Tensor, *, window: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens q [N, H, dh] over the pages [n_pages, page_size, Hkv, dh] (views
+    of any layout whose channels are contiguous): rows cu_q[b] .. cu_q[b+1] - 1 are the last ones
+    of the lens[b] filled slots of sequence b, whose pages are table[b].  window: the number of
+    slots a row sees, up to its own (0: all).  ``scale`` defaults to dh ** -0.5."""
+    dev = _gpu(q)
+    N, H, dh = _rows(q, "q", q).shape
+    desc = _paged(k_pages, v_pages, table, lens, cu_q, q)
+    Hkv = k_pages.shape[2]
+    if k_pages.shape[3] != dh:
+        raise ValueError("the pages must have the channels of q")
+    if out is None:
+        out = torch.empty(N, H, dh, dtype=q.dtype, device=dev)
+    dt = _dt(q)
+    wsz = _size("spider_paged_attention_workspace_size", N, desc.B, H, Hkv, dh, dt)
+    workspace, wptr = _scratch(workspace, wsz, dev)
+    _on(dev, lib().spider_paged_attention, N, H, Hkv, dh, q.data_ptr(), q.stride(0), ctypes.byref(desc), dt,
+        dh ** -0.5 if scale is None else scale, window, _need(out, "out", q.dtype, (N, H, dh), dev), wptr, wsz)
+    return out
+
+
+def pages_fork(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, ref: torch.Tensor, parent: torch.Tensor, *,
+               n_new: Optional[torch.Tensor] = None, table_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+               ref_out: Optional[torch.Tensor] = None, missing: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """The next step's page tables of a cache k and v [L, n_pages, page_size, Hkv, dh] (views of any
+    layout whose channels are contiguous): new sequence b continues old sequence parent[b] (-1:
+    none) of table [B, max_pages] and lens [B], with room for n_new[b] more slots; ref [n_pages]
+    counts who holds a page.  All int32.  Shared last pages are copied in k and v before two
+    sequences write into them.  Returns (table_out, lens_out, ref_out, missing [1])."""
+    if k.dim() != 5 or table.dim() != 2 or parent.dim() != 1:
+        raise ValueError("k and v must be [L, n_pages, page_size, Hkv, dh], table [B, max_pages], parent [B_out]")
+    dev = _gpu(k)
+    L_, n_pages, page_size, Hkv, dh = k.shape
+    if not _alike(k, v) or k.stride(4) != 1 or v.dtype != k.dtype or v.device != dev:
+        raise ValueError("k and v must be alike, with contiguous channels")
+    B, M = table.shape
+    n = parent.shape[0]
+    i32 = torch.int32
+    if table_out is None:
+        table_out = torch.empty(n, M, dtype=i32, device=dev)
+    if lens_out is None:
+        lens_out = torch.empty(n, dtype=i32, device=dev)
+    if ref_out is None:
+        ref_out = torch.empty(n_pages, dtype=i32, device=dev)
+    if missing is None:
+        missing = torch.empty(1, dtype=i32, device=dev)
+    strides = (ctypes.c_int64 * 4)(*k.stride()[:4])
+    wsz = _size("spider_pages_fork_workspace_size", n, n_pages)
+    workspace, wptr = _scratch(workspace, wsz, dev)
+    _on(dev, lib().spider_pages_fork, L_, Hkv, dh, _dt(k), k.data_ptr(), v.data_ptr(), strides, n_pages, page_size, M, B,
+        _need(table, "table", i32, (B, M), dev), _need(lens, "lens", i32, (B,), dev), _need(ref, "ref", i32, (n_pages,), dev), n,
+        _need(parent, "parent", i32, (n,), dev), _need(n_new, "n_new", i32, (n,), dev), _need(table_out, "table_out", i32, (n, M), dev),
+        _need(lens_out, "lens_out", i32, (n,), dev), _need(ref_out, "ref_out", i32, (n_pages,), dev),
+        _need(missing, "missing", i32, (1,), dev), wptr, wsz)
+    return table_out, lens_out, ref_out, missing
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, n_out: int, *, done: Optional[torch.Tensor] = None, eos: int = -1,
+                history: Optional[torch.Tensor] = None, n_history: Optional[torch.Tensor] = None,
+                history_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+    """The n_out best continuations of each sample's beams: logits [B, K, V] (contiguous rows at one
+    distance), scores [B, K] fp32, done [B, K] int32 with ``eos`` the token that ends a beam.
+    history [B * K, cap] int32 with n_history [B * K] filled entries follows into history_out
+    [B * n_out, cap].  Returns {"scores", "parent" (b * K + beam), "token", "done"} [B, n_out], and
+    with a history {"history", "n_history"}."""
+    if logits.dim() != 3 or logits.stride(2) != 1 or (min(logits.shape[:2]) > 1 and logits.stride(0) != logits.shape[1] * logits.stride(1)):
+        raise ValueError("logits must be [B, K, V] with contiguous rows at one distance")
+    B, K, V = logits.shape
+    dev = _gpu(logits)
+    if n_out < 1:
+        raise ValueError("n_out must be at least 1")
+    if (history is None) != (n_history is None) or (history is None and history_out is not None):
+        raise ValueError("history, n_history and history_out go together")
+    row = logits.stride(1) if K > 1 else logits.stride(0)
+    row = max(row, V) if B * K == 1 else row
+    i32 = torch.int32
+    ints = torch.empty(3, B, n_out, dtype=i32, device=dev)
+    best = torch.empty(B, n_out, dtype=torch.float32, device=dev)
+    res = {"scores": best, "parent": ints[0], "token": ints[1], "done": ints[2]}
+    cap = 0
+    if history is not None:
+        if history.dim() != 2 or history.shape[0] != B * K:
+            raise ValueError("history must be [B * K, cap]")
+        cap = history.shape[1]
+        if history_out is None:
+            history_out = torch.empty(B * n_out, cap, dtype=i32, device=dev)
+        res["history"], res["n_history"] = history_out, torch.empty(B * n_out, dtype=i32, device=dev)
+    wsz = _size("spider_beam_select_workspace_size", B, K, n_out, V)
+    workspace, wptr = _scratch(workspace, wsz, dev)
+    _on(dev, lib().spider_beam_select, B, K, n_out, V, logits.data_ptr(), row, _dt(logits),
+        _need(scores, "scores", torch.float32, (B, K), dev), _need(done, "done", i32, (B, K), dev), eos, best.data_ptr(),
+        ints[0].data_ptr(), ints[1].data_ptr(), ints[2].data_ptr(), _need(history, "history", i32, (B * K, cap), dev), cap,
+        _need(n_history, "n_history", i32, (B * K,), dev), cap, _need(history_out, "history_out", i32, (B * n_out, cap), dev), cap,
+        _ptr(res.get("n_history")), wptr, wsz)
+    return res
 
 
 # ----------------------------------------------------------------- profiler

@@ -21,7 +21,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libspider.so")
 SOURCES = ["host.cpp", "score.hip", "select.hip", "gemm.hip", "attention.hip", "prefill.hip",
-           "controller.hip", "anchor.hip", "projector.hip", "tree_attention.hip", "cache.hip", "logits.hip"]
+           "controller.hip", "anchor.hip", "projector.hip", "tree_attention.hip", "cache.hip", "logits.hip",
+           "rope.hip", "paged_attention.hip", "pages.hip", "beam.hip"]
 ARCH = "gfx950"
 
 

@@ -84,31 +84,36 @@ struct AttnTile<uint16_t, DH> {
   __device__ static __forceinline__ void load_k(K& k, const uint16_t* base, int64_t stride, int j0, int n, int lane,
                                                 int dh) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      const uint16_t* row = base + (int64_t)min(j0 + 16 * t + (lane & 15), n - 1) * stride;
+    for (int t = 0; t < KT; ++t)
+      load_k_row<FULL>(k, t, base + (int64_t)min(j0 + 16 * t + (lane & 15), n - 1) * stride, lane >> 4, dh);
+  }
+  // key 16t + lane % 16, whose channels start at row
+  template <bool FULL>
+  __device__ static __forceinline__ void load_k_row(K& k, int t, const uint16_t* row, int g, int dh) {
 #pragma unroll
-      for (int i = 0; i < NK; ++i) k.f[t][i] = chunk<FULL>(row, 32 * i + 8 * (lane >> 4), dh);
-    }
+    for (int i = 0; i < NK; ++i) k.f[t][i] = chunk<FULL>(row, 32 * i + 8 * g, dh);
   }
   template <bool FULL>
   __device__ static __forceinline__ void load_v(V& v, const uint16_t* base, int64_t stride, int j0, int n, int lane,
                                                 int dh) {
     const int m = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint16_t* row = base + (int64_t)min(j0 + value_key(e, g), n - 1) * stride;
-      if constexpr (DH == 64) {
-        uint2 x = make_uint2(0, 0);
-        if (FULL || 4 * m < dh) x = *reinterpret_cast<const uint2*>(row + 4 * m);
-        v.w[e][0] = x.x;
-        v.w[e][1] = x.y;
-      } else {
+    for (int e = 0; e < 8; ++e) load_v_row<FULL>(v, e, base + (int64_t)min(j0 + value_key(e, g), n - 1) * stride, m, dh);
+  }
+  // value e of the lane, whose channels start at row
+  template <bool FULL>
+  __device__ static __forceinline__ void load_v_row(V& v, int e, const uint16_t* row, int m, int dh) {
+    if constexpr (DH == 64) {
+      uint2 x = make_uint2(0, 0);
+      if (FULL || 4 * m < dh) x = *reinterpret_cast<const uint2*>(row + 4 * m);
+      v.w[e][0] = x.x;
+      v.w[e][1] = x.y;
+    } else {
 #pragma unroll
-        for (int q = 0; q < DH / 128; ++q) {
-          const u32x4 x = __builtin_bit_cast(u32x4, chunk<FULL>(row, 128 * q + 8 * m, dh));
+      for (int q = 0; q < DH / 128; ++q) {
+        const u32x4 x = __builtin_bit_cast(u32x4, chunk<FULL>(row, 128 * q + 8 * m, dh));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v.w[e][4 * q + i] = x[i];
-        }
+        for (int i = 0; i < 4; ++i) v.w[e][4 * q + i] = x[i];
       }
     }
   }
@@ -224,19 +229,23 @@ struct AttnTile<float, DH> {
   template <bool FULL>
   __device__ static __forceinline__ void load_k(K& k, const float* base, int64_t stride, int j0, int n, int lane,
                                                 int dh) {
-    const float* row = base + (int64_t)min(j0 + (lane & 15), n - 1) * stride;
+    load_k_row<FULL>(k, 0, base + (int64_t)min(j0 + (lane & 15), n - 1) * stride, lane >> 4, dh);
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_k_row(K& k, int, const float* row, int g, int dh) {
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k.f[i] = chunk<FULL>(row, 16 * i + 4 * (lane >> 4), dh);
+    for (int i = 0; i < NK; ++i) k.f[i] = chunk<FULL>(row, 16 * i + 4 * g, dh);
   }
   template <bool FULL>
   __device__ static __forceinline__ void load_v(V& v, const float* base, int64_t stride, int j0, int n, int lane,
                                                 int dh) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float* row = base + (int64_t)min(j0 + value_key(e, lane >> 4), n - 1) * stride;
+    for (int e = 0; e < 4; ++e) load_v_row<FULL>(v, e, base + (int64_t)min(j0 + value_key(e, lane >> 4), n - 1) * stride, lane & 15, dh);
+  }
+  template <bool FULL>
+  __device__ static __forceinline__ void load_v_row(V& v, int e, const float* row, int m, int dh) {
 #pragma unroll
-      for (int q = 0; q < DH / 64; ++q) v.f[e][q] = chunk<FULL>(row, 64 * q + 4 * (lane & 15), dh);
-    }
+    for (int q = 0; q < DH / 64; ++q) v.f[e][q] = chunk<FULL>(row, 64 * q + 4 * m, dh);
   }
   __device__ static __forceinline__ void scores(floatx4* s, const K& k, const Q& q) {
     s[0] = floatx4{};

@@ -1,0 +1,376 @@
+// Beam search's choice over beams and vocabulary (spider_beam_select).
+//
+//   lse_k = log sum_v e^(x_kv),  cand(k, v) = score_k + (x_kv - lse_k)
+// The n_out best (beam, token) of a sample; a finished beam stands for itself at the end token.
+//
+// Within a beam the order is that of its logits, so one pass over them keeps the n_out best of
+// every piece of 8192 together with the piece's sum of exponentials (beam_scan_kernel, bound by
+// reading the logits); a block per sample joins the pieces (beam_join_kernel), and the token
+// histories follow their beams (beam_history_kernel).  Sums are held in fp64, and so are the
+// candidates: two of them that differ by less than fp32 resolves at -30 still come in order.
+#include <algorithm>
+#include <cmath>
+
+#include "kernels.h"
+
+namespace spider {
+namespace {
+
+constexpr int kMaxBeams = 64;
+constexpr int kBeamPiece = 8192, kBeamMaxV = 64 * kBeamPiece;  // a lane of the join per piece
+constexpr int kCand = 512;                                       // candidates of a piece that are ranked at once
+
+struct BeamArgs {
+  const void* logits;
+  const float* scores;
+  const int32_t* done;
+  float* scores_out;
+  int32_t* parent;
+  int32_t* token;
+  int32_t* done_out;
+  double* sums;     // [B*K][pieces] sum of e^(x - top)
+  float* tops;      // [B*K][pieces] an integer near the largest logit, or +-inf
+  uint64_t* lists;  // [B*K][pieces][M] best logits in order, see beam_key
+  const int32_t* history;
+  const int32_t* n_history;
+  int32_t* history_out;
+  int32_t* n_history_out;
+  int64_t stride, h_stride, ho_stride;
+  int B, K, M, V, eos, pieces, cap;
+};
+
+// Larger is better: the logit, then the lower token.  0: no candidate (-inf, NaN).
+__device__ __forceinline__ uint64_t beam_key(float x, int v) {
+  return x > -INFINITY ? ((uint64_t)float_order_key(x) << 32) | (0xFFFFFFFFu - (uint32_t)v) : 0ull;
+}
+__device__ __forceinline__ float beam_logit(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float((u & 0x80000000u) ? u & 0x7FFFFFFFu : ~u);
+}
+__device__ __forceinline__ int beam_token(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
+
+// The largest key of a wave, in every lane.
+__device__ __forceinline__ uint64_t wave_best(uint64_t key) {
+  const int hi = (int)((uint32_t)(key >> 32) ^ 0x80000000u), top = wave_max_int(hi);
+  const int lo = hi == top ? (int)((uint32_t)key ^ 0x80000000u) : (int)0x80000000;
+  return ((uint64_t)((uint32_t)top ^ 0x80000000u) << 32) | ((uint32_t)wave_max_int(lo) ^ 0x80000000u);
+}
+
+// e^d, d <= 1/2: the product with log2 e in two parts, so that what is left of an error is that
+// of the exponential instruction (1 unit in the last place) and no multiple of |d|.
+__device__ __forceinline__ float exp_accurate(float d) {
+  const float t = d * 1.44269504088896340736f;
+  const float r = fmaf(d, 1.44269504088896340736f, -t) + d * 1.92596299112661746887e-8f;
+  const float e = __builtin_amdgcn_exp2f(t);
+  return d > -200.f ? fmaf(e, r * 0.69314718055994530942f, e) : 0.f;
+}
+
+// Whether beam (row) takes part: a finite score and not finished.
+__device__ __forceinline__ bool beam_open(const BeamArgs& a, int row) { return !(a.done && a.done[row]) && fabsf(a.scores[row]) < INFINITY; }
+
+// A block per piece of a row.  Every thread holds 32 logits.  A bound below the M-th largest of
+// the piece: in each wave the M-th largest of its lanes' maxima, to 16 bits, found bit by bit with
+// ballots; the largest of the waves' bounds.  What reaches it (about 4 M logits) is ranked.
+template <typename LT, int VEC>
+__global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
+  constexpr int PER = kBeamPiece / 256;
+  __shared__ uint64_t cand[kCand];
+  __shared__ double sums[4];
+  __shared__ float tops[4];
+  __shared__ uint32_t bounds[4];
+  __shared__ int n_cand;
+  __shared__ uint64_t best[4];
+  const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (!beam_open(a, row)) return;
+  const int v0 = blockIdx.x * kBeamPiece, n = min(kBeamPiece, a.V - v0);
+  const LT* x0 = reinterpret_cast<const LT*>(a.logits) + row * a.stride + v0;
+  if (tid == 0) n_cand = 0;
+  float x[PER];
+  // token of value i of the thread
+  auto at = [&](int i) { return (i / VEC * 256 + tid) * VEC + i % VEC; };
+#pragma unroll
+  for (int u = 0; u < PER / VEC; ++u) {
+    const int i = (u * 256 + tid) * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[u * VEC + e] = -INFINITY;
+    if (i < n) {  // VEC > 1: rows are whole pieces of VEC
+      struct alignas(sizeof(LT) * VEC) Pack {
+        LT y[VEC];
+      };
+      const Pack p = *reinterpret_cast<const Pack*>(x0 + i);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float y;
+        if constexpr (sizeof(LT) == 2) y = bf16_bits_to_f32(p.y[e]);
+        else y = p.y[e];
+        x[u * VEC + e] = y != y ? -INFINITY : y;
+      }
+    }
+  }
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mx = fmaxf(mx, x[i]);
+  const uint32_t key16 = float_order_key(mx) >> 16;
+  uint32_t bound = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t t = bound | (1u << bit);
+    if (__popcll(__ballot(key16 >= t)) >= a.M) bound = t;
+  }
+  const float wm = wave_max(mx);
+  if (lane == 0) {
+    tops[wave] = wm;
+    bounds[wave] = bound;
+  }
+  __syncthreads();
+  // an integer: the differences of the logits that count are then exact
+  const float top = rintf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+  bound = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3]));
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    sum += (double)exp_accurate(x[i] - top);
+    const bool in = (float_order_key(x[i]) >> 16) >= bound && x[i] > -INFINITY;
+    if (__any(in)) {
+      const uint64_t mask = __ballot(in);
+      int base = 0;
+      if (lane == 0) base = atomicAdd(&n_cand, (int)__popcll(mask));
+      base = __builtin_amdgcn_readfirstlane(base) + (int)__popcll(mask & ((1ull << lane) - 1ull));
+      if (in && base < kCand) cand[base] = beam_key(x[i], v0 + at(i));
+    }
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  const int64_t piece = (int64_t)row * a.pieces + blockIdx.x;
+  uint64_t* list = a.lists + piece * a.M;
+  if (tid == 0) {
+    a.sums[piece] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    a.tops[piece] = top;
+  }
+  const int m = n_cand;
+  if (m <= kCand) {
+    // the rank of a candidate is the number of better ones (keys differ, so their order in the
+    // list does not matter)
+    for (int i = tid; i < m; i += 256) {
+      const uint64_t key = cand[i];
+      int rank = 0;
+      for (int j = 0; j < m; ++j) rank += cand[j] > key;
+      if (rank < a.M) list[rank] = key;
+    }
+    for (int i = m + tid; i < a.M; i += 256) list[i] = 0;
+    return;
+  }
+  // more equal logits than that at the bound: the best ones, one after the other
+  uint64_t limit = ~0ull;
+  for (int r = 0; r < a.M; ++r) {
+    uint64_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint64_t key = beam_key(x[i], v0 + at(i));
+      if (key < limit && key > mine) mine = key;
+    }
+    mine = wave_best(mine);
+    if (lane == 0) best[wave] = mine;
+    __syncthreads();
+    limit = max(max(best[0], best[1]), max(best[2], best[3]));
+    if (tid == 0) list[r] = limit;
+    __syncthreads();
+  }
+}
+
+// A block per sample: a wave per beam joins its pieces' lists, then every entry of the beams'
+// lists finds its rank by a binary search in each of them.
+constexpr int kStage = 512;  // list entries of a wave in LDS
+__global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
+  extern __shared__ double value[];  // [K][M]
+  int* token = reinterpret_cast<int*>(value + a.K * a.M);
+  __shared__ uint64_t stage[16][kStage];
+  __shared__ int counts[kMaxBeams];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int k = wave; k < a.K; k += 16) {
+    const int row = b * a.K + k;
+    const float score = a.scores[row];
+    int count = 0;
+    if (beam_open(a, row)) {
+      const int64_t piece = (int64_t)row * a.pieces;
+      const uint64_t* lists = a.lists + piece * a.M;
+      if (a.pieces * a.M <= kStage) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int i = lane; i < a.pieces * a.M; i += 64) stage[wave][i] = lists[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        lists = stage[wave];
+      }
+      const float top = lane < a.pieces ? a.tops[piece + lane] : -INFINITY, all = wave_max(top);
+      double sum = top == -INFINITY ? 0.0 : a.sums[piece + lane] * exp((double)top - (double)all);
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+      if (fabsf(all) < INFINITY) {
+        const double lse = (double)all + log(sum);
+        int next = 0;
+        uint64_t head = lane < a.pieces ? lists[lane * a.M] : 0ull;
+        while (count < a.M) {
+          const uint64_t key = wave_best(head);
+          if (key == 0) break;
+          if (head == key) {
+            ++next;
+            head = next < a.M ? lists[lane * a.M + next] : 0ull;
+            value[k * a.M + count] = (double)score + ((double)beam_logit(key) - lse);
+            token[k * a.M + count] = beam_token(key);
+          }
+          ++count;
+        }
+      }
+    } else if (fabsf(score) < INFINITY) {
+      count = 1;
+      if (lane == 0) {
+        value[k * a.M] = score;
+        token[k * a.M] = a.eos;
+      }
+    }
+    if (lane == 0) counts[k] = count;
+  }
+  __syncthreads();
+  int total = 0;
+  for (int k = 0; k < a.K; ++k) total += counts[k];
+  for (int i = tid; i < a.K * a.M; i += 1024) {
+    const int k = i / a.M, j = i - k * a.M;
+    if (j >= counts[k]) continue;
+    const double x = value[i];
+    int rank = j;
+    for (int u = 0; u < a.K; ++u) {
+      if (u == k) continue;
+      int lo = 0, hi = counts[u];  // entries of beam u that come first
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        const double y = value[u * a.M + mid];
+        if (y > x || (y == x && u < k)) lo = mid + 1;
+        else hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank >= a.M) continue;
+    const int to = b * a.M + rank;
+    a.scores_out[to] = (float)x;
+    a.parent[to] = b * a.K + k;
+    a.token[to] = token[i];
+    a.done_out[to] = (a.done && a.done[b * a.K + k]) || (a.eos >= 0 && token[i] == a.eos) ? 1 : 0;
+  }
+  for (int r = total + tid; r < a.M; r += 1024) {
+    const int to = b * a.M + r;
+    a.scores_out[to] = -INFINITY;
+    a.parent[to] = -1;
+    a.token[to] = -1;
+    a.done_out[to] = 1;
+  }
+}
+
+// A block row per new beam: its parent's history, then its token.
+__global__ void __launch_bounds__(256) beam_history_kernel(BeamArgs a) {
+  const int row = blockIdx.y, parent = a.parent[row];
+  const int n = parent < 0 ? 0 : min(max(a.n_history[parent], 0), a.cap);
+  const int more = parent >= 0 && !(a.done && a.done[parent]) && n < a.cap ? 1 : 0;
+  const int i0 = blockIdx.x * 1024 + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int i = i0 + 256 * u;
+    if (i < n) a.history_out[row * a.ho_stride + i] = a.history[parent * a.h_stride + i];
+    else if (i < n + more) a.history_out[row * a.ho_stride + i] = a.token[row];
+  }
+  if (i0 == 0) a.n_history_out[row] = n + more;
+}
+
+size_t beam_layout(int B, int K, int M, int V, char* at, BeamArgs* a) {
+  const size_t n = (size_t)B * K * ceil_div(V, kBeamPiece);
+  const size_t lists = align_up(n * M * sizeof(uint64_t), 256), sums = align_up(n * sizeof(double), 256);
+  if (a) {
+    a->lists = reinterpret_cast<uint64_t*>(at);
+    a->sums = reinterpret_cast<double*>(at + lists);
+    a->tops = reinterpret_cast<float*>(at + lists + sums);
+  }
+  return lists + sums + align_up(n * sizeof(float), 256);
+}
+
+bool beam_shape_ok(int B, int K, int M, int V) {
+  return B >= 1 && K >= 1 && M >= 1 && V >= 1 && K <= kMaxBeams && M <= kMaxBeams && V <= kBeamMaxV && (int64_t)B * K <= 65535 && (int64_t)B * M <= 65535;
+}
+
+template <typename LT, int VEC>
+void launch_beam_scan(const BeamArgs& a, hipStream_t st) {
+  beam_scan_kernel<LT, VEC><<<dim3((unsigned)a.pieces, (unsigned)(a.B * a.K)), 256, 0, st>>>(a);
+}
+
+}  // namespace
+}  // namespace spider
+
+using namespace spider;
+
+extern "C" size_t spider_beam_select_workspace_size(int B, int K, int n_out, int V) {
+  return beam_shape_ok(B, K, n_out, V) ? beam_layout(B, K, n_out, V, nullptr, nullptr) : 0;
+}
+
+extern "C" spider_status spider_beam_select(int B, int K, int n_out, int V, const void* logits, int64_t logits_stride, spider_dtype dtype,
+                                            const float* scores, const int32_t* done, int eos, float* scores_out, int32_t* parent_out,
+                                            int32_t* token_out, int32_t* done_out, const int32_t* history, int64_t history_stride,
+                                            const int32_t* n_history, int history_cap, int32_t* history_out, int64_t history_out_stride,
+                                            int32_t* n_history_out, void* workspace, size_t workspace_bytes, spider_stream stream) {
+  clear_error();
+  SPIDER_REQUIRE(logits && scores && scores_out && parent_out && token_out && done_out, SPIDER_ERR_INVALID_ARG, "spider_beam_select: null pointer");
+  SPIDER_REQUIRE(dtype == SPIDER_BF16 || dtype == SPIDER_F32, SPIDER_ERR_INVALID_ARG, "spider_beam_select: bad dtype");
+  SPIDER_REQUIRE(B >= 1 && K >= 1 && n_out >= 1 && V >= 1, SPIDER_ERR_INVALID_ARG, "spider_beam_select: sizes must be positive");
+  SPIDER_REQUIRE(beam_shape_ok(B, K, n_out, V), SPIDER_ERR_UNSUPPORTED,
+                 "spider_beam_select: K and n_out at most %d, V at most %d, B * K and B * n_out at most 65535", kMaxBeams, kBeamMaxV);
+  SPIDER_REQUIRE(logits_stride >= V, SPIDER_ERR_SHAPE, "spider_beam_select: rows of %d logits at a stride of %lld", V, (long long)logits_stride);
+  SPIDER_REQUIRE(eos >= -1 && eos < V && (!done || eos >= 0), SPIDER_ERR_INVALID_ARG, "spider_beam_select: eos must be a token (or -1, without finished beams)");
+  SPIDER_REQUIRE(reinterpret_cast<uintptr_t>(logits) % (dtype == SPIDER_BF16 ? 2 : 4) == 0, SPIDER_ERR_INVALID_ARG,
+                 "spider_beam_select: logits must be aligned to their type");
+  const bool any = history || n_history || history_out || n_history_out;
+  SPIDER_REQUIRE(!any || (history && n_history && history_out && n_history_out && history_cap >= 1), SPIDER_ERR_INVALID_ARG,
+                 "spider_beam_select: history, n_history, history_out and n_history_out go together, with a capacity");
+  SPIDER_REQUIRE(!any || (history_cap <= (1 << 24) && (B * K == 1 || history_stride >= history_cap) && (B * n_out == 1 || history_out_stride >= history_cap)),
+                 SPIDER_ERR_SHAPE, "spider_beam_select: history strides of at least the capacity, which is at most 2^24");
+  // (every row of a sample reads what another one's block would write)
+  const auto apart = [](const void* p, size_t n, const void* q, size_t m) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+    return !p || !q || x + n <= y || y + m <= x;
+  };
+  const size_t in = (size_t)B * K * 4, out = (size_t)B * n_out * 4;
+  for (const void* p : {(const void*)scores_out, (const void*)parent_out, (const void*)token_out, (const void*)done_out, (const void*)n_history_out})
+    SPIDER_REQUIRE(apart(p, out, scores, in) && apart(p, out, done, in) && apart(p, out, n_history, in), SPIDER_ERR_INVALID_ARG,
+                   "spider_beam_select: outputs must not overlap inputs");
+  const size_t h_in = any ? ((size_t)(B * K - 1) * (B * K == 1 ? 0 : history_stride) + history_cap) * 4 : 0;
+  const size_t h_out = any ? ((size_t)(B * n_out - 1) * (B * n_out == 1 ? 0 : history_out_stride) + history_cap) * 4 : 0;
+  SPIDER_REQUIRE(apart(history_out, h_out, history, h_in), SPIDER_ERR_INVALID_ARG, "spider_beam_select: outputs must not overlap inputs");
+  const size_t need = beam_layout(B, K, n_out, V, nullptr, nullptr);
+  SPIDER_REQUIRE(workspace && workspace_bytes >= need, SPIDER_ERR_WORKSPACE, "spider_beam_select: workspace of %zu bytes needed, %zu given", need,
+                 workspace ? workspace_bytes : 0);
+  SPIDER_REQUIRE(reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG, "spider_beam_select: workspace must be 256-byte aligned");
+  BeamArgs a{};
+  beam_layout(B, K, n_out, V, reinterpret_cast<char*>(workspace), &a);
+  a.logits = logits, a.scores = scores, a.done = done;
+  a.scores_out = scores_out, a.parent = parent_out, a.token = token_out, a.done_out = done_out;
+  a.history = history, a.n_history = n_history, a.history_out = history_out, a.n_history_out = n_history_out;
+  a.stride = logits_stride, a.h_stride = history_stride, a.ho_stride = history_out_stride;
+  a.B = B, a.K = K, a.M = n_out, a.V = V, a.eos = eos, a.pieces = ceil_div(V, kBeamPiece), a.cap = history_cap;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  ProfScope ps(KC_BEAM_SELECT, st);
+  // four logits at a time where every row starts on their boundary and has a multiple of 4
+  const uintptr_t four = dtype == SPIDER_BF16 ? 8 : 16;
+  const bool vec = V % 4 == 0 && (B * K == 1 || logits_stride % 4 == 0) && reinterpret_cast<uintptr_t>(logits) % four == 0;
+  if (dtype == SPIDER_BF16) {
+    if (vec) launch_beam_scan<uint16_t, 4>(a, st);
+    else launch_beam_scan<uint16_t, 1>(a, st);
+  } else {
+    if (vec) launch_beam_scan<float, 4>(a, st);
+    else launch_beam_scan<float, 1>(a, st);
+  }
+  SPIDER_LAUNCHED("beam_scan");
+  beam_join_kernel<<<(unsigned)B, 1024, (unsigned)(K * n_out * (sizeof(double) + sizeof(int))), st>>>(a);
+  SPIDER_LAUNCHED("beam_join");
+  if (any) {
+    beam_history_kernel<<<dim3((unsigned)ceil_div(history_cap, 1024), (unsigned)(B * n_out)), 256, 0, st>>>(a);
+    SPIDER_LAUNCHED("beam_history");
+  }
+  return SPIDER_OK;
+}

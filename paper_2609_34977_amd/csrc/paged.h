@@ -1,0 +1,83 @@
+// What the operators over a paged cache share: the sequences of a batch, their rows and pages.
+#pragma once
+
+#include "common.h"
+
+namespace spider {
+
+constexpr int kPagedMaxB = 65535;
+constexpr int kPagedMaxDh = 256;
+
+// Device view of a spider_paged_cache and the N packed rows of its new tokens; strides in elements.
+struct PagedArgs {
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* cu;
+  int64_t table_stride;
+  int64_t sp, ss, sh;  // page, slot, head
+  int B, N, n_pages, shift, max_pages;
+};
+
+// Rows start .. start + rows - 1 are the new tokens of a sequence of len slots: row start + t has
+// position len - rows + t.  Whatever the arrays hold, rows lie in [0, N) and slots in the table.
+struct PagedSeq {
+  int start, rows, len;
+};
+__device__ __forceinline__ int paged_start(const PagedArgs& a, int b) { return min(max(a.cu[b], 0), a.N); }
+__device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& a, int b) {
+  const int start = paged_start(a, b), end = min(max(a.cu[b + 1], start), a.N);
+  return PagedSeq{start, end - start, min(max(a.lens[b], 0), a.max_pages << a.shift)};
+}
+
+// The last i in [0, n) with f(i) <= x for an ascending f, or -1, by all 64 lanes of a wave: each
+// round looks at 64 places at once (two loads one after the other for up to 4096 sequences).
+template <typename F>
+__device__ __forceinline__ int last_at_most(int n, int x, F&& f) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, count = n;
+  while (true) {
+    const int step = (count + 63) / 64, i = lo + lane * step;
+    const int hits = __popcll(__ballot(lane * step < count && f(min(i, n - 1)) <= x));
+    if (hits == 0) return lo - 1;
+    if (step == 1) return lo + hits - 1;
+    count = min(step, count - (hits - 1) * step);
+    lo += (hits - 1) * step;
+  }
+}
+
+// The page that holds slots i * page_size .. of sequence b, or -1 where there is none.
+__device__ __forceinline__ int paged_page(const PagedArgs& a, int b, int i) {
+  const int page = a.table[b * a.table_stride + i];
+  return (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+}
+
+// Checks a cache descriptor for calls named `who`; fills the device view (N rows).  `writes`: the
+// call stores into the pages, so their slots must not share memory.
+inline spider_status paged_check(const char* who, const spider_paged_cache* c, int N, int Hkv, int dh,
+                                 spider_dtype dtype, bool writes, PagedArgs* out) {
+  SPIDER_REQUIRE(c && c->k && c->v && c->table && c->lens && c->cu, SPIDER_ERR_INVALID_ARG, "%s: null pointer in the cache", who);
+  SPIDER_REQUIRE(c->B >= 1 && c->n_pages >= 1 && c->max_pages >= 1, SPIDER_ERR_INVALID_ARG, "%s: B, n_pages and max_pages must be positive", who);
+  SPIDER_REQUIRE(c->page_size >= 8 && c->page_size <= 4096 && (c->page_size & (c->page_size - 1)) == 0, SPIDER_ERR_UNSUPPORTED,
+                 "%s: page_size must be a power of two from 8 to 4096, got %d", who, c->page_size);
+  SPIDER_REQUIRE(c->B <= kPagedMaxB && (int64_t)c->max_pages * c->page_size <= (1 << 30), SPIDER_ERR_UNSUPPORTED,
+                 "%s: B at most %d, max_pages * page_size at most 2^30", who, kPagedMaxB);
+  SPIDER_REQUIRE(c->B == 1 || c->table_stride >= c->max_pages, SPIDER_ERR_SHAPE, "%s: table rows of %d pages at a stride of %lld", who,
+                 c->max_pages, (long long)c->table_stride);
+  const int64_t per16 = dtype == SPIDER_BF16 ? 8 : 4;
+  SPIDER_REQUIRE(dh >= 1 && dh <= kPagedMaxDh && dh % per16 == 0, SPIDER_ERR_UNSUPPORTED,
+                 "%s: dh must be a multiple of 16 bytes and at most %d", who, kPagedMaxDh);
+  // the stride of a dimension of size 1 means nothing
+  const int64_t sp = c->n_pages == 1 ? 0 : c->stride_page, ss = c->stride_slot, sh = Hkv == 1 ? 0 : c->stride_head;
+  SPIDER_REQUIRE(sp >= 0 && ss >= 0 && sh >= 0 && sp % per16 == 0 && ss % per16 == 0 && sh % per16 == 0, SPIDER_ERR_INVALID_ARG,
+                 "%s: the cache's strides must be multiples of 16 bytes", who);
+  SPIDER_REQUIRE(!writes || ((c->n_pages == 1 || sp > 0) && ss > 0 && (Hkv == 1 || sh > 0)), SPIDER_ERR_INVALID_ARG,
+                 "%s: the cache's slots must not share memory (a stride of 0)", who);
+  SPIDER_REQUIRE((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16 == 0, SPIDER_ERR_INVALID_ARG,
+                 "%s: the cache must be 16-byte aligned", who);
+  int shift = 0;
+  while ((1 << shift) < c->page_size) ++shift;
+  *out = PagedArgs{c->table, c->lens, c->cu, c->B == 1 ? 0 : c->table_stride, sp, ss, sh, c->B, N, c->n_pages, shift, c->max_pages};
+  return SPIDER_OK;
+}
+
+}  // namespace spider

@@ -1,0 +1,249 @@
+// The next step's page tables of a paged cache (spider_pages_fork): sequences that one, several or
+// no new ones continue, references counted, a shared last page copied before its readers write
+// into it, pages taken for the new slots.
+//
+// All of it is integers, with one result whatever the order of the atomics; bound by latency
+// except for the copies, which run at the rate of a copy.
+#include <algorithm>
+
+#include "kernels.h"
+#include "paged.h"
+
+namespace spider {
+namespace {
+
+constexpr int kForkMaxB = 4096;
+
+struct ForkArgs {
+  const int32_t* table_in;
+  const int32_t* lens_in;
+  const int32_t* ref_in;
+  const int32_t* parent;
+  const int32_t* n_new;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* ref_out;
+  int32_t* missing;
+  int32_t* free_list;  // [n_pages]
+  int4* copies;        // [B_out] (page, its copy or -1, slots, 0)
+  int B_in, B_out, n_pages, shift, max_pages;
+};
+
+__device__ __forceinline__ int fork_len(const ForkArgs& a, int b) { return min(max(a.lens_in[b], 0), a.max_pages << a.shift); }
+__device__ __forceinline__ int fork_pages(const ForkArgs& a, int len) { return (len + (1 << a.shift) - 1) >> a.shift; }
+// The old sequence that new sequence b continues, or -1, and its length.
+__device__ __forceinline__ int2 fork_from(const ForkArgs& a, int b) {
+  const int p = a.parent[b];
+  return (uint32_t)p < (uint32_t)a.B_in ? make_int2(p, fork_len(a, p)) : make_int2(-1, 0);
+}
+__device__ __forceinline__ int fork_load(int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__global__ void __launch_bounds__(256) fork_refs_kernel(ForkArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < a.n_pages) a.ref_out[i] = a.ref_in[i];
+}
+
+// A block per 256 pages of an old sequence, which gives its references up, or of a new one,
+// which takes its parent's.
+__global__ void __launch_bounds__(256) fork_tables_kernel(ForkArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.max_pages) return;
+  const bool old = (int)blockIdx.y < a.B_in;
+  const int b = old ? blockIdx.y : blockIdx.y - a.B_in;
+  const int2 from = old ? make_int2(b, fork_len(a, b)) : fork_from(a, b);
+  const int page = i < fork_pages(a, from.y) ? a.table_in[(int64_t)from.x * a.max_pages + i] : -1;
+  const bool held = (uint32_t)page < (uint32_t)a.n_pages;
+  if (!old) a.table_out[(int64_t)b * a.max_pages + i] = held ? page : -1;
+  if (held) atomicAdd(a.ref_out + page, old ? -1 : 1);
+}
+
+// Exclusive prefix sum over the block of 1024 and its total.
+__device__ __forceinline__ int2 block_prefix(int x, int* waves) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int y = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int z = __shfl_up(y, d);
+    y += lane >= d ? z : 0;
+  }
+  if (lane == 63) waves[wave] = y;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    before += w < wave ? waves[w] : 0;
+    total += waves[w];
+  }
+  __syncthreads();
+  return make_int2(before + y - x, total);
+}
+
+// One block: who copies, how many pages each sequence takes, the lowest free pages, and who
+// gets which.
+__global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
+  __shared__ int last[kForkMaxB], start[kForkMaxB + 1];  // the page a sequence writes into; its place among the pages taken
+  __shared__ int waves[16];
+  const int tid = threadIdx.x, P = 1 << a.shift;
+  for (int b = tid; b < a.B_out; b += 1024) {
+    const int2 from = fork_from(a, b);
+    const int grown = from.x < 0 ? 0 : (int)min((int64_t)from.y + (a.n_new ? max(a.n_new[b], 0) : 0), (int64_t)a.max_pages << a.shift);
+    a.lens_out[b] = grown;
+    last[b] = grown > from.y && from.y % P ? a.table_out[(int64_t)b * a.max_pages + (from.y >> a.shift)] : -1;
+  }
+  __syncthreads();
+  // The first writer of a page keeps it if nobody but the writers holds it.
+  int taken = 0;
+  uint32_t copies = 0;  // bit i: of sequence i * 1024 + tid
+  for (int b0 = 0, i = 0; b0 < a.B_out; b0 += 1024, ++i) {
+    const int b = b0 + tid;
+    int need = 0;
+    if (b < a.B_out) {
+      const int2 from = fork_from(a, b);
+      const int page = last[b];
+      if (page >= 0) {
+        int same = 0, before = 0;
+        for (int u = 0; u < a.B_out; ++u) {
+          same += last[u] == page;
+          before += last[u] == page && u < b;
+        }
+        if (before > 0 || fork_load(a.ref_out + page) > same) copies |= 1u << i;
+      }
+      need = fork_pages(a, a.lens_out[b]) - fork_pages(a, from.y) + ((copies >> i) & 1u);
+    }
+    const int2 at = block_prefix(need, waves);
+    if (b < a.B_out) start[b] = taken + at.x;
+    taken += at.y;
+  }
+  if (tid == 0) start[a.B_out] = taken;
+  for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i)
+    if ((copies >> i) & 1u) atomicSub(a.ref_out + last[b], 1);
+  __syncthreads();
+  int found = 0;
+  for (int p0 = 0; p0 < a.n_pages && found < taken; p0 += 1024) {
+    const int p = p0 + tid;
+    const bool open = p < a.n_pages && fork_load(a.ref_out + p) <= 0;
+    const int2 at = block_prefix(open, waves);
+    if (open && found + at.x < taken) a.free_list[found + at.x] = p;
+    found += at.y;
+  }
+  found = min(found, taken);
+  __syncthreads();
+  for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i) {
+    const int2 from = fork_from(a, b);
+    const int copy = (copies >> i) & 1u;
+    int4 c = make_int4(-1, -1, 0, 0);
+    for (int n = start[b]; n < start[b + 1]; ++n) {
+      const int page = n < found ? a.free_list[n] : -1, j = n - start[b];
+      const int at = copy && j == 0 ? from.y >> a.shift : fork_pages(a, from.y) + j - copy;
+      a.table_out[(int64_t)b * a.max_pages + at] = page;
+      if (page >= 0) a.ref_out[page] = 1;
+      if (copy && j == 0) c = make_int4(last[b], page, from.y % P, 0);
+    }
+    a.copies[b] = c;
+  }
+  if (tid == 0) a.missing[0] = taken - found;
+}
+
+struct ForkCopyArgs {
+  char* kv[2];
+  const int4* copies;
+  int64_t sl, sp, ss, sh;  // strides, bytes
+  int B, Hkv, nv, n_pieces;
+  int slots_inner;  // whether a head's slots lie closer together than a slot's heads
+};
+
+// A thread per 16-byte piece of a page, its key and its value.
+__global__ void __launch_bounds__(256) fork_copy_kernel(ForkCopyArgs a) {
+  const int l = blockIdx.y / a.B, b = blockIdx.y % a.B;
+  const int4 copy = a.copies[b];
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (copy.y < 0 || i >= copy.z * a.Hkv * a.nv) return;
+  const int c = i % a.nv, r = i / a.nv;
+  const int s = a.slots_inner ? r % copy.z : r / a.Hkv, h = a.slots_inner ? r / copy.z : r % a.Hkv;
+  const int64_t at = l * a.sl + s * a.ss + h * a.sh + 16 * c;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(a.kv[0] + at + copy.x * a.sp), v = *reinterpret_cast<const u32x4*>(a.kv[1] + at + copy.x * a.sp);
+  *reinterpret_cast<u32x4*>(a.kv[0] + at + copy.y * a.sp) = k;
+  *reinterpret_cast<u32x4*>(a.kv[1] + at + copy.y * a.sp) = v;
+}
+
+bool fork_shape_ok(int B_out, int n_pages) { return B_out >= 1 && B_out <= kForkMaxB && n_pages >= 1; }
+
+bool overlap(const void* p, size_t n, const void* q, size_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+  return x < y + m && y < x + n;
+}
+
+}  // namespace
+}  // namespace spider
+
+using namespace spider;
+
+extern "C" size_t spider_pages_fork_workspace_size(int B_out, int n_pages) {
+  if (!fork_shape_ok(B_out, n_pages)) return 0;
+  return align_up((size_t)B_out * sizeof(int4), 256) + align_up((size_t)n_pages * sizeof(int32_t), 256);
+}
+
+extern "C" spider_status spider_pages_fork(int L, int Hkv, int dh, spider_dtype dtype, void* k, void* v, const int64_t strides[4],
+                                           int n_pages, int page_size, int max_pages, int B_in, const int32_t* table_in,
+                                           const int32_t* lens_in, const int32_t* ref_in, int B_out, const int32_t* parent,
+                                           const int32_t* n_new, int32_t* table_out, int32_t* lens_out, int32_t* ref_out,
+                                           int32_t* missing_out, void* workspace, size_t workspace_bytes, spider_stream stream) {
+  clear_error();
+  SPIDER_REQUIRE(k && v && strides && table_in && lens_in && ref_in && parent && table_out && lens_out && ref_out && missing_out,
+                 SPIDER_ERR_INVALID_ARG, "spider_pages_fork: null pointer");
+  SPIDER_REQUIRE(dtype == SPIDER_BF16 || dtype == SPIDER_F32, SPIDER_ERR_INVALID_ARG, "spider_pages_fork: bad dtype");
+  SPIDER_REQUIRE(L >= 1 && Hkv >= 1 && dh >= 1 && n_pages >= 1 && max_pages >= 1 && B_in >= 1 && B_out >= 1, SPIDER_ERR_INVALID_ARG,
+                 "spider_pages_fork: sizes must be positive");
+  SPIDER_REQUIRE(B_in <= kForkMaxB && B_out <= kForkMaxB && (int64_t)L * B_out <= 65535, SPIDER_ERR_UNSUPPORTED,
+                 "spider_pages_fork: at most %d sequences, L * B_out at most 65535", kForkMaxB);
+  SPIDER_REQUIRE(page_size >= 8 && page_size <= 4096 && (page_size & (page_size - 1)) == 0, SPIDER_ERR_UNSUPPORTED,
+                 "spider_pages_fork: page_size must be a power of two from 8 to 4096, got %d", page_size);
+  SPIDER_REQUIRE((int64_t)max_pages * page_size <= (1 << 30), SPIDER_ERR_UNSUPPORTED, "spider_pages_fork: max_pages * page_size at most 2^30");
+  const int es = dtype == SPIDER_BF16 ? 2 : 4;
+  SPIDER_REQUIRE(dh * (int64_t)es % 16 == 0 && dh <= kPagedMaxDh && Hkv <= 65535 && (int64_t)page_size * Hkv * dh <= (1 << 30), SPIDER_ERR_UNSUPPORTED,
+                 "spider_pages_fork: dh must be a multiple of 16 bytes and at most %d, a page at most 2^30 elements", kPagedMaxDh);
+  SPIDER_REQUIRE((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % 16 == 0, SPIDER_ERR_INVALID_ARG,
+                 "spider_pages_fork: the caches must be 16-byte aligned");
+  const int n[4] = {L, n_pages, page_size, Hkv};
+  int64_t s[4];  // bytes; the stride of a dimension of size 1 means nothing
+  for (int i = 0; i < 4; ++i) {
+    s[i] = n[i] == 1 ? 0 : strides[i] * es;
+    SPIDER_REQUIRE(s[i] % 16 == 0, SPIDER_ERR_INVALID_ARG, "spider_pages_fork: strides must be multiples of 16 bytes");
+    SPIDER_REQUIRE(n[i] == 1 || s[i] > 0, SPIDER_ERR_INVALID_ARG, "spider_pages_fork: the cache's slots must not share memory (a stride of 0)");
+  }
+  const size_t need = spider_pages_fork_workspace_size(B_out, n_pages);
+  SPIDER_REQUIRE(workspace && workspace_bytes >= need, SPIDER_ERR_WORKSPACE, "spider_pages_fork: workspace of %zu bytes needed, %zu given", need,
+                 workspace ? workspace_bytes : 0);
+  SPIDER_REQUIRE(reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG, "spider_pages_fork: workspace must be 256-byte aligned");
+  // (blocks read old rows while others write new ones)
+  const void* in[5] = {table_in, lens_in, ref_in, parent, n_new};
+  const size_t in_n[5] = {(size_t)B_in * max_pages, (size_t)B_in, (size_t)n_pages, (size_t)B_out, n_new ? (size_t)B_out : 0};
+  const void* out[4] = {table_out, lens_out, ref_out, missing_out};
+  const size_t out_n[4] = {(size_t)B_out * max_pages, (size_t)B_out, (size_t)n_pages, 1};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < 5; ++i)
+      SPIDER_REQUIRE(!overlap(out[o], 4 * out_n[o], in[i], 4 * in_n[i]), SPIDER_ERR_INVALID_ARG, "spider_pages_fork: outputs must not overlap inputs");
+    for (int i = 0; i < o; ++i)
+      SPIDER_REQUIRE(!overlap(out[o], 4 * out_n[o], out[i], 4 * out_n[i]), SPIDER_ERR_INVALID_ARG, "spider_pages_fork: outputs must not overlap each other");
+  }
+  char* ws = reinterpret_cast<char*>(workspace);
+  ForkArgs a{table_in, lens_in, ref_in, parent, n_new, table_out, lens_out, ref_out, missing_out, nullptr, reinterpret_cast<int4*>(ws), B_in, B_out, n_pages, 0,
+             max_pages};
+  a.free_list = reinterpret_cast<int32_t*>(ws + align_up((size_t)B_out * sizeof(int4), 256));
+  while ((1 << a.shift) < page_size) ++a.shift;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  ProfScope ps(KC_PAGES_FORK, st);
+  fork_refs_kernel<<<(unsigned)((n_pages + 255LL) / 256), 256, 0, st>>>(a);
+  SPIDER_LAUNCHED("fork_refs");
+  fork_tables_kernel<<<dim3((unsigned)ceil_div(max_pages, 256), (unsigned)(B_in + B_out)), 256, 0, st>>>(a);
+  SPIDER_LAUNCHED("fork_tables");
+  fork_assign_kernel<<<1, 1024, 0, st>>>(a);
+  SPIDER_LAUNCHED("fork_assign");
+  if (n_new) {  // (a sequence that takes no new slots copies nothing)
+    ForkCopyArgs c{{reinterpret_cast<char*>(k), reinterpret_cast<char*>(v)}, a.copies, s[0], s[1], s[2], s[3], B_out, Hkv, dh * es / 16, page_size * Hkv * (dh * es / 16),
+                   Hkv > 1 && s[2] < s[3]};
+    fork_copy_kernel<<<dim3((unsigned)ceil_div(c.n_pieces, 256), (unsigned)(L * B_out)), 256, 0, st>>>(c);
+    SPIDER_LAUNCHED("fork_copy");
+  }
+  return SPIDER_OK;
+}

@@ -1,0 +1,260 @@
+// Rotary positions with several axes (spider_rope_axes, spider_rope_append): queries turned,
+// keys turned and stored with the values in the pages of their sequences.
+//
+//   a_i = pos[axis_i] freq_i,  (x_i, x_{i+half}) -> (x_i cos a_i - x_{i+half} sin a_i,
+//                                                    x_{i+half} cos a_i + x_i sin a_i)
+// Bound by the copy: every query, key and value is read once and written once, in 16-byte
+// pieces.  The angles are the only arithmetic of note, one per token and frequency: a block
+// turns all heads of a few tokens by the same angles, which it holds in LDS.
+#include <algorithm>
+#include <cmath>
+
+#include "kernels.h"
+#include "paged.h"
+
+namespace spider {
+namespace {
+
+constexpr int kMaxAxes = 8;
+constexpr int kTokens = 4;  // of a block, one per wave
+
+struct RopeAppendArgs {
+  PagedArgs p;  // table null: no pages, every row is turned
+  const int32_t* pos;
+  int64_t pos_stride;
+  const double* freq;
+  const uint8_t* axis;
+  const void* q;
+  void* q_out;
+  const void* k;
+  const void* v;
+  void* k_pages;
+  void* v_pages;
+  int64_t qs, qos, ks, vs;
+  int N, H, Hkv, dh, half, n_axes, tokens;
+};
+
+// cos and sin of an angle in double, rounded once.  The angle minus its n quarter turns (pi/2 in
+// two doubles) lies in [-pi/4, pi/4], where the Taylor polynomials to x^13 and x^12 are within
+// 4e-13.  (In fp32 the angle of position 10^6 itself would be off by 0.03.)
+__device__ __forceinline__ float2 cos_sin(double a) {
+  const double n = rint(a * 0.63661977236758134308);
+  const double x = fma(-n, 6.123233995736766036e-17, fma(-n, 1.5707963267948965580, a)), z = x * x;
+  double s = fma(z, 1.0 / 6227020800.0, -1.0 / 39916800.0);
+  s = fma(z, s, 1.0 / 362880.0);
+  s = fma(z, s, -1.0 / 5040.0);
+  s = fma(z, s, 1.0 / 120.0);
+  s = fma(z, s, -1.0 / 6.0);
+  s = fma(x * z, s, x);
+  double c = fma(z, 1.0 / 479001600.0, -1.0 / 3628800.0);
+  c = fma(z, c, 1.0 / 40320.0);
+  c = fma(z, c, -1.0 / 720.0);
+  c = fma(z, c, 1.0 / 24.0);
+  c = fma(z, c, -0.5);
+  c = fma(z, c, 1.0);
+  const int quarter = (int)((int64_t)n & 3);
+  const float fs = (float)((quarter & 1) ? c : s), fc = (float)((quarter & 1) ? s : c);
+  return make_float2(quarter == 1 || quarter == 2 ? -fc : fc, quarter >= 2 ? -fs : fs);
+}
+
+template <typename AT, int VEC>
+struct alignas(sizeof(AT) * VEC) Piece {
+  AT x[VEC];
+};
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(uint16_t x) { return bf16_bits_to_f32(x); }
+template <typename AT>
+__device__ __forceinline__ AT from_f32(float x) {
+  if constexpr (sizeof(AT) == 4) return x;
+  else return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+// VEC: channels of a thread's piece; it divides half, so that a piece and its partner half a
+// rotation on are aligned and turn by the same frequencies.
+template <typename AT, int VEC>
+__global__ void __launch_bounds__(256) rope_append_kernel(RopeAppendArgs a) {
+  __shared__ float cs[kTokens][kPagedMaxDh / 2], sn[kTokens][kPagedMaxDh / 2];
+  __shared__ int64_t slot[kTokens];  // where a token's key and value go, in elements; -1: nowhere
+  __shared__ int live[kTokens];
+  using P = Piece<AT, VEC>;
+  const int tid = threadIdx.x, row0 = blockIdx.x * a.tokens;
+  const int rows = min(a.tokens, a.N - row0);
+  for (int i = tid; i < rows * a.half; i += 256) {
+    const int t = i / a.half, f = i - t * a.half;
+    const int ax = min((int)a.axis[f], a.n_axes - 1);
+    const float2 y = cos_sin((double)a.pos[ax * a.pos_stride + row0 + t] * a.freq[f]);
+    cs[t][f] = y.x;
+    sn[t][f] = y.y;
+  }
+  if (tid / 64 < rows) {
+    const int t = tid / 64, row = row0 + t;
+    int64_t to = -1;
+    int on = 1;
+    if (a.p.table) {
+      const int b = last_at_most(a.p.B, row, [&](int i) { return paged_start(a.p, i); });
+      on = 0;
+      if (b >= 0) {
+        const PagedSeq s = paged_seq(a.p, b);
+        const int at = s.len - s.rows + row - s.start;
+        on = row - s.start < s.rows;
+        if (on && at >= 0) {
+          const int page = paged_page(a.p, b, at >> a.p.shift);
+          if (page >= 0) to = page * a.p.sp + (at & ((1 << a.p.shift) - 1)) * a.p.ss;
+        }
+      }
+    }
+    if ((tid & 63) == 0) {
+      slot[t] = to;
+      live[t] = on;
+    }
+  }
+  __syncthreads();
+  // (token, head) pairs side by side, pp threads each: pairs of pieces, then what is not turned
+  const int turned = a.half / VEC, pp = turned + (a.dh - 2 * a.half) / VEC, per = 256 / pp;
+  const int c = tid % pp, first = tid / pp;
+  const int h0 = a.q ? 0 : a.H, heads = (a.k ? a.H + a.Hkv : a.H) - h0;
+  if (first < per) {
+    for (int i = first; i < rows * heads; i += per) {
+      const int t = i / heads, h = h0 + i - t * heads;
+      const int64_t row = row0 + t;
+      const AT* src;
+      AT* dst;
+      if (h < a.H) {
+        if (!live[t]) continue;
+        src = reinterpret_cast<const AT*>(a.q) + row * a.qs + (int64_t)h * a.dh;
+        dst = reinterpret_cast<AT*>(a.q_out) + row * a.qos + (int64_t)h * a.dh;
+      } else {
+        if (slot[t] < 0) continue;
+        src = reinterpret_cast<const AT*>(a.k) + row * a.ks + (int64_t)(h - a.H) * a.dh;
+        dst = reinterpret_cast<AT*>(a.k_pages) + slot[t] + (h - a.H) * a.p.sh;
+      }
+      if (c < turned) {
+        const P x = *reinterpret_cast<const P*>(src + c * VEC), y = *reinterpret_cast<const P*>(src + a.half + c * VEC);
+        P u, w;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float2 z = rope_rotate(to_f32(x.x[e]), to_f32(y.x[e]), cs[t][c * VEC + e], sn[t][c * VEC + e]);
+          u.x[e] = from_f32<AT>(z.x);
+          w.x[e] = from_f32<AT>(z.y);
+        }
+        *reinterpret_cast<P*>(dst + c * VEC) = u;
+        *reinterpret_cast<P*>(dst + a.half + c * VEC) = w;
+      } else {
+        const int at = a.half + c * VEC;
+        *reinterpret_cast<P*>(dst + at) = *reinterpret_cast<const P*>(src + at);
+      }
+    }
+  }
+  if (a.v) {
+    constexpr int W = 16 / sizeof(AT);
+    const int nv = a.dh / W, each = 256 / nv, cv = tid % nv;
+    if (tid / nv < each) {
+      for (int i = tid / nv; i < rows * a.Hkv; i += each) {
+        const int t = i / a.Hkv, h = i - t * a.Hkv;
+        if (slot[t] < 0) continue;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(reinterpret_cast<const AT*>(a.v) + (int64_t)(row0 + t) * a.vs + (int64_t)h * a.dh + cv * W);
+        *reinterpret_cast<u32x4*>(reinterpret_cast<AT*>(a.v_pages) + slot[t] + h * a.p.sh + cv * W) = x;
+      }
+    }
+  }
+}
+
+template <typename AT, int VEC>
+void launch_rope_append(const RopeAppendArgs& a, hipStream_t st) {
+  rope_append_kernel<AT, VEC><<<(unsigned)ceil_div(a.N, a.tokens), 256, 0, st>>>(a);
+}
+
+}  // namespace
+}  // namespace spider
+
+using namespace spider;
+
+extern "C" spider_status spider_rope_axes(int rot, double theta, int n_axes, const int32_t* sections, int interleaved,
+                                          double* freq_out, uint8_t* axis_out) {
+  clear_error();
+  SPIDER_REQUIRE(sections && freq_out && axis_out, SPIDER_ERR_INVALID_ARG, "spider_rope_axes: null pointer");
+  SPIDER_REQUIRE(rot >= 2 && rot % 2 == 0 && n_axes >= 1 && theta > 0.0 && std::isfinite(theta) && (interleaved == 0 || interleaved == 1),
+                 SPIDER_ERR_INVALID_ARG, "spider_rope_axes: rot must be even and positive, theta positive, interleaved 0 or 1");
+  SPIDER_REQUIRE(rot <= kPagedMaxDh && n_axes <= kMaxAxes, SPIDER_ERR_UNSUPPORTED, "spider_rope_axes: rot at most %d, at most %d axes", kPagedMaxDh,
+                 kMaxAxes);
+  const int half = rot / 2;
+  int64_t total = 0;
+  for (int x = 0; x < n_axes; ++x) {
+    SPIDER_REQUIRE(sections[x] >= 0, SPIDER_ERR_INVALID_ARG, "spider_rope_axes: negative section");
+    total += sections[x];
+  }
+  SPIDER_REQUIRE(total == half, SPIDER_ERR_SHAPE, "spider_rope_axes: sections of %lld frequencies, %d wanted", (long long)total, half);
+  // in turn: frequency i is axis i % n_axes while that axis has any left, else of the first one
+  for (int x = 1; interleaved && x < n_axes; ++x)
+    SPIDER_REQUIRE(sections[x] == 0 || (int64_t)(sections[x] - 1) * n_axes + x < half, SPIDER_ERR_SHAPE,
+                   "spider_rope_axes: %d frequencies of axis %d do not fit in turn", sections[x], x);
+  for (int i = 0, x = 0, left = sections[0]; i < half; ++i) {
+    freq_out[i] = std::pow(theta, -2.0 * i / rot);
+    if (interleaved) {
+      const int y = i % n_axes;
+      axis_out[i] = (uint8_t)(y > 0 && i / n_axes < sections[y] ? y : 0);
+    } else {
+      while (left == 0) left = sections[++x];
+      axis_out[i] = (uint8_t)x;
+      --left;
+    }
+  }
+  return SPIDER_OK;
+}
+
+extern "C" spider_status spider_rope_append(int N, int H, int Hkv, int dh, int rot, int n_axes, const int32_t* pos,
+                                            int64_t pos_stride, const double* freq, const uint8_t* axis, const void* q,
+                                            int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k,
+                                            int64_t k_stride, const void* v, int64_t v_stride,
+                                            const spider_paged_cache* cache, spider_dtype dtype, spider_stream stream) {
+  clear_error();
+  SPIDER_REQUIRE(pos && freq && axis, SPIDER_ERR_INVALID_ARG, "spider_rope_append: null pointer");
+  SPIDER_REQUIRE((q != nullptr) == (q_out != nullptr) && (k != nullptr) == (v != nullptr) && (k != nullptr) == (cache != nullptr),
+                 SPIDER_ERR_INVALID_ARG, "spider_rope_append: q and q_out go together, and k, v and the cache");
+  SPIDER_REQUIRE(q || k, SPIDER_ERR_INVALID_ARG, "spider_rope_append: neither queries nor keys");
+  SPIDER_REQUIRE(dtype == SPIDER_BF16 || dtype == SPIDER_F32, SPIDER_ERR_INVALID_ARG, "spider_rope_append: bad dtype");
+  if (!q) H = 0;
+  if (!k) Hkv = 0;
+  SPIDER_REQUIRE(N >= 1 && dh >= 1 && (!q || H >= 1) && (!k || Hkv >= 1) && n_axes >= 1, SPIDER_ERR_INVALID_ARG,
+                 "spider_rope_append: sizes must be positive");
+  const int per16 = dtype == SPIDER_BF16 ? 8 : 4;
+  SPIDER_REQUIRE(dh <= kPagedMaxDh && dh % per16 == 0 && H <= 65535 && Hkv <= 65535 && n_axes <= kMaxAxes && N < (1 << 24), SPIDER_ERR_UNSUPPORTED,
+                 "spider_rope_append: dh a multiple of 16 bytes up to %d, H and Hkv <= 65535, n_axes <= %d, N below 2^24", kPagedMaxDh, kMaxAxes);
+  SPIDER_REQUIRE(rot >= 2 && rot % 2 == 0 && rot <= dh, SPIDER_ERR_SHAPE, "spider_rope_append: rot = %d of %d channels", rot, dh);
+  SPIDER_REQUIRE(n_axes == 1 || pos_stride >= N, SPIDER_ERR_SHAPE, "spider_rope_append: positions of %d rows at a stride of %lld", N,
+                 (long long)pos_stride);
+  if (N == 1) q_stride = q_out_stride = k_stride = v_stride = 0;
+  const auto row_ok = [&](const void* p, int64_t stride, int heads) {
+    return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % per16 == 0 && (N == 1 || stride >= (int64_t)heads * dh));
+  };
+  SPIDER_REQUIRE(row_ok(q, q_stride, H) && row_ok(q_out, q_out_stride, H) && row_ok(k, k_stride, Hkv) && row_ok(v, v_stride, Hkv), SPIDER_ERR_INVALID_ARG,
+                 "spider_rope_append: rows must be 16-byte aligned, their strides multiples of 16 bytes and at least a row");
+  SPIDER_REQUIRE(q != q_out || q_stride == q_out_stride, SPIDER_ERR_INVALID_ARG, "spider_rope_append: in place needs equal strides");
+  RopeAppendArgs a{};
+  if (cache) {
+    const spider_status s = paged_check("spider_rope_append", cache, N, Hkv, dh, dtype, true, &a.p);
+    if (s != SPIDER_OK) return s;
+    a.k_pages = cache->k;
+    a.v_pages = cache->v;
+  }
+  a.pos = pos;
+  a.pos_stride = n_axes == 1 ? 0 : pos_stride;
+  a.freq = freq;
+  a.axis = axis;
+  a.q = q, a.q_out = q_out, a.k = k, a.v = v;
+  a.qs = q_stride, a.qos = q_out_stride, a.ks = k_stride, a.vs = v_stride;
+  a.N = N, a.H = H, a.Hkv = Hkv, a.dh = dh, a.half = rot / 2, a.n_axes = n_axes;
+  a.tokens = N >= 1024 ? kTokens : 1;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  ProfScope ps(KC_ROPE_APPEND, st);
+  if (dtype == SPIDER_BF16) {
+    if (a.half % 8 == 0) launch_rope_append<uint16_t, 8>(a, st);
+    else if (a.half % 4 == 0) launch_rope_append<uint16_t, 4>(a, st);
+    else launch_rope_append<uint16_t, 1>(a, st);
+  } else {
+    if (a.half % 4 == 0) launch_rope_append<float, 4>(a, st);
+    else launch_rope_append<float, 1>(a, st);
+  }
+  SPIDER_LAUNCHED("rope_append");
+  return SPIDER_OK;
+}
