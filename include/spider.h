@@ -751,10 +751,10 @@ spider_status spider_rope_append(int N, int H, int Hkv, int dh, int rot, int n_a
  * the sum that divides them is that of the rounded ones.
  * Requires H % Hkv == 0, H <= 65535, N * H < 2^24, B * Hkv < 2^22, q and out 16-byte
  * aligned, q_stride a multiple of 16 bytes.  Workspace:
- * spider_paged_attention_workspace_size(N, B, H, Hkv, dh, dtype) bytes, 256-byte
- * aligned.
+ * spider_paged_attention_workspace_size(N, B, H, Hkv, dh, max_pages * page_size,
+ * dtype) bytes, 256-byte aligned.
  * ------------------------------------------------------------------------ */
-size_t spider_paged_attention_workspace_size(int N, int B, int H, int Hkv, int dh, spider_dtype dtype);
+size_t spider_paged_attention_workspace_size(int N, int B, int H, int Hkv, int dh, int slots, spider_dtype dtype);
 
 spider_status spider_paged_attention(int N, int H, int Hkv, int dh, const void* q, int64_t q_stride,
                                      const spider_paged_cache* cache, spider_dtype dtype, float scale, int window,

@@ -104,7 +104,7 @@ _SIGS = {
     "spider_rope_axes": ([_I, _D, _I, _VP, _I, _VP, _VP], _I),
     "spider_rope_append": ([_I, _I, _I, _I, _I, _I, _VP, _I64, _VP, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64,
                             ctypes.POINTER(PagedCache), _I, _VP], _I),
-    "spider_paged_attention_workspace_size": ([_I, _I, _I, _I, _I, _I], _SZ),
+    "spider_paged_attention_workspace_size": ([_I, _I, _I, _I, _I, _I, _I], _SZ),
     "spider_paged_attention": ([_I, _I, _I, _I, _VP, _I64, ctypes.POINTER(PagedCache), _I, _F, _I, _VP, _VP, _SZ, _VP], _I),
     "spider_pages_fork_workspace_size": ([_I, _I], _SZ),
     "spider_pages_fork": ([_I, _I, _I, _I, _VP, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ,
@@ -744,26 +744,35 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
 
 
 # ----------------------------------------------------------------- beams and chunks over a paged cache
-def _paged(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, like: torch.Tensor):
-    """Descriptor of one layer's pages k and v [n_pages, page_size, Hkv, dh] and its batch."""
-    dev = like.device
-    if k.dim() != 4 or k.stride(3) != 1 or not _alike(k, v):
+# (as above: one call of .shape, .stride() and get_device() per tensor, and no loops over arguments)
+def _paged(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, dtype, gpu: int):
+    """Descriptor of one layer's pages k and v [n_pages, page_size, Hkv, dh] and its batch, (Hkv, dh)."""
+    shape, stride = k.shape, k.stride()
+    if len(shape) != 4 or stride[3] != 1 or ((v.shape != shape or v.stride() != stride) and not _alike(k, v)):
         raise ValueError("k and v pages must be [n_pages, page_size, Hkv, dh] alike, with contiguous channels")
-    if k.dtype != like.dtype or v.dtype != like.dtype or k.device != dev or v.device != dev:
+    if k.dtype is not dtype or v.dtype is not dtype or k.get_device() != gpu or v.get_device() != gpu:
         raise ValueError("rows and pages must share dtype and device")
-    if table.dim() != 2 or table.dtype is not torch.int32 or table.device != dev or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError(f"table must be an int32 [B, max_pages] tensor on {dev} with contiguous rows")
-    B = table.shape[0]
-    return PagedCache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.shape[0], k.shape[1], table.data_ptr(),
-                      table.stride(0), table.shape[1], _need(lens, "lens", torch.int32, (B,), dev),
-                      _need(cu, "cu_q", torch.int32, (B + 1,), dev), B)
+    i32 = torch.int32
+    if table.dim() != 2 or table.dtype is not i32 or table.get_device() != gpu:
+        raise ValueError(f"table must be an int32 [B, max_pages] tensor on cuda:{gpu}")
+    (B, M), (row, one) = table.shape, table.stride()
+    if M > 1 and one != 1:
+        raise ValueError("the rows of table must be contiguous")
+    if lens.dtype is not i32 or lens.shape != (B,) or lens.get_device() != gpu or not lens.is_contiguous():
+        raise ValueError(f"lens must be a contiguous int32 [{B}] tensor on cuda:{gpu}")
+    if cu.dtype is not i32 or cu.shape != (B + 1,) or cu.get_device() != gpu or not cu.is_contiguous():
+        raise ValueError(f"cu_q must be a contiguous int32 [{B + 1}] tensor on cuda:{gpu}")
+    return PagedCache(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], shape[0], shape[1], table.data_ptr(), row, M,
+                      lens.data_ptr(), cu.data_ptr(), B), shape[2], shape[3]
 
 
-def _rows(t: torch.Tensor, name: str, like: torch.Tensor):
-    """Checks rows [N, heads, dh] whose heads lie side by side."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name} must be [N, heads, dh] with the heads of a row side by side, of one dtype and device")
-    return t
+def _rows(t: torch.Tensor, name: str, dtype, gpu: int):
+    """(N, heads, dh, row stride) of rows [N, heads, dh] whose heads lie side by side."""
+    if t.dim() == 3 and t.dtype is dtype and t.get_device() == gpu:
+        (n, h, dh), (row, head, one) = t.shape, t.stride()
+        if one == 1 and (h == 1 or head == dh):
+            return n, h, dh, row
+    raise ValueError(f"{name} must be [N, heads, dh] with the heads of a row side by side, of one dtype and device")
 
 
 def rope_axes(rot: int, theta: float, sections, interleaved: bool = False):
@@ -789,35 +798,45 @@ def rope_append(pos: torch.Tensor, freq: torch.Tensor, axis: torch.Tensor, *, q:
     ref = q if q is not None else k
     if ref is None:
         raise ValueError("q or k is needed")
-    dev = _gpu(ref)
-    N, _, dh = _rows(ref, "q" if q is not None else "k", ref).shape
-    if any((t is None) != (k is None) for t in (v, k_pages, v_pages, table, lens, cu_q)):
+    dev, dtype, dt = _gpu(ref), ref.dtype, _dt(ref)
+    gpu = dev.index
+    if k is None:
+        if not (v is k_pages is v_pages is table is lens is cu_q is None):
+            raise ValueError("k, v, k_pages, v_pages, table, lens and cu_q go together")
+    elif v is None or k_pages is None or v_pages is None or table is None or lens is None or cu_q is None:
         raise ValueError("k, v, k_pages, v_pages, table, lens and cu_q go together")
-    if q is None and q_out is not None:
-        raise ValueError("q_out without q")
-    if pos.dim() != 2 or pos.shape[1] != N or pos.dtype is not torch.int32 or pos.device != dev or (N > 1 and pos.stride(1) != 1):
-        raise ValueError(f"pos must be an int32 [n_axes, {N}] tensor on {dev} with contiguous rows")
-    if freq.dim() != 1:
-        raise ValueError("freq must be [rot / 2]")
-    half = freq.shape[0]
-    f, ax = _need(freq, "freq", torch.float64, (half,), dev), _need(axis, "axis", torch.uint8, (half,), dev)
+    H = Hkv = qs = os_ = ks = vs = 0
+    qp = op = kp = vp = desc = None
     if q is not None:
+        N, H, dh, qs = _rows(q, "q", dtype, gpu)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        elif _rows(q_out, "q_out", q).shape != q.shape:
+            q_out = torch.empty(N, H, dh, dtype=dtype, device=dev)
+        n, h, c, os_ = _rows(q_out, "q_out", dtype, gpu)
+        if n != N or h != H or c != dh:
             raise ValueError("q_out must have the shape of q")
-    desc = None
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
     if k is not None:
-        if _rows(k, "k", ref).shape != _rows(v, "v", ref).shape or k.shape[0] != N or k.shape[2] != dh:
+        n, Hkv, c, ks = _rows(k, "k", dtype, gpu)
+        n2, h2, c2, vs = _rows(v, "v", dtype, gpu)
+        if q is None:
+            N, dh = n, c
+        if n != N or c != dh or n2 != n or h2 != Hkv or c2 != c:
             raise ValueError("k and v must be [N, Hkv, dh] alike, with the N and dh of q")
-        desc = _paged(k_pages, v_pages, table, lens, cu_q, ref)
-        if k_pages.shape[2:] != k.shape[1:]:
+        kp, vp = k.data_ptr(), v.data_ptr()
+        desc, heads, channels = _paged(k_pages, v_pages, table, lens, cu_q, dtype, gpu)
+        if heads != Hkv or channels != dh:
             raise ValueError("the pages must have the heads and channels of k")
-    _on(dev, lib().spider_rope_append, N, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, dh, 2 * half, pos.shape[0],
-        pos.data_ptr(), pos.stride(0), f, ax, None if q is None else q.data_ptr(), 0 if q is None else q.stride(0),
-        None if q is None else q_out.data_ptr(), 0 if q is None else q_out.stride(0), None if k is None else k.data_ptr(),
-        0 if k is None else k.stride(0), None if k is None else v.data_ptr(), 0 if k is None else v.stride(0),
-        None if desc is None else ctypes.byref(desc), _dt(ref))
+        desc = ctypes.byref(desc)
+    if pos.dim() != 2 or pos.dtype is not torch.int32 or pos.get_device() != gpu:
+        raise ValueError(f"pos must be an int32 [n_axes, {N}] tensor on {dev}")
+    (n_axes, n), (ps, one) = pos.shape, pos.stride()
+    if n != N or (N > 1 and one != 1):
+        raise ValueError(f"pos must be [n_axes, {N}] with contiguous rows")
+    half = freq.numel()
+    f, ax = _need(freq, "freq", torch.float64, (half,), dev), _need(axis, "axis", torch.uint8, (half,), dev)
+    _on(dev, lib().spider_rope_append, N, H, Hkv, dh, 2 * half, n_axes, pos.data_ptr(), ps, f, ax, qp, qs, op, os_, kp, ks, vp, vs, desc, dt)
     return q_out
 
 
@@ -828,19 +847,17 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     of any layout whose channels are contiguous): rows cu_q[b] .. cu_q[b+1] - 1 are the last ones
     of the lens[b] filled slots of sequence b, whose pages are table[b].  window: the number of
     slots a row sees, up to its own (0: all).  ``scale`` defaults to dh ** -0.5."""
-    dev = _gpu(q)
-    N, H, dh = _rows(q, "q", q).shape
-    desc = _paged(k_pages, v_pages, table, lens, cu_q, q)
-    Hkv = k_pages.shape[2]
-    if k_pages.shape[3] != dh:
+    dev, dt = _gpu(q), _dt(q)
+    N, H, dh, row = _rows(q, "q", q.dtype, dev.index)
+    desc, Hkv, channels = _paged(k_pages, v_pages, table, lens, cu_q, q.dtype, dev.index)
+    if channels != dh:
         raise ValueError("the pages must have the channels of q")
     if out is None:
         out = torch.empty(N, H, dh, dtype=q.dtype, device=dev)
-    dt = _dt(q)
-    wsz = _size("spider_paged_attention_workspace_size", N, desc.B, H, Hkv, dh, dt)
+    wsz = _size("spider_paged_attention_workspace_size", N, desc.B, H, Hkv, dh, desc.max_pages * desc.page_size, dt)
     workspace, wptr = _scratch(workspace, wsz, dev)
-    _on(dev, lib().spider_paged_attention, N, H, Hkv, dh, q.data_ptr(), q.stride(0), ctypes.byref(desc), dt,
-        dh ** -0.5 if scale is None else scale, window, _need(out, "out", q.dtype, (N, H, dh), dev), wptr, wsz)
+    _on(dev, lib().spider_paged_attention, N, H, Hkv, dh, q.data_ptr(), row, ctypes.byref(desc), dt, dh ** -0.5 if scale is None else scale,
+        window, _need(out, "out", q.dtype, (N, H, dh), dev), wptr, wsz)
     return out
 
 

@@ -27,13 +27,21 @@ struct ChunkArgs {
   const void* k;
   const void* v;
   void* out;
-  float2* part_ml;  // [N * H][splits] (largest raw score, sum) of a split
-  float* part_o;    // .. [dh] its unscaled output
   int64_t qs;
   int H, Hkv, dh, window;
   float scale;
-  int row_blocks, splits, min_tiles;
+  int limit;  // sequences of up to this many rows per kv head are the few-row kernel's, the others the other's
 };
+
+// A launch of one of the two kernels.
+struct ChunkLaunch {
+  float2* part_ml;  // [rows][splits] (largest raw score, sum) of a split
+  float* part_o;    // .. [dh] its unscaled output
+  int keys, rows;   // of a tile, of a row block
+  int row_blocks, splits;
+  int whole;  // each sequence is one row block, and rows of part_* are numbered [b][hk][rows], else as in out
+};
+constexpr int kMinTiles = 8;  // tiles of a split, see chunk_plan
 
 // What a block works on: rows r0 .. of the R rows of a sequence and kv head, tiles [t0, t1) of
 // its keys, which are split `split` of ns.
@@ -42,15 +50,15 @@ struct ChunkWork {
   int b, hk, split, ns, r0, R, t0, t1;
 };
 
-// The tiles that any of the rows r0 .. r0 + rows - 1 sees, and their splits: at most a.splits, each
-// of at least a.min_tiles tiles, and no more of them than have a tile.
-__device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, ChunkWork& w, int keys, int rows) {
+// The tiles that any of the rows of block w.r0 sees, and their splits: at most l.splits, each of
+// at least kMinTiles tiles, and no more of them than have a tile.
+__device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const ChunkLaunch& l, ChunkWork& w, int keys) {
   const int G = a.H / a.Hkv, first = w.s.len - w.s.rows + w.r0 / G;
-  const int last = w.s.len - w.s.rows + (min(w.r0 + rows, w.R) - 1) / G;
+  const int last = w.s.len - w.s.rows + (min(w.r0 + l.rows, w.R) - 1) / G;
   const int lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
   w.t0 = last < 0 ? 0 : lo / keys;
   const int end = last < 0 ? 0 : last / keys + 1, n = end - w.t0;
-  const int most = max(1, min(a.splits, n / a.min_tiles));
+  const int most = max(1, min(l.splits, n / kMinTiles));
   const int per = max(1, (n + most - 1) / most);
   w.ns = most == 1 ? 1 : (n + per - 1) / per;
   w.t0 += w.split * per;
@@ -61,29 +69,30 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, ChunkWork& w, in
 // leaves every sequence as many as it needs, so that nobody has to count them beforehand; the
 // later rows of a sequence, which see more, come first.  Blocks of a (kv head, split) lie on one
 // XCD, whose L2 then holds its keys and values, where their number is a multiple of the 8 XCDs.
-template <int KEYS, int ROWS>
-__device__ __forceinline__ bool chunk_work(const ChunkArgs& a, ChunkWork& w) {
-  const int units = a.Hkv * a.splits, G = a.H / a.Hkv;
+template <int KEYS, int ROWS, bool FEW>
+__device__ __forceinline__ bool chunk_work(const ChunkArgs& a, const ChunkLaunch& l, ChunkWork& w) {
+  const int units = a.Hkv * l.splits, G = a.H / a.Hkv;
   int unit, rb;
   if (units % 8 == 0) {
     const int slot = blockIdx.x >> 3;
-    unit = slot / a.row_blocks * 8 + (blockIdx.x & 7);
-    rb = slot % a.row_blocks;
+    unit = slot / l.row_blocks * 8 + (blockIdx.x & 7);
+    rb = slot % l.row_blocks;
   } else {
     unit = blockIdx.x % units;
     rb = blockIdx.x / units;
   }
   w.hk = unit % a.Hkv;
   w.split = unit / a.Hkv;
-  auto at = [&](int b) { return (int)((int64_t)paged_start(a.p, b) * G / ROWS) + b; };
-  w.b = last_at_most(a.p.B, rb, at);
+  auto at = [&](int b) { return l.whole ? b : (int)((int64_t)paged_start(a.p, b) * G / ROWS) + b; };
+  w.b = l.whole ? rb : last_at_most(a.p.B, rb, at);
   if (w.b < 0) return false;
   w.s = paged_seq(a.p, w.b);
   w.R = w.s.rows * G;
+  if ((w.R <= a.limit) != FEW) return false;
   const int i = (w.R + ROWS - 1) / ROWS - 1 - (rb - at(w.b));
   if (i < 0) return false;
   w.r0 = i * ROWS;
-  chunk_tiles(a, w, KEYS, ROWS);
+  chunk_tiles(a, l, w, KEYS);
   return w.split < w.ns;
 }
 
@@ -109,22 +118,19 @@ struct PageIds {
   }
 };
 
-// Where the keys of a tile lie: element offsets of its groups of eight, and which of its keys
-// there are (bits).  An absent page's keys are read from page 0 and not seen.
+// Where the keys of a tile lie: element offsets of its groups of eight.  Returns which of its
+// keys there are (bits).  An absent page's keys are read from page 0 and not seen.
 template <int KEYS>
-struct TileAt {
-  int64_t off[KEYS / 8];
-  uint32_t present;
-  __device__ __forceinline__ void find(const ChunkArgs& a, PageIds& ids, int j0) {
-    present = 0;
+__device__ __forceinline__ uint32_t tile_at(const ChunkArgs& a, PageIds& ids, int j0, int64_t (&off)[KEYS / 8]) {
+  uint32_t present = 0;
 #pragma unroll
-    for (int u = 0; u < KEYS / 8; ++u) {
-      const int j = j0 + 8 * u, id = ids.get(j >> a.p.shift);
-      present |= id >= 0 ? 0xFFu << (8 * u) : 0u;
-      off[u] = max(id, 0) * a.p.sp + (j & ((1 << a.p.shift) - 1)) * a.p.ss;
-    }
+  for (int u = 0; u < KEYS / 8; ++u) {
+    const int j = j0 + 8 * u, id = ids.get(j >> a.p.shift);
+    present |= id >= 0 ? 0xFFu << (8 * u) : 0u;
+    off[u] = max(id, 0) * a.p.sp + (j & ((1 << a.p.shift) - 1)) * a.p.ss;
   }
-};
+  return present;
+}
 
 // Bits of the keys from j0 that a row at position pos sees, of those that are present.
 __device__ __forceinline__ uint32_t chunk_window(uint32_t present, int pos, int window, int j0) {
@@ -186,9 +192,10 @@ struct ChunkRows {
   }
 
   // scores to weights
-  __device__ __forceinline__ void soften(uint32_t present, int window, int j0, bool mask, int g, float sc) {
+  template <bool mask>
+  __device__ __forceinline__ void soften(uint32_t present, int window, int j0, int g, float sc) {
     uint32_t seen[RT];
-    if (mask) {
+    if constexpr (mask) {
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         const uint32_t x = chunk_window(present, pos[r], window, j0) >> (4 * g);
@@ -226,7 +233,7 @@ struct ChunkRows {
 #pragma unroll
       for (int i = 0; i < NS; ++i) p[r][i] = __builtin_amdgcn_exp2f(fmaf(p[r][i], sc, -mc));
     }
-    if (mask) {
+    if constexpr (mask) {
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -236,10 +243,10 @@ struct ChunkRows {
 
   // the values of tile t into the outputs.  Infinite and NaN values of a masked tile must not
   // reach the rows that do not see them (0 times one of them is NaN): they leave the product, and
-  // settle() puts them right after the loop.
-  template <typename S>
-  __device__ __forceinline__ void add(S& v, bool mask, int t) {
-    if (mask) {
+  // what the rows see of them is put right afterwards (seen_nonfinite).
+  template <bool mask, typename S>
+  __device__ __forceinline__ void add(S& v, int t) {
+    if constexpr (mask) {
       const bool dropped = T::drop_nonfinite(v);
       if (__any(dropped)) {
         bad0 = min(bad0, t);
@@ -272,34 +279,6 @@ struct ChunkRows {
     }
   }
 
-  // After the tiles t0, t0 + 1, .. < t1: a row's outputs are infinite or NaN where it sees such a
-  // value in a masked tile.  channel(c, i): of output o[.][c][i]
-  template <typename F>
-  __device__ __forceinline__ void settle(const ChunkArgs& a, const ChunkWork& w, const AT* vb, F&& channel) {
-    if (bad0 > bad1) return;
-    const int P = 1 << a.p.shift;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int c = 0; c < CPL; ++c) {
-        floatx4 s = floatx4{};
-#pragma unroll 1
-        for (int j = bad0 * KEYS; j < min((bad1 + 1) * KEYS, w.s.len); ++j) {
-          const int page = paged_page(a.p, w.b, j >> a.p.shift);
-          if (page < 0 || !(chunk_window(1u, pos[r], a.window, j) & 1u)) continue;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int ch = channel(c, i);
-            const float y = ch < a.dh ? T::value(vb + page * a.p.sp + (j & (P - 1)) * a.p.ss + ch) : 0.f;
-            if (!(fabsf(y) < INFINITY)) s[i] += y;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(fabsf(s[i]) < INFINITY)) o[r][c][i] = s[i];
-      }
-  }
-
   // the row's sum, in every lane of its column
   __device__ __forceinline__ float row_sum(int r) const {
     if constexpr (BF16) return sum[r][0];
@@ -309,17 +288,36 @@ struct ChunkRows {
   }
 };
 
-// Row rr of the block's sequence and kv head: its place in the output, in units of dh.
+// Row rr of the block's sequence and kv head: its place in the output, in units of dh, and that
+// of its split in part_*.
 __device__ __forceinline__ int64_t chunk_row(const ChunkArgs& a, const ChunkWork& w, int rr) {
   const int G = a.H / a.Hkv;
   return (int64_t)(w.s.start + rr / G) * a.H + w.hk * G + rr % G;
+}
+__device__ __forceinline__ int64_t chunk_part(const ChunkArgs& a, const ChunkLaunch& l, const ChunkWork& w, int rr) {
+  return (l.whole ? ((int64_t)w.b * a.Hkv + w.hk) * l.rows + rr : chunk_row(a, w, rr)) * l.splits + w.split;
+}
+
+// The sum of the infinite and NaN values in channel ch that row rr of the block's sequence sees
+// among the keys j0 <= j < j1, 0 without any: it is then that row's output, whatever the weights.
+template <typename AT, int DH>
+__device__ __forceinline__ float seen_nonfinite(const ChunkArgs& a, int b, const PagedSeq& s, int hk, int rr, int ch, int j0, int j1) {
+  const int pos = s.len - s.rows + rr / (a.H / a.Hkv), P = 1 << a.p.shift;
+  float sum = 0.f;
+  for (int j = max(j0, a.window > 0 ? pos - a.window + 1 : 0); j < min(j1, pos + 1); ++j) {
+    const int page = paged_page(a.p, b, j >> a.p.shift);
+    if (page < 0) continue;
+    const float y = AttnTile<AT, DH>::value(reinterpret_cast<const AT*>(a.v) + page * a.p.sp + (j & (P - 1)) * a.p.ss + hk * a.p.sh + ch);
+    if (!(fabsf(y) < INFINITY)) sum += y;
+  }
+  return sum;
 }
 
 // Few rows: bound by the reads of keys and values, which go straight from memory to the registers
 // of the wave that uses them, the next tile's keys on their way during the softmax.  Each of the
 // 4 waves takes a run of the block's tiles; their sums meet in LDS.
 template <typename AT, int DH, int RT, bool FULL>
-__global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(ChunkArgs a) {
+__global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(ChunkArgs a, ChunkLaunch l) {
   using Rows = ChunkRows<AT, DH, RT>;
   using T = typename Rows::T;
   constexpr int KEYS = T::KEYS, CPL = T::CPL;
@@ -329,7 +327,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, g = lane >> 4;
   ChunkWork w;
-  if (!chunk_work<KEYS, ROWS>(a, w)) return;
+  if (!chunk_work<KEYS, ROWS, true>(a, l, w)) return;
   const AT* kb = reinterpret_cast<const AT*>(a.k) + w.hk * a.p.sh;
   const AT* vb = reinterpret_cast<const AT*>(a.v) + w.hk * a.p.sh;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
@@ -338,75 +336,89 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
   typename T::V v;
   PageIds ids;
   ids.start(a, w);
-  TileAt<KEYS> now, next;
   // the lane's places within a group of eight keys
   const int64_t k_at = (m & 7) * a.p.ss, v_at = 4 * (g & 1) * a.p.ss;
-  auto load_k = [&](const TileAt<KEYS>& at) {
+  auto load_k = [&](const int64_t* off) {
 #pragma unroll
-    for (int t = 0; t < T::KT; ++t) T::template load_k_row<FULL>(k, t, kb + (m < 8 ? at.off[2 * t] : at.off[2 * t + 1]) + k_at, g, a.dh);
+    for (int t = 0; t < T::KT; ++t) T::template load_k_row<FULL>(k, t, kb + (m < 8 ? off[2 * t] : off[2 * t + 1]) + k_at, g, a.dh);
   };
   const int each = (w.t1 - w.t0 + 3) / 4, end = min(w.t1, w.t0 + (wave + 1) * each);
   int t = w.t0 + wave * each;
+  int64_t off[KEYS / 8] = {};
+  uint32_t present = 0;
   if (t < end) {
-    now.find(a, ids, t * KEYS);
-    load_k(now);
+    present = tile_at<KEYS>(a, ids, t * KEYS, off);
+    load_k(off);
   }
   rows.template start<FULL>(a, w, w.r0, lane);
-  for (; t < end; ++t) {
+  auto step = [&](auto mask_) {
+    constexpr bool mask = decltype(mask_)::value;
 #pragma unroll
     for (int h = 0; h < T::KT; ++h) {
-      const AT* row = vb + (g < 2 ? now.off[2 * h] : now.off[2 * h + 1]) + v_at;
+      const AT* row = vb + (g < 2 ? off[2 * h] : off[2 * h + 1]) + v_at;
 #pragma unroll
       for (int e = 0; e < 4; ++e) T::template load_v_row<FULL>(v, 4 * h + e, row + e * a.p.ss, m, a.dh);
     }
     rows.scores(k);
+    const uint32_t here = present;
     if (t + 1 < end) {
-      next.find(a, ids, (t + 1) * KEYS);
-      load_k(next);
+      present = tile_at<KEYS>(a, ids, (t + 1) * KEYS, off);
+      load_k(off);
     }
-    const bool mask = rows.masked(now.present, a.window, t * KEYS);
-    rows.soften(now.present, a.window, t * KEYS, mask, g, sc);
-    rows.add(v, mask, t);
-    now = next;
+    rows.template soften<mask>(here, a.window, t * KEYS, g, sc);
+    rows.template add<mask>(v, t);
+    ++t;
+  };
+  while (t < end) {
+    while (t < end && !rows.masked(present, a.window, t * KEYS)) step(std::false_type{});
+    while (t < end && rows.masked(present, a.window, t * KEYS)) step(std::true_type{});
   }
-  rows.settle(a, w, vb, [&](int c, int i) { return T::channel(c, 4 * g + i); });
 
   // the waves' sums onto their common maximum, in wave order
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const float l = rows.row_sum(r);
+    const float sum = rows.row_sum(r);
     if (g == 0) {
       xm[wave][16 * r + m] = rows.top[r];
-      xl[wave][16 * r + m] = l;
+      xl[wave][16 * r + m] = sum;
     }
 #pragma unroll
     for (int c = 0; c < CPL; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) xo[wave][16 * r + m][T::channel(c, 4 * g + i)] = rows.o[r][c][i];
   }
+  if (rows.bad0 <= rows.bad1) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+    for (int i = lane; i < ROWS * a.dh; i += 64) {
+      const int r = i / a.dh, ch = i - r * a.dh;
+      const float s = seen_nonfinite<AT, DH>(a, w.b, w.s, w.hk, min(w.r0 + r, w.R - 1), ch, rows.bad0 * KEYS, (rows.bad1 + 1) * KEYS);
+      if (!(fabsf(s) < INFINITY)) xo[wave][r][ch] = s;
+    }
+  }
   __syncthreads();
   constexpr int PER = 256 / ROWS;  // threads of a row
   const int c0 = 4 * (tid % PER), row = tid / PER;
   if (row >= w.R - w.r0) return;
-  float mx = -INFINITY, l = 0.f, f[4];
+  float mx = -INFINITY, sum = 0.f, f[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) mx = fmaxf(mx, xm[u][row]);
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     f[u] = xm[u][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm[u][row] - mx) * sc);
     // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
-    l += xm[u][row] == -INFINITY ? xl[u][row] : xl[u][row] * f[u];
+    sum += xm[u][row] == -INFINITY ? xl[u][row] : xl[u][row] * f[u];
   }
-  const int64_t out_row = chunk_row(a, w, w.r0 + row), part_row = out_row * a.splits + w.split;
-  if (tid % PER == 0 && w.ns > 1) a.part_ml[part_row] = make_float2(mx, l);
+  const int64_t out_row = chunk_row(a, w, w.r0 + row), part_row = chunk_part(a, l, w, w.r0 + row);
+  if (tid % PER == 0 && w.ns > 1) l.part_ml[part_row] = make_float2(mx, sum);
   for (int c = c0; c < a.dh; c += 4 * PER) {
     floatx4 x = floatx4{};
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] += rescaled(xo[u][row][c + i], f[u]);
-    if (w.ns > 1) *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + c) = x;
-    else attn_store<AT>(a.out, out_row * a.dh + c, x, l);
+    if (w.ns > 1) *reinterpret_cast<floatx4*>(l.part_o + part_row * a.dh + c) = x;
+    else attn_store<AT>(a.out, out_row * a.dh + c, x, sum);
   }
 }
 
@@ -415,7 +427,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
 // for values; 16-byte piece c of key j lies at piece c ^ (j % 16 or less), so that both the reads
 // of one piece of 16 keys and those of all pieces of a key spread over the banks.
 template <int DH, int NW, bool FULL>
-__global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a) {
+__global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l) {
   constexpr int RT = DH == 256 ? 1 : 2;
   using Rows = ChunkRows<uint16_t, DH, RT>;
   using T = typename Rows::T;
@@ -427,7 +439,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, g = lane >> 4;
   ChunkWork w;
-  if (!chunk_work<32, ROWS>(a, w)) return;
+  if (!chunk_work<32, ROWS, false>(a, l, w)) return;
   const uint16_t* kb = reinterpret_cast<const uint16_t*>(a.k) + w.hk * a.p.sh;
   const uint16_t* vb = reinterpret_cast<const uint16_t*>(a.v) + w.hk * a.p.sh;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
@@ -442,11 +454,11 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a) {
   constexpr int KD = DH / 16 / NW, DMAS = KD ? 2 * KD : 1;
   auto fetch = [&](int t) {
     const uint32_t to = lds0 + (uint32_t)((t - w.t0) % STAGES * 4 * TILE);
-    TileAt<32> at;
-    at.find(a, ids, 32 * t);
+    int64_t at[4];
+    const uint32_t found = tile_at<32>(a, ids, 32 * t, at);
     auto from = [&](int part) {
       const int j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ (j & SWZ), u = part * KPD / 8;
-      const int64_t off = u == 0 ? at.off[0] : (u == 1 ? at.off[1] : (u == 2 ? at.off[2] : at.off[3]));
+      const int64_t off = u == 0 ? at[0] : (u == 1 ? at[1] : (u == 2 ? at[2] : at[3]));
       return off + (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
     };
     if constexpr (KD > 0) {
@@ -461,13 +473,15 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a) {
       const int part = wave % (NW / 2);
       dma16((wave < NW / 2 ? kb : vb) + from(part), to + (wave < NW / 2 ? 0 : 2 * TILE) + part * 1024);
     }
-    return at.present;
+    return found;
   };
   dma_wait_all();  // the queries are here: from now on only the DMAs count as loads in flight
   uint32_t present[3] = {};  // of this tile and the next two
   if (w.t0 < w.t1) present[0] = fetch(w.t0);
   if (w.t0 + 1 < w.t1) present[1] = fetch(w.t0 + 1);
-  for (int t = w.t0; t < w.t1; ++t) {
+  int t = w.t0;
+  auto step = [&](auto mask_) {
+    constexpr bool mask = decltype(mask_)::value;
     // tile t has landed, and every wave is done with tile t - 1, whose place tile t + 2 takes
     if (t + 1 < w.t1) dma_wait_barrier<DMAS>();
     else dma_wait_barrier<0>();
@@ -502,35 +516,48 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a) {
       }
       v.f[c] = x;
     }
-    const bool mask = rows.masked(present[0], a.window, 32 * t);
-    rows.soften(present[0], a.window, 32 * t, mask, g, sc);
-    rows.add(v, mask, t);
+    rows.template soften<mask>(present[0], a.window, 32 * t, g, sc);
+    rows.template add<mask>(v, t);
     present[0] = present[1];
     present[1] = present[2];
+    ++t;
+  };
+  while (t < w.t1) {
+    while (t < w.t1 && !rows.masked(present[0], a.window, 32 * t)) step(std::false_type{});
+    while (t < w.t1 && rows.masked(present[0], a.window, 32 * t)) step(std::true_type{});
   }
-  rows.settle(a, w, vb, [&](int c, int i) { return 16 * c + 4 * g + i; });
 
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const float l = rows.row_sum(r);
+    const float sum = rows.row_sum(r);
     const int rr = w.r0 + 16 * (RT * wave + r) + m;
     if (rr >= w.R) continue;
-    const int64_t out_row = chunk_row(a, w, rr), part_row = out_row * a.splits + w.split;
-    if (g == 0 && w.ns > 1) a.part_ml[part_row] = make_float2(rows.top[r], l);
+    const int64_t out_row = chunk_row(a, w, rr), part_row = chunk_part(a, l, w, rr);
+    if (g == 0 && w.ns > 1) l.part_ml[part_row] = make_float2(rows.top[r], sum);
 #pragma unroll
     for (int c = 0; c < CPL; ++c) {
       const int ch = 16 * c + 4 * g;  // of four consecutive outputs
       if (!FULL && ch >= a.dh) continue;
-      if (w.ns > 1) *reinterpret_cast<floatx4*>(a.part_o + part_row * a.dh + ch) = rows.o[r][c];
-      else attn_store<uint16_t>(a.out, out_row * a.dh + ch, rows.o[r][c], l);
+      if (w.ns > 1) *reinterpret_cast<floatx4*>(l.part_o + part_row * a.dh + ch) = rows.o[r][c];
+      else attn_store<uint16_t>(a.out, out_row * a.dh + ch, rows.o[r][c], sum);
     }
+  }
+  if (rows.bad0 > rows.bad1) return;
+#pragma unroll 1
+  for (int i = 0; i < RT * CPL * 4; ++i) {
+    const int rr = w.r0 + 16 * (RT * wave + i / (CPL * 4)) + m, ch = 16 * (i / 4 % CPL) + 4 * g + i % 4;
+    if (rr >= w.R || ch >= a.dh) continue;
+    const float s = seen_nonfinite<uint16_t, DH>(a, w.b, w.s, w.hk, rr, ch, rows.bad0 * 32, (rows.bad1 + 1) * 32);
+    if (fabsf(s) < INFINITY) continue;
+    if (w.ns > 1) l.part_o[chunk_part(a, l, w, rr) * a.dh + ch] = s;
+    else reinterpret_cast<uint16_t*>(a.out)[chunk_row(a, w, rr) * a.dh + ch] = (uint16_t)((__float_as_uint(s) >> 16) | (s != s ? 0x40u : 0u));
   }
 }
 
 // A wave per row (new token, head): its splits onto their common maximum, in order.  Groups of
 // dh / 4 lanes, four channels each, take every ng-th split; their sums meet by shuffles.
 template <typename AT>
-__global__ void __launch_bounds__(256) paged_join_kernel(ChunkArgs a, int keys, int block_rows) {
+__global__ void __launch_bounds__(256) paged_join_kernel(ChunkArgs a, ChunkLaunch few, ChunkLaunch chunk) {
   const int lane = threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= (int64_t)a.p.N * a.H) return;
@@ -541,106 +568,150 @@ __global__ void __launch_bounds__(256) paged_join_kernel(ChunkArgs a, int keys, 
   w.s = paged_seq(a.p, w.b);
   if (n - w.s.start >= w.s.rows) return;
   w.R = w.s.rows * G;
+  const ChunkLaunch l = w.R <= a.limit ? few : chunk;
+  const int rr = (n - w.s.start) * G + h % G;
+  w.hk = h / G;
   w.split = 0;
-  w.r0 = ((n - w.s.start) * G + h % G) / block_rows * block_rows;
-  chunk_tiles(a, w, keys, block_rows);
+  w.r0 = rr / l.rows * l.rows;
+  chunk_tiles(a, l, w, l.keys);
   if (w.ns == 1) return;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
-  const int64_t part = r * a.splits;
+  const int64_t part = chunk_part(a, l, w, rr);
   float mx = -INFINITY;
-  for (int s = lane; s < w.ns; s += 64) mx = fmaxf(mx, a.part_ml[part + s].x);
+  for (int s = lane; s < w.ns; s += 64) mx = fmaxf(mx, l.part_ml[part + s].x);
   mx = wave_max(mx);
   const int per = a.dh / 4, ng = 64 / per, grp = lane / per, c = 4 * (lane % per);
-  float l = 0.f;
+  float sum = 0.f;
   floatx4 x = floatx4{};
-  for (int s = grp; grp < ng && s < w.ns; s += ng) {
-    const float2 ml = a.part_ml[part + s];
-    const floatx4 o = *reinterpret_cast<const floatx4*>(a.part_o + (part + s) * a.dh + c);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mx) * sc);
-    // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
-    l += ml.x == -INFINITY ? ml.y : ml.y * f;
+  if (grp < ng) {
+    for (int s0 = grp; s0 < w.ns; s0 += 4 * ng) {
+      float2 ml[4];
+      floatx4 o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] += rescaled(o[i], f);
+      for (int u = 0; u < 4; ++u) {
+        const int s = min(s0 + u * ng, w.ns - 1);
+        ml[u] = l.part_ml[part + s];
+        o[u] = *reinterpret_cast<const floatx4*>(l.part_o + (part + s) * a.dh + c);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (s0 + u * ng >= w.ns) break;
+        const float f = ml[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[u].x - mx) * sc);
+        // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
+        sum += ml[u].x == -INFINITY ? ml[u].y : ml[u].y * f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += rescaled(o[u][i], f);
+      }
+    }
   }
   floatx4 y = x;
-  float total = l;
+  float total = sum;
   for (int i = 1; i < ng; ++i) {
-    total += __shfl(l, (lane + i * per) & 63);
+    total += __shfl(sum, (lane + i * per) & 63);
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] += __shfl(x[e], (lane + i * per) & 63);
   }
   if (grp == 0) attn_store<AT>(a.out, r * a.dh + c, y, total);
 }
 
-// Tiles, row blocks and splits of a call, and its workspace.
+// The launches of a call, and its workspace.  The few-row kernel serves 16 or 32 rows of a
+// sequence and kv head per block, the other one (bf16) up to 256.  How many rows a sequence has is
+// known on the device only: a batch whose average is within 32 rows goes to the first kernel,
+// whatever its sequences are, one sequence to the other; else both are launched, and the
+// sequences of up to 16 rows are the first one's.
 struct ChunkPlan {
   int dhp;  // kernel width: 64, 128 or 256
-  int rt;   // row tiles of a wave of paged_few_kernel, or 0:
-  int nw;   // waves of paged_chunk_kernel
-  int rows, row_blocks, splits, min_tiles;
-  size_t o_off, bytes;
+  int rt;   // row tiles of a wave of paged_few_kernel, or 0: not launched
+  int nw;   // waves of paged_chunk_kernel, or 0
+  int limit;
+  ChunkLaunch few, chunk;
+  size_t few_o, chunk_ml, chunk_o, bytes;
 };
 
-ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, spider_dtype dtype) {
+ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, spider_dtype dtype) {
   ChunkPlan p{};
   const bool bf16 = dtype == SPIDER_BF16;
   const int64_t G = H / Hkv, R = N * G;  // rows of a kv head, R / B of an average sequence
   p.dhp = dh <= 64 ? 64 : (dh <= 128 ? 128 : 256);
-  const int wave_rows = p.dhp == 256 ? 16 : 32;
-  int64_t target;
+  const int wave_rows = p.dhp == 256 ? 16 : 32, keys = bf16 ? 32 : 16;
+  const int most = std::max(1, ceil_div(slots, keys) / kMinTiles);  // splits of the longest sequence
+  size_t off = 0;
   if (!bf16 || R <= (int64_t)B * wave_rows) {
     p.rt = R <= (int64_t)B * 16 || p.dhp == 256 ? 1 : 2;
-    p.rows = 16 * p.rt;
-    target = 768;
-  } else {
-    // (width 256 has no registers for two waves per SIMD)
-    p.nw = R <= (int64_t)B * 2 * wave_rows ? 2 : (R <= (int64_t)B * 4 * wave_rows || p.dhp == 256 ? 4 : 8);
-    p.rows = wave_rows * p.nw;
-    target = p.dhp == 256 ? 256 : 256 * 8 / p.nw;
+    p.limit = 0x7fffffff;
+    const int rows = 16 * p.rt, blocks = (int)(R / rows);
+    p.few = ChunkLaunch{nullptr, nullptr, keys, rows, blocks + B, 1, 0};
+    p.few.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 768 / (Hkv * std::max<int64_t>(B, blocks))));
+    if (p.few.splits > 1) {
+      const size_t n = (size_t)N * H * p.few.splits;
+      p.few_o = align_up(n * sizeof(float2), 256);
+      off = align_up(p.few_o + n * dh * sizeof(float), 256);
+    }
+    p.bytes = off;
+    return p;
   }
-  p.row_blocks = (int)(R / p.rows) + B;
-  p.min_tiles = 8;
-  const int64_t blocks = Hkv * std::max<int64_t>(B, R / p.rows);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(target / blocks, 128));
-  size_t off = 0;
-  if (p.splits > 1) {
-    const size_t rows = (size_t)N * H * p.splits;
-    p.o_off = align_up(rows * sizeof(float2), 256);
-    off = align_up(p.o_off + rows * dh * sizeof(float), 256);
+  p.limit = -1;
+  if (B > 1) {
+    p.rt = 1;
+    p.limit = 16;
+    p.few = ChunkLaunch{nullptr, nullptr, keys, 16, B, 1, 1};
+    p.few.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 768 / ((int64_t)Hkv * B)));
+    if (p.few.splits > 1) {
+      const size_t n = (size_t)B * Hkv * 16 * p.few.splits;
+      p.few_o = align_up(n * sizeof(float2), 256);
+      off = align_up(p.few_o + n * dh * sizeof(float), 256);
+    }
+  }
+  // (width 256 has no registers for two waves per SIMD)
+  p.nw = R <= (int64_t)B * 2 * wave_rows ? 2 : (R <= (int64_t)B * 4 * wave_rows || p.dhp == 256 ? 4 : 8);
+  const int rows = wave_rows * p.nw, at_once = p.dhp == 256 ? 256 : 256 * 8 / p.nw;  // blocks that run at once
+  const int64_t blocks = Hkv * std::max<int64_t>(1, R / rows);
+  p.chunk = ChunkLaunch{nullptr, nullptr, keys, rows, (int)(R / rows) + B, 1, 0};
+  // The splits that leave the least of the last round of blocks empty; each costs its joining.
+  double best = 1e30;
+  for (int s = 1; s <= std::min(most, 16); ++s) {
+    const double rounds = (double)((blocks * s + at_once - 1) / at_once) / s * (1.0 + 0.03 * (s - 1));
+    if (rounds < best) best = rounds, p.chunk.splits = s;
+  }
+  if (p.chunk.splits > 1) {
+    const size_t n = (size_t)N * H * p.chunk.splits;
+    p.chunk_ml = off;
+    p.chunk_o = align_up(off + n * sizeof(float2), 256);
+    off = align_up(p.chunk_o + n * dh * sizeof(float), 256);
   }
   p.bytes = off;
   return p;
 }
 
-unsigned chunk_blocks(const ChunkArgs& a) { return (unsigned)(a.Hkv * a.splits) * (unsigned)a.row_blocks; }
+unsigned chunk_blocks(const ChunkArgs& a, const ChunkLaunch& l) { return (unsigned)(a.Hkv * l.splits) * (unsigned)l.row_blocks; }
 
 template <typename AT, int DH, int RT>
-void launch_few(const ChunkArgs& a, hipStream_t st) {
-  if (a.dh == DH) paged_few_kernel<AT, DH, RT, true><<<chunk_blocks(a), 256, 0, st>>>(a);
-  else paged_few_kernel<AT, DH, RT, false><<<chunk_blocks(a), 256, 0, st>>>(a);
+void launch_few(const ChunkArgs& a, const ChunkLaunch& l, hipStream_t st) {
+  if (a.dh == DH) paged_few_kernel<AT, DH, RT, true><<<chunk_blocks(a, l), 256, 0, st>>>(a, l);
+  else paged_few_kernel<AT, DH, RT, false><<<chunk_blocks(a, l), 256, 0, st>>>(a, l);
 }
 
 template <int DH, int NW>
-void launch_chunk(const ChunkArgs& a, hipStream_t st) {
-  if (a.dh == DH) paged_chunk_kernel<DH, NW, true><<<chunk_blocks(a), 64 * NW, 0, st>>>(a);
-  else paged_chunk_kernel<DH, NW, false><<<chunk_blocks(a), 64 * NW, 0, st>>>(a);
+void launch_chunk(const ChunkArgs& a, const ChunkLaunch& l, hipStream_t st) {
+  if (a.dh == DH) paged_chunk_kernel<DH, NW, true><<<chunk_blocks(a, l), 64 * NW, 0, st>>>(a, l);
+  else paged_chunk_kernel<DH, NW, false><<<chunk_blocks(a, l), 64 * NW, 0, st>>>(a, l);
 }
 
 template <typename AT, int DH>
 spider_status run_chunk(const ChunkArgs& a, const ChunkPlan& p, hipStream_t st) {
   ProfScope ps(KC_PAGED_ATTN, st);
-  if (p.rt == 1) launch_few<AT, DH, 1>(a, st);
-  if constexpr (DH <= 128)
-    if (p.rt == 2) launch_few<AT, DH, 2>(a, st);
   if constexpr (sizeof(AT) == 2) {
-    if (p.nw == 2) launch_chunk<DH, 2>(a, st);
-    if (p.nw == 4) launch_chunk<DH, 4>(a, st);
+    if (p.nw == 2) launch_chunk<DH, 2>(a, p.chunk, st);
+    if (p.nw == 4) launch_chunk<DH, 4>(a, p.chunk, st);
     if constexpr (DH <= 128)
-      if (p.nw == 8) launch_chunk<DH, 8>(a, st);
+      if (p.nw == 8) launch_chunk<DH, 8>(a, p.chunk, st);
   }
+  if (p.rt == 1) launch_few<AT, DH, 1>(a, p.few, st);
+  if constexpr (DH <= 128)
+    if (p.rt == 2) launch_few<AT, DH, 2>(a, p.few, st);
   SPIDER_LAUNCHED("paged_attention");
-  if (a.splits > 1) {
-    paged_join_kernel<AT><<<(unsigned)(((int64_t)a.p.N * a.H + 3) / 4), 256, 0, st>>>(a, AttnTile<AT, DH>::KEYS, p.rows);
+  if (p.few.splits > 1 || p.chunk.splits > 1) {
+    paged_join_kernel<AT><<<(unsigned)(((int64_t)a.p.N * a.H + 3) / 4), 256, 0, st>>>(a, p.few, p.chunk);
     SPIDER_LAUNCHED("paged_join");
   }
   return SPIDER_OK;
@@ -661,8 +732,8 @@ bool chunk_shape_ok(int N, int B, int H, int Hkv, int dh, spider_dtype dtype) {
 
 using namespace spider;
 
-extern "C" size_t spider_paged_attention_workspace_size(int N, int B, int H, int Hkv, int dh, spider_dtype dtype) {
-  return chunk_shape_ok(N, B, H, Hkv, dh, dtype) ? chunk_plan(N, B, H, Hkv, dh, dtype).bytes : 0;
+extern "C" size_t spider_paged_attention_workspace_size(int N, int B, int H, int Hkv, int dh, int slots, spider_dtype dtype) {
+  return chunk_shape_ok(N, B, H, Hkv, dh, dtype) && slots >= 1 && slots <= (1 << 30) ? chunk_plan(N, B, H, Hkv, dh, slots, dtype).bytes : 0;
 }
 
 extern "C" spider_status spider_paged_attention(int N, int H, int Hkv, int dh, const void* q, int64_t q_stride,
@@ -684,17 +755,21 @@ extern "C" spider_status spider_paged_attention(int N, int H, int Hkv, int dh, c
   SPIDER_REQUIRE(q_stride % per16 == 0 && q_stride >= 0, SPIDER_ERR_INVALID_ARG, "spider_paged_attention: q_stride must be a multiple of 16 bytes");
   SPIDER_REQUIRE((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) % 16 == 0, SPIDER_ERR_INVALID_ARG,
                  "spider_paged_attention: q and out must be 16-byte aligned");
-  const ChunkPlan p = chunk_plan(N, cache->B, H, Hkv, dh, dtype);
+  ChunkPlan p = chunk_plan(N, cache->B, H, Hkv, dh, cache->max_pages * cache->page_size, dtype);
   SPIDER_REQUIRE(p.bytes == 0 || (workspace && workspace_bytes >= p.bytes), SPIDER_ERR_WORKSPACE,
                  "spider_paged_attention: workspace of %zu bytes needed, %zu given", p.bytes, workspace ? workspace_bytes : 0);
   SPIDER_REQUIRE(p.bytes == 0 || reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG,
                  "spider_paged_attention: workspace must be 256-byte aligned");
   a.q = q, a.k = cache->k, a.v = cache->v, a.out = out, a.qs = q_stride;
-  a.H = H, a.Hkv = Hkv, a.dh = dh, a.window = window, a.scale = scale;
-  a.row_blocks = p.row_blocks, a.splits = p.splits, a.min_tiles = p.min_tiles;
-  if (p.splits > 1) {
-    a.part_ml = reinterpret_cast<float2*>(workspace);
-    a.part_o = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + p.o_off);
+  a.H = H, a.Hkv = Hkv, a.dh = dh, a.window = window, a.scale = scale, a.limit = p.limit;
+  char* ws = reinterpret_cast<char*>(workspace);
+  if (p.few.splits > 1) {
+    p.few.part_ml = reinterpret_cast<float2*>(ws);
+    p.few.part_o = reinterpret_cast<float*>(ws + p.few_o);
+  }
+  if (p.chunk.splits > 1) {
+    p.chunk.part_ml = reinterpret_cast<float2*>(ws + p.chunk_ml);
+    p.chunk.part_o = reinterpret_cast<float*>(ws + p.chunk_o);
   }
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   return dtype == SPIDER_BF16 ? run_chunk<uint16_t>(a, p, st) : run_chunk<float>(a, p, st);

@@ -94,7 +94,7 @@ def test_chunk_sizes(dtype, T, dh):
 def test_splits(dtype, lens, news, H, Hkv, dh):
     lib = need_gpu()
     q, kp, vp, table, cu = case(len(lens), H, Hkv, dh, 16, lens, news, dtype)
-    need = lib.lib().spider_paged_attention_workspace_size(sum(news), len(lens), H, Hkv, dh, lib.BF16 if dtype == "bf16" else lib.F32)
+    need = lib.lib().spider_paged_attention_workspace_size(sum(news), len(lens), H, Hkv, dh, table.shape[1] * 16, lib.BF16 if dtype == "bf16" else lib.F32)
     assert need > 0  # the keys are split
     for window in (0, 777):
         out = lib.paged_attention(q, kp, vp, ints(table), ints(lens), ints(cu), window=window)
@@ -257,7 +257,7 @@ def test_captured_calls_follow_the_tables(dtype):
     kp, vp = (pages(rng, 60, P, 2, 64, dtype) for _ in range(2))
     q = rows(rng, N, 4, 64, dtype, 1.5)
     t, n, c = ints(np.full((B, 24), -1)), ints([0] * B), ints([0] * (B + 1))
-    size = lib.lib().spider_paged_attention_workspace_size(N, B, 4, 2, 64, lib.BF16 if dtype == "bf16" else lib.F32)
+    size = lib.lib().spider_paged_attention_workspace_size(N, B, 4, 2, 64, 24 * P, lib.BF16 if dtype == "bf16" else lib.F32)
     graphs = []
     for window in (0, 50):
         ws = torch.empty(max(size, 256), dtype=torch.uint8, device="cuda")

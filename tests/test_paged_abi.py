@@ -97,7 +97,7 @@ ATTN = dict(N=9, H=4, Hkv=2, dh=64, q=6 * P, qs=256, cache=None, dt=1, scale=0.1
     (dict(ws=None), WORKSPACE), (dict(wsb=255), WORKSPACE), (dict(ws=8 * P + 16), INVALID), (dict(dt=0, dh=2), UNSUPPORTED),
 ])
 def test_paged_attention_refusals(L, change, status):
-    a = dict(ATTN, cache=cache())
+    a = dict(ATTN, cache=cache(max_pages=800, table_stride=800))
     a.update(change)
     a["cache"] = ctypes.byref(a["cache"]) if a["cache"] else None
     assert L.spider_paged_attention(*a.values(), None) == status
@@ -153,9 +153,10 @@ def test_beam_select_refusals(L, change, status):
 
 
 def test_workspace_sizes(L):
-    assert L.spider_paged_attention_workspace_size(0, 1, 4, 2, 64, 1) == 0
-    assert L.spider_paged_attention_workspace_size(9, 3, 5, 2, 64, 1) == 0
-    assert L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 1) > 0
+    assert L.spider_paged_attention_workspace_size(0, 1, 4, 2, 64, 9000, 1) == 0
+    assert L.spider_paged_attention_workspace_size(9, 3, 5, 2, 64, 9000, 1) == 0
+    assert L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 0, 1) == 0
+    assert L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 256, 1) == 0 < L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 9000, 1)
     assert L.spider_pages_fork_workspace_size(0, 10) == 0 and L.spider_pages_fork_workspace_size(4097, 10) == 0
     assert L.spider_pages_fork_workspace_size(5, 1000) >= 5 * 16 + 4000
     assert L.spider_beam_select_workspace_size(1, 65, 1, 100) == 0 and L.spider_beam_select_workspace_size(1, 1, 1, (1 << 19) + 1) == 0
