@@ -745,6 +745,9 @@ def adjust_logits(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
 
 # ----------------------------------------------------------------- beams and chunks over a paged cache
 # (as above: one call of .shape, .stride() and get_device() per tensor, and no loops over arguments)
+_I64x4 = ctypes.c_int64 * 4
+
+
 def _paged(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, dtype, gpu: int):
     """Descriptor of one layer's pages k and v [n_pages, page_size, Hkv, dh] and its batch, (Hkv, dh)."""
     shape, stride = k.shape, k.stride()
@@ -869,14 +872,14 @@ def pages_fork(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torc
     none) of table [B, max_pages] and lens [B], with room for n_new[b] more slots; ref [n_pages]
     counts who holds a page.  All int32.  Shared last pages are copied in k and v before two
     sequences write into them.  Returns (table_out, lens_out, ref_out, missing [1])."""
-    if k.dim() != 5 or table.dim() != 2 or parent.dim() != 1:
+    dev, shape, stride = _gpu(k), k.shape, k.stride()
+    if len(shape) != 5 or table.dim() != 2 or parent.dim() != 1:
         raise ValueError("k and v must be [L, n_pages, page_size, Hkv, dh], table [B, max_pages], parent [B_out]")
-    dev = _gpu(k)
-    L_, n_pages, page_size, Hkv, dh = k.shape
-    if not _alike(k, v) or k.stride(4) != 1 or v.dtype != k.dtype or v.device != dev:
+    if stride[4] != 1 or ((v.shape != shape or v.stride() != stride) and not _alike(k, v)) or v.dtype is not k.dtype or v.device != dev:
         raise ValueError("k and v must be alike, with contiguous channels")
+    L_, n_pages, page_size, Hkv, dh = shape
     B, M = table.shape
-    n = parent.shape[0]
+    n, = parent.shape
     i32 = torch.int32
     if table_out is None:
         table_out = torch.empty(n, M, dtype=i32, device=dev)
@@ -886,10 +889,9 @@ def pages_fork(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torc
         ref_out = torch.empty(n_pages, dtype=i32, device=dev)
     if missing is None:
         missing = torch.empty(1, dtype=i32, device=dev)
-    strides = (ctypes.c_int64 * 4)(*k.stride()[:4])
     wsz = _size("spider_pages_fork_workspace_size", n, n_pages)
     workspace, wptr = _scratch(workspace, wsz, dev)
-    _on(dev, lib().spider_pages_fork, L_, Hkv, dh, _dt(k), k.data_ptr(), v.data_ptr(), strides, n_pages, page_size, M, B,
+    _on(dev, lib().spider_pages_fork, L_, Hkv, dh, _dt(k), k.data_ptr(), v.data_ptr(), _I64x4(*stride[:4]), n_pages, page_size, M, B,
         _need(table, "table", i32, (B, M), dev), _need(lens, "lens", i32, (B,), dev), _need(ref, "ref", i32, (n_pages,), dev), n,
         _need(parent, "parent", i32, (n,), dev), _need(n_new, "n_new", i32, (n,), dev), _need(table_out, "table_out", i32, (n, M), dev),
         _need(lens_out, "lens_out", i32, (n,), dev), _need(ref_out, "ref_out", i32, (n_pages,), dev),
@@ -905,35 +907,37 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, n_out: int, *, done:
     history [B * K, cap] int32 with n_history [B * K] filled entries follows into history_out
     [B * n_out, cap].  Returns {"scores", "parent" (b * K + beam), "token", "done"} [B, n_out], and
     with a history {"history", "n_history"}."""
-    if logits.dim() != 3 or logits.stride(2) != 1 or (min(logits.shape[:2]) > 1 and logits.stride(0) != logits.shape[1] * logits.stride(1)):
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, K, V]")
+    (B, K, V), (sb, sk, one) = logits.shape, logits.stride()
+    if one != 1 or (B > 1 and K > 1 and sb != K * sk):
         raise ValueError("logits must be [B, K, V] with contiguous rows at one distance")
-    B, K, V = logits.shape
     dev = _gpu(logits)
     if n_out < 1:
         raise ValueError("n_out must be at least 1")
     if (history is None) != (n_history is None) or (history is None and history_out is not None):
         raise ValueError("history, n_history and history_out go together")
-    row = logits.stride(1) if K > 1 else logits.stride(0)
-    row = max(row, V) if B * K == 1 else row
+    row = sk if K > 1 else (sb if B > 1 else V)
     i32 = torch.int32
-    ints = torch.empty(3, B, n_out, dtype=i32, device=dev)
     best = torch.empty(B, n_out, dtype=torch.float32, device=dev)
-    res = {"scores": best, "parent": ints[0], "token": ints[1], "done": ints[2]}
-    cap = 0
+    parent, token, ended = torch.empty(3, B, n_out, dtype=i32, device=dev).unbind(0)
+    res = {"scores": best, "parent": parent, "token": token, "done": ended}
+    cap, n_history_out = 0, None
     if history is not None:
         if history.dim() != 2 or history.shape[0] != B * K:
             raise ValueError("history must be [B * K, cap]")
         cap = history.shape[1]
         if history_out is None:
             history_out = torch.empty(B * n_out, cap, dtype=i32, device=dev)
-        res["history"], res["n_history"] = history_out, torch.empty(B * n_out, dtype=i32, device=dev)
+        n_history_out = torch.empty(B * n_out, dtype=i32, device=dev)
+        res["history"], res["n_history"] = history_out, n_history_out
     wsz = _size("spider_beam_select_workspace_size", B, K, n_out, V)
     workspace, wptr = _scratch(workspace, wsz, dev)
     _on(dev, lib().spider_beam_select, B, K, n_out, V, logits.data_ptr(), row, _dt(logits),
         _need(scores, "scores", torch.float32, (B, K), dev), _need(done, "done", i32, (B, K), dev), eos, best.data_ptr(),
-        ints[0].data_ptr(), ints[1].data_ptr(), ints[2].data_ptr(), _need(history, "history", i32, (B * K, cap), dev), cap,
+        parent.data_ptr(), token.data_ptr(), ended.data_ptr(), _need(history, "history", i32, (B * K, cap), dev), cap,
         _need(n_history, "n_history", i32, (B * K,), dev), cap, _need(history_out, "history_out", i32, (B * n_out, cap), dev), cap,
-        _ptr(res.get("n_history")), wptr, wsz)
+        None if n_history_out is None else n_history_out.data_ptr(), wptr, wsz)
     return res
 
 

@@ -29,7 +29,7 @@ struct BeamArgs {
   int32_t* token;
   int32_t* done_out;
   double* sums;     // [B*K][pieces] sum of e^(x - top)
-  float* tops;      // [B*K][pieces] an integer near the largest logit, or +-inf
+  float* tops;      // [B*K][pieces] the largest logit
   uint64_t* lists;  // [B*K][pieces][M] best logits in order, see beam_key
   const int32_t* history;
   const int32_t* n_history;
@@ -56,24 +56,21 @@ __device__ __forceinline__ uint64_t wave_best(uint64_t key) {
   return ((uint64_t)((uint32_t)top ^ 0x80000000u) << 32) | ((uint32_t)wave_max_int(lo) ^ 0x80000000u);
 }
 
-// e^d, d <= 1/2: the product with log2 e in two parts, so that what is left of an error is that
-// of the exponential instruction (1 unit in the last place) and no multiple of |d|.
-__device__ __forceinline__ float exp_accurate(float d) {
-  const float t = d * 1.44269504088896340736f;
-  const float r = fmaf(d, 1.44269504088896340736f, -t) + d * 1.92596299112661746887e-8f;
-  const float e = __builtin_amdgcn_exp2f(t);
-  return d > -200.f ? fmaf(e, r * 0.69314718055994530942f, e) : 0.f;
-}
-
 // Whether beam (row) takes part: a finite score and not finished.
 __device__ __forceinline__ bool beam_open(const BeamArgs& a, int row) { return !(a.done && a.done[row]) && fabsf(a.scores[row]) < INFINITY; }
 
-// A block per piece of a row.  Every thread holds 32 logits.  A bound below the M-th largest of
-// the piece: in each wave the M-th largest of its lanes' maxima, to 16 bits, found bit by bit with
-// ballots; the largest of the waves' bounds.  What reaches it (about 4 M logits) is ranked.
-template <typename LT, int VEC>
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A block per piece of a row.  Every thread holds 32 logits, read 16 bytes at a time wherever the
+// row starts: the order of the sum depends on the tokens alone, so that equal rows have equal
+// sums and beams with them come in their order.  The exponentials' arguments x - top are exact or small for the terms that
+// count; four exponentials are added in fp32, those sums in fp64.
+// A bound below the M-th largest of the piece: in each wave the M-th largest of its lanes'
+// maxima, to 16 bits, found bit by bit with ballots; the largest of the waves' bounds.  What
+// reaches it (about 4 M logits) is ranked.  512 rows of 151000 bf16 logits, M = 8: see below.
+template <typename LT>
 __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
-  constexpr int PER = kBeamPiece / 256;
+  constexpr int PER = kBeamPiece / 256, VEC = 16 / sizeof(LT);
   __shared__ uint64_t cand[kCand];
   __shared__ double sums[4];
   __shared__ float tops[4];
@@ -85,31 +82,33 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
   const int v0 = blockIdx.x * kBeamPiece, n = min(kBeamPiece, a.V - v0);
   const LT* x0 = reinterpret_cast<const LT*>(a.logits) + row * a.stride + v0;
   if (tid == 0) n_cand = 0;
+  auto value = [&](LT y) {
+    float f;
+    if constexpr (sizeof(LT) == 2) f = bf16_bits_to_f32(y);
+    else f = y;
+    return fmaxf(f, -INFINITY);  // NaN: -inf
+  };
   float x[PER];
-  // token of value i of the thread
+  // place of value i of the thread within the piece
   auto at = [&](int i) { return (i / VEC * 256 + tid) * VEC + i % VEC; };
 #pragma unroll
   for (int u = 0; u < PER / VEC; ++u) {
     const int i = (u * 256 + tid) * VEC;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) x[u * VEC + e] = -INFINITY;
-    if (i < n) {  // VEC > 1: rows are whole pieces of VEC
-      struct alignas(sizeof(LT) * VEC) Pack {
+    if (i + VEC <= n) {
+      struct __attribute__((packed, aligned(sizeof(LT)))) Pack {
         LT y[VEC];
       };
       const Pack p = *reinterpret_cast<const Pack*>(x0 + i);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        float y;
-        if constexpr (sizeof(LT) == 2) y = bf16_bits_to_f32(p.y[e]);
-        else y = p.y[e];
-        x[u * VEC + e] = y != y ? -INFINITY : y;
-      }
+      for (int e = 0; e < VEC; ++e) x[u * VEC + e] = value(p.y[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[u * VEC + e] = i + e < n ? value(x0[i + e]) : -INFINITY;
     }
   }
-  float mx = -INFINITY;
+  float mx = x[0];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) mx = fmaxf(mx, x[i]);
+  for (int i = 1; i < PER; ++i) mx = fmaxf(mx, x[i]);
   const uint32_t key16 = float_order_key(mx) >> 16;
   uint32_t bound = 0;
 #pragma unroll
@@ -123,20 +122,26 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
     bounds[wave] = bound;
   }
   __syncthreads();
-  // an integer: the differences of the logits that count are then exact
-  const float top = rintf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+  const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   bound = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3]));
+  // the smallest logit of that bound (-inf and what lies below reach none)
+  const float least = bound <= 0x007Fu ? -3.40282347e38f : beam_logit((uint64_t)bound << 48);
   double sum = 0.0;
 #pragma unroll
+  for (int i = 0; i < PER; i += 4) {
+    float e[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f((x[i + j] - top) * kLog2e);
+    sum += (double)((e[0] + e[1]) + (e[2] + e[3]));
+  }
+#pragma unroll
   for (int i = 0; i < PER; ++i) {
-    sum += (double)exp_accurate(x[i] - top);
-    const bool in = (float_order_key(x[i]) >> 16) >= bound && x[i] > -INFINITY;
-    if (__any(in)) {
-      const uint64_t mask = __ballot(in);
+    const uint64_t mask = __ballot(x[i] >= least);
+    if (mask) {
       int base = 0;
       if (lane == 0) base = atomicAdd(&n_cand, (int)__popcll(mask));
       base = __builtin_amdgcn_readfirstlane(base) + (int)__popcll(mask & ((1ull << lane) - 1ull));
-      if (in && base < kCand) cand[base] = beam_key(x[i], v0 + at(i));
+      if (((mask >> lane) & 1ull) && base < kCand) cand[base] = beam_key(x[i], v0 + at(i));
     }
   }
 #pragma unroll
@@ -180,14 +185,37 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
   }
 }
 
+// New beam `row`: its parent's history, then its token; entries i0, i0 + by, ..
+__device__ __forceinline__ void beam_history(const BeamArgs& a, int row, int parent, int token, int i0, int by) {
+  const int n = parent < 0 ? 0 : min(max(a.n_history[parent], 0), a.cap);
+  const int more = parent >= 0 && !(a.done && a.done[parent]) && n < a.cap ? 1 : 0;
+  const int32_t* from = a.history + max(parent, 0) * a.h_stride;
+  int32_t* to = a.history_out + row * a.ho_stride;
+  int i = i0;
+  for (; i + 3 * by < n; i += 4 * by) {
+    int x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = from[i + u * by];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) to[i + u * by] = x[u];
+  }
+  for (; i < n; i += by) to[i] = from[i];
+  if (i0 == 0) {
+    if (more) to[n] = token;
+    a.n_history_out[row] = n + more;
+  }
+}
+
 // A block per sample: a wave per beam joins its pieces' lists, then every entry of the beams'
 // lists finds its rank by a binary search in each of them.
 constexpr int kStage = 512;  // list entries of a wave in LDS
+template <bool HISTORY>
 __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
   extern __shared__ double value[];  // [K][M]
   int* token = reinterpret_cast<int*>(value + a.K * a.M);
   __shared__ uint64_t stage[16][kStage];
   __shared__ int counts[kMaxBeams];
+  __shared__ int2 chosen[kMaxBeams];  // (parent, token) of the new beams
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int k = wave; k < a.K; k += 16) {
     const int row = b * a.K + k;
@@ -255,6 +283,7 @@ __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
     a.scores_out[to] = (float)x;
     a.parent[to] = b * a.K + k;
     a.token[to] = token[i];
+    chosen[rank] = make_int2(b * a.K + k, token[i]);
     a.done_out[to] = (a.done && a.done[b * a.K + k]) || (a.eos >= 0 && token[i] == a.eos) ? 1 : 0;
   }
   for (int r = total + tid; r < a.M; r += 1024) {
@@ -262,24 +291,23 @@ __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
     a.scores_out[to] = -INFINITY;
     a.parent[to] = -1;
     a.token[to] = -1;
+    chosen[r] = make_int2(-1, -1);
     a.done_out[to] = 1;
+  }
+  if constexpr (HISTORY) {
+    __syncthreads();
+    for (int r = wave; r < a.M; r += 16) beam_history(a, b * a.M + r, chosen[r].x, chosen[r].y, lane, 64);
   }
 }
 
-// A block row per new beam: its parent's history, then its token.
+// A row of blocks per new beam.
 __global__ void __launch_bounds__(256) beam_history_kernel(BeamArgs a) {
-  const int row = blockIdx.y, parent = a.parent[row];
-  const int n = parent < 0 ? 0 : min(max(a.n_history[parent], 0), a.cap);
-  const int more = parent >= 0 && !(a.done && a.done[parent]) && n < a.cap ? 1 : 0;
-  const int i0 = blockIdx.x * 1024 + threadIdx.x;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int i = i0 + 256 * u;
-    if (i < n) a.history_out[row * a.ho_stride + i] = a.history[parent * a.h_stride + i];
-    else if (i < n + more) a.history_out[row * a.ho_stride + i] = a.token[row];
-  }
-  if (i0 == 0) a.n_history_out[row] = n + more;
+  const int row = blockIdx.y;
+  beam_history(a, row, a.parent[row], a.token[row], blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
+
+// Entries of history that a wave copies at the end of the join, at most.
+constexpr int kWithJoin = 4096;
 
 size_t beam_layout(int B, int K, int M, int V, char* at, BeamArgs* a) {
   const size_t n = (size_t)B * K * ceil_div(V, kBeamPiece);
@@ -294,11 +322,6 @@ size_t beam_layout(int B, int K, int M, int V, char* at, BeamArgs* a) {
 
 bool beam_shape_ok(int B, int K, int M, int V) {
   return B >= 1 && K >= 1 && M >= 1 && V >= 1 && K <= kMaxBeams && M <= kMaxBeams && V <= kBeamMaxV && (int64_t)B * K <= 65535 && (int64_t)B * M <= 65535;
-}
-
-template <typename LT, int VEC>
-void launch_beam_scan(const BeamArgs& a, hipStream_t st) {
-  beam_scan_kernel<LT, VEC><<<dim3((unsigned)a.pieces, (unsigned)(a.B * a.K)), 256, 0, st>>>(a);
 }
 
 }  // namespace
@@ -355,21 +378,18 @@ extern "C" spider_status spider_beam_select(int B, int K, int n_out, int V, cons
   a.B = B, a.K = K, a.M = n_out, a.V = V, a.eos = eos, a.pieces = ceil_div(V, kBeamPiece), a.cap = history_cap;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_BEAM_SELECT, st);
-  // four logits at a time where every row starts on their boundary and has a multiple of 4
-  const uintptr_t four = dtype == SPIDER_BF16 ? 8 : 16;
-  const bool vec = V % 4 == 0 && (B * K == 1 || logits_stride % 4 == 0) && reinterpret_cast<uintptr_t>(logits) % four == 0;
-  if (dtype == SPIDER_BF16) {
-    if (vec) launch_beam_scan<uint16_t, 4>(a, st);
-    else launch_beam_scan<uint16_t, 1>(a, st);
-  } else {
-    if (vec) launch_beam_scan<float, 4>(a, st);
-    else launch_beam_scan<float, 1>(a, st);
-  }
+  const dim3 grid((unsigned)a.pieces, (unsigned)(B * K));
+  if (dtype == SPIDER_BF16) beam_scan_kernel<uint16_t><<<grid, 256, 0, st>>>(a);
+  else beam_scan_kernel<float><<<grid, 256, 0, st>>>(a);
   SPIDER_LAUNCHED("beam_scan");
-  beam_join_kernel<<<(unsigned)B, 1024, (unsigned)(K * n_out * (sizeof(double) + sizeof(int))), st>>>(a);
+  // Short histories go with the join, a wave per new beam.
+  const bool with = any && (int64_t)ceil_div(n_out, 16) * history_cap <= kWithJoin;
+  const unsigned lds = (unsigned)(K * n_out * (sizeof(double) + sizeof(int)));
+  if (with) beam_join_kernel<true><<<(unsigned)B, 1024, lds, st>>>(a);
+  else beam_join_kernel<false><<<(unsigned)B, 1024, lds, st>>>(a);
   SPIDER_LAUNCHED("beam_join");
-  if (any) {
-    beam_history_kernel<<<dim3((unsigned)ceil_div(history_cap, 1024), (unsigned)(B * n_out)), 256, 0, st>>>(a);
+  if (any && !with) {
+    beam_history_kernel<<<dim3((unsigned)std::min(ceil_div(history_cap, 1024), 1024), (unsigned)(B * n_out)), 256, 0, st>>>(a);
     SPIDER_LAUNCHED("beam_history");
   }
   return SPIDER_OK;

@@ -78,17 +78,42 @@ __device__ __forceinline__ int2 block_prefix(int x, int* waves) {
   return make_int2(before + y - x, total);
 }
 
-// One block: who copies, how many pages each sequence takes, the lowest free pages, and who
-// gets which.
+// One block: who copies, how many pages each sequence takes, the lowest free pages, and who gets
+// which.  WHOLE: it counts the references too, in LDS, a wave per sequence, so that the step is
+// one launch and the copies.
+template <bool WHOLE>
 __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
   __shared__ int last[kForkMaxB], start[kForkMaxB + 1];  // the page a sequence writes into; its place among the pages taken
   __shared__ int waves[16];
+  extern __shared__ int counts[];
   const int tid = threadIdx.x, P = 1 << a.shift;
+  int32_t* ref = WHOLE ? counts : a.ref_out;
+  if constexpr (WHOLE) {
+    for (int p = tid; p < a.n_pages; p += 1024) ref[p] = a.ref_in[p];
+    __syncthreads();
+    for (int r = tid / 64; r < a.B_in + a.B_out; r += 16) {
+      const bool old = r < a.B_in;
+      const int b = old ? r : r - a.B_in;
+      const int2 from = old ? make_int2(b, fork_len(a, b)) : fork_from(a, b);
+      const int n = fork_pages(a, from.y);
+      for (int i = tid & 63; i < (old ? n : a.max_pages); i += 64) {
+        const int page = i < n ? a.table_in[(int64_t)from.x * a.max_pages + i] : -1;
+        const bool held = (uint32_t)page < (uint32_t)a.n_pages;
+        if (!old) a.table_out[(int64_t)b * a.max_pages + i] = held ? page : -1;
+        if (held) atomicAdd(ref + page, old ? -1 : 1);
+      }
+    }
+  }
+  const auto load = [&](int p) {
+    if constexpr (WHOLE) return ref[p];
+    else return fork_load(ref + p);
+  };
   for (int b = tid; b < a.B_out; b += 1024) {
     const int2 from = fork_from(a, b);
     const int grown = from.x < 0 ? 0 : (int)min((int64_t)from.y + (a.n_new ? max(a.n_new[b], 0) : 0), (int64_t)a.max_pages << a.shift);
     a.lens_out[b] = grown;
-    last[b] = grown > from.y && from.y % P ? a.table_out[(int64_t)b * a.max_pages + (from.y >> a.shift)] : -1;
+    const int page = grown > from.y && from.y % P ? a.table_in[(int64_t)from.x * a.max_pages + (from.y >> a.shift)] : -1;
+    last[b] = (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
   }
   __syncthreads();
   // The first writer of a page keeps it if nobody but the writers holds it.
@@ -106,7 +131,7 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
           same += last[u] == page;
           before += last[u] == page && u < b;
         }
-        if (before > 0 || fork_load(a.ref_out + page) > same) copies |= 1u << i;
+        if (before > 0 || load(page) > same) copies |= 1u << i;
       }
       need = fork_pages(a, a.lens_out[b]) - fork_pages(a, from.y) + ((copies >> i) & 1u);
     }
@@ -116,12 +141,12 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
   }
   if (tid == 0) start[a.B_out] = taken;
   for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i)
-    if ((copies >> i) & 1u) atomicSub(a.ref_out + last[b], 1);
+    if ((copies >> i) & 1u) atomicSub(ref + last[b], 1);
   __syncthreads();
   int found = 0;
   for (int p0 = 0; p0 < a.n_pages && found < taken; p0 += 1024) {
     const int p = p0 + tid;
-    const bool open = p < a.n_pages && fork_load(a.ref_out + p) <= 0;
+    const bool open = p < a.n_pages && load(p) <= 0;
     const int2 at = block_prefix(open, waves);
     if (open && found + at.x < taken) a.free_list[found + at.x] = p;
     found += at.y;
@@ -136,12 +161,16 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
       const int page = n < found ? a.free_list[n] : -1, j = n - start[b];
       const int at = copy && j == 0 ? from.y >> a.shift : fork_pages(a, from.y) + j - copy;
       a.table_out[(int64_t)b * a.max_pages + at] = page;
-      if (page >= 0) a.ref_out[page] = 1;
+      if (page >= 0) ref[page] = 1;
       if (copy && j == 0) c = make_int4(last[b], page, from.y % P, 0);
     }
     a.copies[b] = c;
   }
   if (tid == 0) a.missing[0] = taken - found;
+  if constexpr (WHOLE) {
+    __syncthreads();
+    for (int p = tid; p < a.n_pages; p += 1024) a.ref_out[p] = ref[p];
+  }
 }
 
 struct ForkCopyArgs {
@@ -165,6 +194,9 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(ForkCopyArgs a) {
   *reinterpret_cast<u32x4*>(a.kv[0] + at + copy.y * a.sp) = k;
   *reinterpret_cast<u32x4*>(a.kv[1] + at + copy.y * a.sp) = v;
 }
+
+// Pools and tables that one block counts.
+constexpr int kForkLdsPages = 16384, kForkLdsEntries = 65536;
 
 bool fork_shape_ok(int B_out, int n_pages) { return B_out >= 1 && B_out <= kForkMaxB && n_pages >= 1; }
 
@@ -233,11 +265,15 @@ extern "C" spider_status spider_pages_fork(int L, int Hkv, int dh, spider_dtype 
   while ((1 << a.shift) < page_size) ++a.shift;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   ProfScope ps(KC_PAGES_FORK, st);
-  fork_refs_kernel<<<(unsigned)((n_pages + 255LL) / 256), 256, 0, st>>>(a);
-  SPIDER_LAUNCHED("fork_refs");
-  fork_tables_kernel<<<dim3((unsigned)ceil_div(max_pages, 256), (unsigned)(B_in + B_out)), 256, 0, st>>>(a);
-  SPIDER_LAUNCHED("fork_tables");
-  fork_assign_kernel<<<1, 1024, 0, st>>>(a);
+  if (n_pages <= kForkLdsPages && (int64_t)(B_in + B_out) * max_pages <= kForkLdsEntries) {
+    fork_assign_kernel<true><<<1, 1024, (unsigned)(n_pages * sizeof(int32_t)), st>>>(a);
+  } else {
+    fork_refs_kernel<<<(unsigned)((n_pages + 255LL) / 256), 256, 0, st>>>(a);
+    SPIDER_LAUNCHED("fork_refs");
+    fork_tables_kernel<<<dim3((unsigned)ceil_div(max_pages, 256), (unsigned)(B_in + B_out)), 256, 0, st>>>(a);
+    SPIDER_LAUNCHED("fork_tables");
+    fork_assign_kernel<false><<<1, 1024, 0, st>>>(a);
+  }
   SPIDER_LAUNCHED("fork_assign");
   if (n_new) {  // (a sequence that takes no new slots copies nothing)
     ForkCopyArgs c{{reinterpret_cast<char*>(k), reinterpret_cast<char*>(v)}, a.copies, s[0], s[1], s[2], s[3], B_out, Hkv, dh * es / 16, page_size * Hkv * (dh * es / 16),
