@@ -91,19 +91,30 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
   float x[PER];
   // place of value i of the thread within the piece
   auto at = [&](int i) { return (i / VEC * 256 + tid) * VEC + i % VEC; };
+  struct __attribute__((packed, aligned(sizeof(LT)))) Pack {
+    LT y[VEC];
+  };
+  if (n == kBeamPiece) {  // every load before the first conversion
+    Pack p[PER / VEC];
 #pragma unroll
-  for (int u = 0; u < PER / VEC; ++u) {
-    const int i = (u * 256 + tid) * VEC;
-    if (i + VEC <= n) {
-      struct __attribute__((packed, aligned(sizeof(LT)))) Pack {
-        LT y[VEC];
-      };
-      const Pack p = *reinterpret_cast<const Pack*>(x0 + i);
+    for (int u = 0; u < PER / VEC; ++u) p[u] = *reinterpret_cast<const Pack*>(x0 + (u * 256 + tid) * VEC);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[u * VEC + e] = value(p.y[e]);
-    } else {
+    for (int i = 0; i < PER; ++i) x[i] = value(p[i / VEC].y[i % VEC]);
+  } else {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[u * VEC + e] = i + e < n ? value(x0[i + e]) : -INFINITY;
+    for (int u = 0; u < PER / VEC; ++u) {
+      const int i = (u * 256 + tid) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[u * VEC + e] = -INFINITY;
+      if (i + VEC <= n) {
+        const Pack p = *reinterpret_cast<const Pack*>(x0 + i);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u * VEC + e] = value(p.y[e]);
+      } else if (i < n) {
+#pragma unroll
+        for (int e = 0; e < VEC - 1; ++e)
+          if (i + e < n) x[u * VEC + e] = value(x0[i + e]);
+      }
     }
   }
   float mx = x[0];
@@ -185,25 +196,28 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
   }
 }
 
-// New beam `row`: its parent's history, then its token; entries i0, i0 + by, ..
-__device__ __forceinline__ void beam_history(const BeamArgs& a, int row, int parent, int token, int i0, int by) {
-  const int n = parent < 0 ? 0 : min(max(a.n_history[parent], 0), a.cap);
-  const int more = parent >= 0 && !(a.done && a.done[parent]) && n < a.cap ? 1 : 0;
+// New beam `row`: its parent's first n entries of history, then its token if `more`; entries i0,
+// i0 + by, ..
+__device__ __forceinline__ void beam_history(const BeamArgs& a, int row, int parent, int n, int more, int token, int i0, int by) {
   const int32_t* from = a.history + max(parent, 0) * a.h_stride;
   int32_t* to = a.history_out + row * a.ho_stride;
-  int i = i0;
-  for (; i + 3 * by < n; i += 4 * by) {
+  for (int i = i0; i < n; i += 4 * by) {
     int x[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = from[i + u * by];
+    for (int u = 0; u < 4; ++u) x[u] = from[min(i + u * by, n - 1)];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) to[i + u * by] = x[u];
+    for (int u = 0; u < 4; ++u)
+      if (i + u * by < n) to[i + u * by] = x[u];
   }
-  for (; i < n; i += by) to[i] = from[i];
   if (i0 == 0) {
     if (more) to[n] = token;
     a.n_history_out[row] = n + more;
   }
+}
+// The entries of history of beam `parent`, and whether its continuations get another one.
+__device__ __forceinline__ int2 beam_filled(const BeamArgs& a, int parent) {
+  const int n = parent < 0 ? 0 : min(max(a.n_history[parent], 0), a.cap);
+  return make_int2(n, parent >= 0 && !(a.done && a.done[parent]) && n < a.cap ? 1 : 0);
 }
 
 // A block per sample: a wave per beam joins its pieces' lists, then every entry of the beams'
@@ -216,7 +230,9 @@ __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
   __shared__ uint64_t stage[16][kStage];
   __shared__ int counts[kMaxBeams];
   __shared__ int2 chosen[kMaxBeams];  // (parent, token) of the new beams
+  __shared__ int2 filled[kMaxBeams];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (HISTORY && tid < a.K) filled[tid] = beam_filled(a, b * a.K + tid);
   for (int k = wave; k < a.K; k += 16) {
     const int row = b * a.K + k;
     const float score = a.scores[row];
@@ -296,14 +312,21 @@ __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
   }
   if constexpr (HISTORY) {
     __syncthreads();
-    for (int r = wave; r < a.M; r += 16) beam_history(a, b * a.M + r, chosen[r].x, chosen[r].y, lane, 64);
+    const int each = a.M < 16 ? 16 / a.M : 1;  // waves per row
+    for (int r = wave / each; r < a.M; r += 16 / each)
+      if (wave < each * (16 / each)) {
+        const int parent = chosen[r].x;
+        const int2 f = parent < 0 ? make_int2(0, 0) : filled[parent - b * a.K];
+        beam_history(a, b * a.M + r, parent, f.x, f.y, chosen[r].y, wave % each * 64 + lane, 64 * each);
+      }
   }
 }
 
 // A row of blocks per new beam.
 __global__ void __launch_bounds__(256) beam_history_kernel(BeamArgs a) {
-  const int row = blockIdx.y;
-  beam_history(a, row, a.parent[row], a.token[row], blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+  const int row = blockIdx.y, parent = a.parent[row];
+  const int2 f = beam_filled(a, parent);
+  beam_history(a, row, parent, f.x, f.y, a.token[row], blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 // Entries of history that a wave copies at the end of the join, at most.
@@ -382,7 +405,7 @@ extern "C" spider_status spider_beam_select(int B, int K, int n_out, int V, cons
   if (dtype == SPIDER_BF16) beam_scan_kernel<uint16_t><<<grid, 256, 0, st>>>(a);
   else beam_scan_kernel<float><<<grid, 256, 0, st>>>(a);
   SPIDER_LAUNCHED("beam_scan");
-  // Short histories go with the join, a wave per new beam.
+  // Short histories go with the join, a wave or more per new beam.
   const bool with = any && (int64_t)ceil_div(n_out, 16) * history_cap <= kWithJoin;
   const unsigned lds = (unsigned)(K * n_out * (sizeof(double) + sizeof(int)));
   if (with) beam_join_kernel<true><<<(unsigned)B, 1024, lds, st>>>(a);

@@ -422,17 +422,25 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
   }
 }
 
+// 16-byte piece c of key j of a tile lies at piece c ^ swizzle(j).  The eight keys that half a wave
+// reads two pieces of each (values) then lie in eight different places of two pieces, and one
+// piece of 16 keys (keys) in 16 different ones, or eight in each half of the banks at width 64.
+// (With c ^ (j % 16), keys 2i and 2i + 1 shared the banks of a value read.)
+template <int DH>
+__device__ __forceinline__ int swizzle(int j) {
+  return DH == 64 ? ((j & 6) | ((j >> 3) & 1)) : (((j << 1) & 14) | ((j >> 3) & 1));
+}
+
 // Many rows (bf16): NW waves of 32 (dh <= 128) or 16 rows each share the keys and values, which
 // come through LDS by DMA, two tiles ahead.  A tile is 32 rows of DH channels for keys and as many
-// for values; 16-byte piece c of key j lies at piece c ^ (j % 16 or less), so that both the reads
-// of one piece of 16 keys and those of all pieces of a key spread over the banks.
+// for values.
 template <int DH, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l) {
   constexpr int RT = DH == 256 ? 1 : 2;
   using Rows = ChunkRows<uint16_t, DH, RT>;
   using T = typename Rows::T;
   constexpr int CPL = T::CPL, ROWS = 16 * RT * NW;
-  constexpr int PIECES = DH / 8, SWZ = PIECES < 16 ? PIECES - 1 : 15;  // 16-byte pieces of a row
+  constexpr int PIECES = DH / 8;  // 16-byte pieces of a row
   constexpr int KPD = 64 / PIECES;                                       // keys of a DMA
   constexpr int TILE = 32 * DH, STAGES = 3;                             // elements of a key or value tile
   __shared__ __align__(16) uint16_t buf[STAGES][2][TILE];
@@ -457,7 +465,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a, Ch
     int64_t at[4];
     const uint32_t found = tile_at<32>(a, ids, 32 * t, at);
     auto from = [&](int part) {
-      const int j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ (j & SWZ), u = part * KPD / 8;
+      const int j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ swizzle<DH>(j), u = part * KPD / 8;
       const int64_t off = u == 0 ? at[0] : (u == 1 ? at[1] : (u == 2 ? at[2] : at[3]));
       return off + (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
     };
@@ -494,7 +502,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a, Ch
 #pragma unroll
       for (int i = 0; i < T::NK; ++i) {
         const int c = 4 * i + g;
-        u32x4 x = *reinterpret_cast<const u32x4*>(ks + (16 * u + m) * DH + 8 * (c ^ (m & SWZ)));
+        u32x4 x = *reinterpret_cast<const u32x4*>(ks + (16 * u + m) * DH + 8 * (c ^ swizzle<DH>(m)));
         if (!FULL && c > last_piece) x = u32x4{0, 0, 0, 0};
         k.f[u][i] = __builtin_bit_cast(bf16x8, x);
       }
@@ -509,7 +517,7 @@ __global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a, Ch
       for (int e = 0; e < 2; ++e) {
         const int j = 16 * e + 4 * g + m / 4, piece = 2 * c + m % 4 / 2;
         const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ (j & SWZ)) + 4 * (m % 2)));
+            (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ swizzle<DH>(j)) + 4 * (m % 2)));
         const uint2 z = __builtin_bit_cast(uint2, y);
         x[2 * e] = z.x;
         x[2 * e + 1] = z.y;
@@ -628,13 +636,17 @@ struct ChunkPlan {
   size_t few_o, chunk_ml, chunk_o, bytes;
 };
 
-ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, spider_dtype dtype) {
+// slots: of the longest sequence, window (0: none): what a row sees of them.  (Fewer slots never
+// give more splits, so a workspace for all slots serves every window.)
+ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window, spider_dtype dtype) {
   ChunkPlan p{};
   const bool bf16 = dtype == SPIDER_BF16;
   const int64_t G = H / Hkv, R = N * G;  // rows of a kv head, R / B of an average sequence
   p.dhp = dh <= 64 ? 64 : (dh <= 128 ? 128 : 256);
   const int wave_rows = p.dhp == 256 ? 16 : 32, keys = bf16 ? 32 : 16;
-  const int most = std::max(1, ceil_div(slots, keys) / kMinTiles);  // splits of the longest sequence
+  // splits of the longest sequence, of row blocks of up to 256 rows
+  const int64_t reach = window > 0 ? std::min<int64_t>(slots, (int64_t)window + std::min<int64_t>(N, ceil_div(256, (int)G) + 1) + keys) : slots;
+  const int most = std::max(1, (int)((reach + keys - 1) / keys) / kMinTiles);
   size_t off = 0;
   if (!bf16 || R <= (int64_t)B * wave_rows) {
     p.rt = R <= (int64_t)B * 16 || p.dhp == 256 ? 1 : 2;
@@ -733,7 +745,7 @@ bool chunk_shape_ok(int N, int B, int H, int Hkv, int dh, spider_dtype dtype) {
 using namespace spider;
 
 extern "C" size_t spider_paged_attention_workspace_size(int N, int B, int H, int Hkv, int dh, int slots, spider_dtype dtype) {
-  return chunk_shape_ok(N, B, H, Hkv, dh, dtype) && slots >= 1 && slots <= (1 << 30) ? chunk_plan(N, B, H, Hkv, dh, slots, dtype).bytes : 0;
+  return chunk_shape_ok(N, B, H, Hkv, dh, dtype) && slots >= 1 && slots <= (1 << 30) ? chunk_plan(N, B, H, Hkv, dh, slots, 0, dtype).bytes : 0;
 }
 
 extern "C" spider_status spider_paged_attention(int N, int H, int Hkv, int dh, const void* q, int64_t q_stride,
@@ -755,7 +767,7 @@ extern "C" spider_status spider_paged_attention(int N, int H, int Hkv, int dh, c
   SPIDER_REQUIRE(q_stride % per16 == 0 && q_stride >= 0, SPIDER_ERR_INVALID_ARG, "spider_paged_attention: q_stride must be a multiple of 16 bytes");
   SPIDER_REQUIRE((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) % 16 == 0, SPIDER_ERR_INVALID_ARG,
                  "spider_paged_attention: q and out must be 16-byte aligned");
-  ChunkPlan p = chunk_plan(N, cache->B, H, Hkv, dh, cache->max_pages * cache->page_size, dtype);
+  ChunkPlan p = chunk_plan(N, cache->B, H, Hkv, dh, cache->max_pages * cache->page_size, window, dtype);
   SPIDER_REQUIRE(p.bytes == 0 || (workspace && workspace_bytes >= p.bytes), SPIDER_ERR_WORKSPACE,
                  "spider_paged_attention: workspace of %zu bytes needed, %zu given", p.bytes, workspace ? workspace_bytes : 0);
   SPIDER_REQUIRE(p.bytes == 0 || reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG,
