@@ -422,143 +422,222 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
   }
 }
 
-// 16-byte piece c of key j of a tile lies at piece c ^ swizzle(j).  The eight keys that half a wave
-// reads two pieces of each (values) then lie in eight different places of two pieces, and one
-// piece of 16 keys (keys) in 16 different ones, or eight in each half of the banks at width 64.
-// (With c ^ (j % 16), keys 2i and 2i + 1 shared the banks of a value read.)
+// 16-byte piece c of key j of a tile lies at piece c ^ swizzle(j).  16 lanes read one piece of 16
+// keys (keys: 16 different places), 32 lanes four pieces of four keys (values, transposing: again
+// 16 different places, in whole groups of four); at width 64 two keys share the 64 banks.
 template <int DH>
 __device__ __forceinline__ int swizzle(int j) {
-  return DH == 64 ? ((j & 6) | ((j >> 3) & 1)) : (((j << 1) & 14) | ((j >> 3) & 1));
+  return DH == 64 ? (((j & 2) << 1) | ((j & 4) >> 1) | ((j & 8) >> 3)) : (((j & 3) << 2) | ((j & 4) >> 1) | ((j & 8) >> 3));
 }
 
-// Many rows (bf16): NW waves of 32 (dh <= 128) or 16 rows each share the keys and values, which
-// come through LDS by DMA, two tiles ahead.  A tile is 32 rows of DH channels for keys and as many
-// for values.
+// Many rows (bf16): NW waves of 32 rows each share the keys and values, which come through LDS by
+// DMA.  A wave computes S^T = K Q^T and O^T += V^T P^T with 32x32x16 MFMAs on KT * 32 keys at a
+// time, so a lane owns row lane % 32 in both, with half h = lane / 32 of the keys: register r of a
+// product holds key (channel) r % 4 + 8 (r / 4) + 4 h.  Eight such registers are the operand of a
+// product over 16 keys as they stand, whose values are read transposed in the same order.
+// The sums of the rounded weights are products with ones on the 16x16x32 unit, half as many cycles:
+// it sees the rows 16 apart in one column, so one half of its ones serves each of them.
 template <int DH, int NW, bool FULL>
-__global__ void __launch_bounds__(64 * NW, 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l) {
-  constexpr int RT = DH == 256 ? 1 : 2;
-  using Rows = ChunkRows<uint16_t, DH, RT>;
-  using T = typename Rows::T;
-  constexpr int CPL = T::CPL, ROWS = 16 * RT * NW;
-  constexpr int PIECES = DH / 8;  // 16-byte pieces of a row
-  constexpr int KPD = 64 / PIECES;                                       // keys of a DMA
-  constexpr int TILE = 32 * DH, STAGES = 3;                             // elements of a key or value tile
-  __shared__ __align__(16) uint16_t buf[STAGES][2][TILE];
+__global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l) {
+  constexpr int KT = DH == 256 || NW == 2 ? 1 : 2, KEYS = 32 * KT, NK = DH / 16, CT = DH / 32, ROWS = 32 * NW;
+  constexpr int PIECES = DH / 8, KPD = 64 / PIECES;           // 16-byte pieces of a row, keys of a DMA
+  constexpr int TILE = KEYS * DH;                              // elements of a key or value tile
+  constexpr int AHEAD = KT == 2 && NW < 8 ? 1 : 2;             // tiles on their way during the products
+  constexpr int KD = TILE / 512 / NW, DMAS = 2 * KD;           // DMAs of a wave and tile
+  static_assert(KD >= 1, "every wave fetches");
+  __shared__ __align__(16) uint16_t buf[AHEAD + 1][2][TILE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int m = lane & 15, g = lane >> 4;
+  const int col = lane & 31, h = lane >> 5, m = lane & 15;
   ChunkWork w;
-  if (!chunk_work<32, ROWS, false>(a, l, w)) return;
+  if (!chunk_work<KEYS, ROWS, false>(a, l, w)) return;
   const uint16_t* kb = reinterpret_cast<const uint16_t*>(a.k) + w.hk * a.p.sh;
   const uint16_t* vb = reinterpret_cast<const uint16_t*>(a.v) + w.hk * a.p.sh;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
   const uint32_t lds0 = lds_offset(&buf[0][0][0]);
-  const int last_piece = a.dh / 8 - 1;
-  Rows rows;
-  rows.template start<FULL>(a, w, w.r0 + 16 * RT * wave, lane);
+  const int last_piece = a.dh / 8 - 1, G = a.H / a.Hkv;
+
+  // the wave's rows
+  const int r0 = w.r0 + 32 * wave, rr = min(r0 + col, w.R - 1), p0 = w.s.len - w.s.rows, pos = p0 + rr / G;
+  const int first = p0 + min(r0, w.R - 1) / G, last = p0 + min(r0 + 31, w.R - 1) / G;
+  bf16x8 q[NK];
+  {
+    const uint16_t* row = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(w.s.start + rr / G) * a.qs + (int64_t)(w.hk * G + rr % G) * a.dh;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      u32x4 x = u32x4{0, 0, 0, 0};
+      if (FULL || 2 * i + h <= last_piece) x = *reinterpret_cast<const u32x4*>(row + 16 * i + 8 * h);
+      if (a.scale < 0.f) x ^= 0x80008000u;
+      q[i] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  floatx16 o[CT] = {};
+  floatx4 sum = {};
+  float top = -INFINITY;
+  int bad0 = 0x7fffffff, bad1 = -1;  // the first and last masked tile with an infinite or NaN value
+  const uint32_t one = (m >= 8) == ((lane >> 4) & 1) ? 0x3F803F80u : 0u;
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{one, one, one, one});
+
   PageIds ids;
   ids.start(a, w);
-  // A DMA of a wave fills 1 KB, KPD keys.  Every wave fetches the same keys and values, KD times
-  // (width 64 in 8 waves: once, keys or values).  A wave's keys lie within a group of eight.
-  constexpr int KD = DH / 16 / NW, DMAS = KD ? 2 * KD : 1;
+  // A DMA of a wave fills 1 KB: KPD keys, within a group of eight.
+  struct Present {
+    uint32_t x[KT];
+  };
   auto fetch = [&](int t) {
-    const uint32_t to = lds0 + (uint32_t)((t - w.t0) % STAGES * 4 * TILE);
-    int64_t at[4];
-    const uint32_t found = tile_at<32>(a, ids, 32 * t, at);
-    auto from = [&](int part) {
-      const int j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ swizzle<DH>(j), u = part * KPD / 8;
-      const int64_t off = u == 0 ? at[0] : (u == 1 ? at[1] : (u == 2 ? at[2] : at[3]));
-      return off + (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
-    };
-    if constexpr (KD > 0) {
+    const uint32_t to = lds0 + (uint32_t)((t - w.t0) % (AHEAD + 1) * 4 * TILE);
+    int64_t at[4 * KT];
+    Present found;
 #pragma unroll
-      for (int i = 0; i < KD; ++i) {
-        const int part = i * NW + wave;
-        const int64_t off = from(part);
-        dma16(kb + off, to + part * 1024);
-        dma16(vb + off, to + 2 * TILE + part * 1024);
-      }
-    } else {
-      const int part = wave % (NW / 2);
-      dma16((wave < NW / 2 ? kb : vb) + from(part), to + (wave < NW / 2 ? 0 : 2 * TILE) + part * 1024);
+    for (int s = 0; s < KT; ++s) {
+      int64_t (&part)[4] = *reinterpret_cast<int64_t (*)[4]>(at + 4 * s);
+      found.x[s] = tile_at<32>(a, ids, t * KEYS + 32 * s, part);
+    }
+#pragma unroll
+    for (int i = 0; i < KD; ++i) {
+      const int part = i * NW + wave, j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ swizzle<DH>(j), u = part * KPD / 8;
+      int64_t off = at[0];
+#pragma unroll
+      for (int e = 1; e < 4 * KT; ++e) off = u == e ? at[e] : off;
+      off += (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
+      dma16(kb + off, to + part * 1024);
+      dma16(vb + off, to + 2 * TILE + part * 1024);
     }
     return found;
   };
   dma_wait_all();  // the queries are here: from now on only the DMAs count as loads in flight
-  uint32_t present[3] = {};  // of this tile and the next two
-  if (w.t0 < w.t1) present[0] = fetch(w.t0);
-  if (w.t0 + 1 < w.t1) present[1] = fetch(w.t0 + 1);
+  Present present[AHEAD + 1] = {};  // of this tile and the next ones
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (w.t0 + i < w.t1) present[i] = fetch(w.t0 + i);
+
   int t = w.t0;
   auto step = [&](auto mask_) {
     constexpr bool mask = decltype(mask_)::value;
-    // tile t has landed, and every wave is done with tile t - 1, whose place tile t + 2 takes
-    if (t + 1 < w.t1) dma_wait_barrier<DMAS>();
+    // tile t has landed, and every wave is done with tile t - 1, whose place the next fetch takes
+    if (AHEAD == 2 && t + 1 < w.t1) dma_wait_barrier<DMAS>();
     else dma_wait_barrier<0>();
-    if (t + 2 < w.t1) present[2] = fetch(t + 2);
-    const uint16_t* ks = buf[(t - w.t0) % STAGES][0];
-    const uint16_t* vs = buf[(t - w.t0) % STAGES][1];
-    typename T::K k;
+    if (t + AHEAD < w.t1) present[AHEAD] = fetch(t + AHEAD);
+    const uint16_t* ks = buf[(t - w.t0) % (AHEAD + 1)][0];
+    const uint16_t* vs = buf[(t - w.t0) % (AHEAD + 1)][1];
+    floatx16 s[KT] = {};
 #pragma unroll
-    for (int u = 0; u < T::KT; ++u)
+    for (int i = 0; i < NK; ++i)
 #pragma unroll
-      for (int i = 0; i < T::NK; ++i) {
-        const int c = 4 * i + g;
-        u32x4 x = *reinterpret_cast<const u32x4*>(ks + (16 * u + m) * DH + 8 * (c ^ swizzle<DH>(m)));
-        if (!FULL && c > last_piece) x = u32x4{0, 0, 0, 0};
-        k.f[u][i] = __builtin_bit_cast(bf16x8, x);
+      for (int u = 0; u < KT; ++u) {
+        u32x4 x = *reinterpret_cast<const u32x4*>(ks + (32 * u + col) * DH + 8 * ((2 * i + h) ^ swizzle<DH>(col & 15)));
+        if (!FULL && 2 * i + h > last_piece) x = u32x4{0, 0, 0, 0};
+        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), q[i], s[u], 0, 0, 0);
       }
-    rows.scores(k);
-    // the value operands by transposing reads: 16 lanes read four keys of 16 channels, a lane
-    // gets the four keys of channel 16 n + lane % 16
-    typename T::Ops v;
+    uint32_t seen[KT];
+    if constexpr (mask) {
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) {
-      u32x4 x;
+      for (int u = 0; u < KT; ++u) {
+        seen[u] = chunk_window(present[0].x[u], pos, a.window, t * KEYS + 32 * u) >> (4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = (seen[u] >> (r % 4 + 8 * (r / 4))) & 1u ? s[u][r] : -INFINITY;
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int u = 0; u < KT; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
+    const float2 both = lanes_x32(mx);
+    mx = fmaxf(both.x, both.y);
+    if (__any(mx * sc > top * sc + kLazyMax || (top == -INFINITY && mx > -INFINITY))) {
+      const float nt = fmaxf(top, mx);
+      const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - nt) * sc);
+      top = nt;
+      sum *= __shfl(f, m + ((lane >> 5) << 4));
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[c] *= f;
+    }
+    const float mc = top == -INFINITY ? 0.f : top * sc;
+    bf16x8 p[2 * KT];  // weights of 16 keys each
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], sc, -mc));
+        if constexpr (mask) s[u][r] = (seen[u] >> (r % 4 + 8 * (r / 4))) & 1u ? s[u][r] : 0.f;
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int j = 16 * e + 4 * g + m / 4, piece = 2 * c + m % 4 / 2;
-        const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ swizzle<DH>(j)) + 4 * (m % 2)));
-        const uint2 z = __builtin_bit_cast(uint2, y);
-        x[2 * e] = z.x;
-        x[2 * e + 1] = z.y;
+        u32x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{s[u][8 * e + 2 * i], s[u][8 * e + 2 * i + 1]}, bf16x2v));
+        p[2 * u + e] = __builtin_bit_cast(bf16x8, x);
       }
-      v.f[c] = x;
     }
-    rows.template soften<mask>(present[0], a.window, 32 * t, g, sc);
-    rows.template add<mask>(v, t);
-    present[0] = present[1];
-    present[1] = present[2];
+    // 16 lanes read four keys of 16 channels, a lane gets the four keys of channel lane % 16
+    uint32_t bad = 0;
+#pragma unroll
+    for (int k = 0; k < 2 * KT; ++k) {
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[k], sum, 0, 0, 0);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        u32x4 x;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int j = 16 * k + 8 * e + 4 * h + m / 4, piece = 4 * c + 2 * ((lane >> 4) & 1) + m % 4 / 2;
+          const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ swizzle<DH>(j & 15)) + 4 * (m % 2)));
+          const uint2 z = __builtin_bit_cast(uint2, y);
+          x[2 * e] = z.x;
+          x[2 * e + 1] = z.y;
+        }
+        if constexpr (mask) {
+          // (infinite and NaN values must not reach the rows that do not see them, see below)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = AttnTile<uint16_t, DH>::finite(x[e], bad);
+        }
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), p[k], o[c], 0, 0, 0);
+      }
+    }
+    if constexpr (mask)
+      if (__any(bad != 0)) {
+        bad0 = min(bad0, t);
+        bad1 = max(bad1, t);
+      }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) present[i] = present[i + 1];
     ++t;
   };
+  // whether some row of the wave does not see some key of the tile
+  auto masked = [&] {
+    bool all = true;
+#pragma unroll
+    for (int u = 0; u < KT; ++u) all = all && present[0].x[u] == ~0u;
+    return !all || t * KEYS + KEYS - 1 > first || (a.window > 0 && t * KEYS <= last - a.window);
+  };
   while (t < w.t1) {
-    while (t < w.t1 && !rows.masked(present[0], a.window, 32 * t)) step(std::false_type{});
-    while (t < w.t1 && rows.masked(present[0], a.window, 32 * t)) step(std::true_type{});
+    while (t < w.t1 && !masked()) step(std::false_type{});
+    while (t < w.t1 && masked()) step(std::true_type{});
   }
 
+  const float total = __shfl(sum[0], m + ((col >> 4) << 5));
+  if (r0 + col >= w.R) return;
+  const int64_t out_row = chunk_row(a, w, rr), part_row = chunk_part(a, l, w, rr);
+  if (h == 0 && w.ns > 1) l.part_ml[part_row] = make_float2(top, total);
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const float sum = rows.row_sum(r);
-    const int rr = w.r0 + 16 * (RT * wave + r) + m;
-    if (rr >= w.R) continue;
-    const int64_t out_row = chunk_row(a, w, rr), part_row = chunk_part(a, l, w, rr);
-    if (g == 0 && w.ns > 1) l.part_ml[part_row] = make_float2(rows.top[r], sum);
+  for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int c = 0; c < CPL; ++c) {
-      const int ch = 16 * c + 4 * g;  // of four consecutive outputs
+    for (int i = 0; i < 4; ++i) {
+      const int ch = 32 * c + 8 * i + 4 * h;  // of four consecutive outputs
       if (!FULL && ch >= a.dh) continue;
-      if (w.ns > 1) *reinterpret_cast<floatx4*>(l.part_o + part_row * a.dh + ch) = rows.o[r][c];
-      else attn_store<uint16_t>(a.out, out_row * a.dh + ch, rows.o[r][c], sum);
+      const floatx4 x = floatx4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+      if (w.ns > 1) *reinterpret_cast<floatx4*>(l.part_o + part_row * a.dh + ch) = x;
+      else attn_store<uint16_t>(a.out, out_row * a.dh + ch, x, total);
     }
-  }
-  if (rows.bad0 > rows.bad1) return;
+  if (bad0 > bad1) return;
 #pragma unroll 1
-  for (int i = 0; i < RT * CPL * 4; ++i) {
-    const int rr = w.r0 + 16 * (RT * wave + i / (CPL * 4)) + m, ch = 16 * (i / 4 % CPL) + 4 * g + i % 4;
-    if (rr >= w.R || ch >= a.dh) continue;
-    const float s = seen_nonfinite<uint16_t, DH>(a, w.b, w.s, w.hk, rr, ch, rows.bad0 * 32, (rows.bad1 + 1) * 32);
-    if (fabsf(s) < INFINITY) continue;
-    if (w.ns > 1) l.part_o[chunk_part(a, l, w, rr) * a.dh + ch] = s;
-    else reinterpret_cast<uint16_t*>(a.out)[chunk_row(a, w, rr) * a.dh + ch] = (uint16_t)((__float_as_uint(s) >> 16) | (s != s ? 0x40u : 0u));
+  for (int i = 0; i < CT * 16; ++i) {
+    const int ch = 32 * (i / 16) + 8 * (i / 4 % 4) + 4 * h + i % 4;
+    if (ch >= a.dh) continue;
+    const float x = seen_nonfinite<uint16_t, DH>(a, w.b, w.s, w.hk, rr, ch, bad0 * KEYS, (bad1 + 1) * KEYS);
+    if (fabsf(x) < INFINITY) continue;
+    if (w.ns > 1) l.part_o[part_row * a.dh + ch] = x;
+    else reinterpret_cast<uint16_t*>(a.out)[out_row * a.dh + ch] = (uint16_t)((__float_as_uint(x) >> 16) | (x != x ? 0x40u : 0u));
   }
 }
 
@@ -643,12 +722,12 @@ ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window
   const bool bf16 = dtype == SPIDER_BF16;
   const int64_t G = H / Hkv, R = N * G;  // rows of a kv head, R / B of an average sequence
   p.dhp = dh <= 64 ? 64 : (dh <= 128 ? 128 : 256);
-  const int wave_rows = p.dhp == 256 ? 16 : 32, keys = bf16 ? 32 : 16;
+  const int keys = bf16 ? 32 : 16;
   // splits of the longest sequence, of row blocks of up to 256 rows
   const int64_t reach = window > 0 ? std::min<int64_t>(slots, (int64_t)window + std::min<int64_t>(N, ceil_div(256, (int)G) + 1) + keys) : slots;
   const int most = std::max(1, (int)((reach + keys - 1) / keys) / kMinTiles);
   size_t off = 0;
-  if (!bf16 || R <= (int64_t)B * wave_rows) {
+  if (!bf16 || R <= (int64_t)B * (p.dhp == 256 ? 16 : 32)) {
     p.rt = R <= (int64_t)B * 16 || p.dhp == 256 ? 1 : 2;
     p.limit = 0x7fffffff;
     const int rows = 16 * p.rt, blocks = (int)(R / rows);
@@ -674,14 +753,15 @@ ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window
       off = align_up(p.few_o + n * dh * sizeof(float), 256);
     }
   }
-  // (width 256 has no registers for two waves per SIMD)
-  p.nw = R <= (int64_t)B * 2 * wave_rows ? 2 : (R <= (int64_t)B * 4 * wave_rows || p.dhp == 256 ? 4 : 8);
-  const int rows = wave_rows * p.nw, at_once = p.dhp == 256 ? 256 : 256 * 8 / p.nw;  // blocks that run at once
+  // (width 256 has registers for one wave per SIMD)
+  p.nw = R <= (int64_t)B * 64 ? 2 : (R <= (int64_t)B * 128 || p.dhp == 256 ? 4 : 8);
+  const int rows = 32 * p.nw, at_once = p.dhp == 256 ? 256 : 256 * 8 / p.nw;  // blocks that run at once
   const int64_t blocks = Hkv * std::max<int64_t>(1, R / rows);
-  p.chunk = ChunkLaunch{nullptr, nullptr, keys, rows, (int)(R / rows) + B, 1, 0};
+  const int chunk_keys = p.dhp == 256 || p.nw == 2 ? 32 : 64;
+  p.chunk = ChunkLaunch{nullptr, nullptr, chunk_keys, rows, (int)(R / rows) + B, 1, 0};
   // The splits that leave the least of the last round of blocks empty; each costs its joining.
   double best = 1e30;
-  for (int s = 1; s <= std::min(most, 16); ++s) {
+  for (int s = 1; s <= std::min(std::max(1, most * keys / chunk_keys), 16); ++s) {
     const double rounds = (double)((blocks * s + at_once - 1) / at_once) / s * (1.0 + 0.03 * (s - 1));
     if (rounds < best) best = rounds, p.chunk.splits = s;
   }
