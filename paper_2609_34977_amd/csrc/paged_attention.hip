@@ -100,37 +100,39 @@ __device__ __forceinline__ bool chunk_work(const ChunkArgs& a, const ChunkLaunch
 struct PageIds {
   const int32_t* row;
   int last, n_pages, base, id;
+  uint64_t absent;  // lanes whose entry is no page
   __device__ __forceinline__ void start(const ChunkArgs& a, const ChunkWork& w) {
     row = a.p.table + w.b * a.p.table_stride;
     last = (w.s.len - 1) >> a.p.shift;
     n_pages = a.p.n_pages;
     base = -64;
   }
-  // entry i, the same in every lane and not below earlier ones; -1: absent
-  __device__ __forceinline__ int get(int i) {
-    if (i >= base + 64) {
-      base = i;
-      const int at = i + (int)(threadIdx.x & 63);
+  // the entries of n keys from j0 (no more than 64 of them, and not below earlier ones) at hand
+  __device__ __forceinline__ void cover(const ChunkArgs& a, int j0, int n) {
+    if ((j0 + n - 1) >> a.p.shift >= base + 64) {
+      base = j0 >> a.p.shift;
+      const int at = base + (int)(threadIdx.x & 63);
       id = at <= last ? row[at] : -1;
-      id = (uint32_t)id < (uint32_t)n_pages ? id : -1;
+      absent = __ballot((uint32_t)id >= (uint32_t)n_pages);
     }
-    return __builtin_amdgcn_readlane(id, i - base);
+  }
+  // where key j lies, in elements; an absent page's keys are read from page 0 and not seen
+  __device__ __forceinline__ int64_t at(const ChunkArgs& a, int j) const {
+    const int lane = (j >> a.p.shift) - base, page = (absent >> lane) & 1ull ? 0 : __builtin_amdgcn_readlane(id, lane);
+    return page * a.p.sp + (j & ((1 << a.p.shift) - 1)) * a.p.ss;
+  }
+  // which of the N keys from j0 (16 or 32), whose entries are at hand, there are
+  template <int N>
+  __device__ __forceinline__ uint32_t present(const ChunkArgs& a, int j0) const {
+    const int lane = (j0 >> a.p.shift) - base, n = ((j0 + N - 1) >> a.p.shift) - (j0 >> a.p.shift);  // pages after the first
+    const uint64_t gone = absent >> lane & ((2ull << n) - 1ull);
+    if (gone == 0) return N == 32 ? ~0u : 0xFFFFu;
+    uint32_t x = 0;
+#pragma unroll
+    for (int u = 0; u < N / 8; ++u) x |= (gone >> (((j0 + 8 * u) >> a.p.shift) - (j0 >> a.p.shift))) & 1ull ? 0u : 0xFFu << (8 * u);
+    return x;
   }
 };
-
-// Where the keys of a tile lie: element offsets of its groups of eight.  Returns which of its
-// keys there are (bits).  An absent page's keys are read from page 0 and not seen.
-template <int KEYS>
-__device__ __forceinline__ uint32_t tile_at(const ChunkArgs& a, PageIds& ids, int j0, int64_t (&off)[KEYS / 8]) {
-  uint32_t present = 0;
-#pragma unroll
-  for (int u = 0; u < KEYS / 8; ++u) {
-    const int j = j0 + 8 * u, id = ids.get(j >> a.p.shift);
-    present |= id >= 0 ? 0xFFu << (8 * u) : 0u;
-    off[u] = max(id, 0) * a.p.sp + (j & ((1 << a.p.shift) - 1)) * a.p.ss;
-  }
-  return present;
-}
 
 // Bits of the keys from j0 that a row at position pos sees, of those that are present.
 __device__ __forceinline__ uint32_t chunk_window(uint32_t present, int pos, int window, int j0) {
@@ -344,10 +346,16 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
   };
   const int each = (w.t1 - w.t0 + 3) / 4, end = min(w.t1, w.t0 + (wave + 1) * each);
   int t = w.t0 + wave * each;
-  int64_t off[KEYS / 8] = {};
+  int64_t off[KEYS / 8] = {};  // of the tile's groups of eight keys
   uint32_t present = 0;
+  auto find = [&](int j0) {
+    ids.cover(a, j0, KEYS);
+#pragma unroll
+    for (int u = 0; u < KEYS / 8; ++u) off[u] = ids.at(a, j0 + 8 * u);
+    present = ids.present<KEYS>(a, j0);
+  };
   if (t < end) {
-    present = tile_at<KEYS>(a, ids, t * KEYS, off);
+    find(t * KEYS);
     load_k(off);
   }
   rows.template start<FULL>(a, w, w.r0, lane);
@@ -362,7 +370,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
     rows.scores(k);
     const uint32_t here = present;
     if (t + 1 < end) {
-      present = tile_at<KEYS>(a, ids, (t + 1) * KEYS, off);
+      find((t + 1) * KEYS);
       load_k(off);
     }
     rows.template soften<mask>(here, a.window, t * KEYS, g, sc);
@@ -479,54 +487,53 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
 
   PageIds ids;
   ids.start(a, w);
-  // A DMA of a wave fills 1 KB: KPD keys, within a group of eight.
   struct Present {
     uint32_t x[KT];
   };
-  auto fetch = [&](int t) {
-    const uint32_t to = lds0 + (uint32_t)((t - w.t0) % (AHEAD + 1) * 4 * TILE);
-    int64_t at[4 * KT];
-    Present found;
-#pragma unroll
-    for (int s = 0; s < KT; ++s) {
-      int64_t (&part)[4] = *reinterpret_cast<int64_t (*)[4]>(at + 4 * s);
-      found.x[s] = tile_at<32>(a, ids, t * KEYS + 32 * s, part);
-    }
+  // A DMA of a wave fills 1 KB: KPD keys, within a group of eight.
+  auto fetch = [&](int t, int stage) {
+    const uint32_t to = lds0 + (uint32_t)(stage * 4 * TILE);
+    ids.cover(a, t * KEYS, KEYS);
 #pragma unroll
     for (int i = 0; i < KD; ++i) {
-      const int part = i * NW + wave, j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ swizzle<DH>(j), u = part * KPD / 8;
-      int64_t off = at[0];
-#pragma unroll
-      for (int e = 1; e < 4 * KT; ++e) off = u == e ? at[e] : off;
-      off += (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
+      const int part = i * NW + wave, j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ swizzle<DH>(j);
+      const int64_t off = ids.at(a, t * KEYS + part * KPD / 8 * 8) + (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
       dma16(kb + off, to + part * 1024);
       dma16(vb + off, to + 2 * TILE + part * 1024);
     }
+    Present found;
+#pragma unroll
+    for (int s = 0; s < KT; ++s) found.x[s] = ids.present<32>(a, t * KEYS + 32 * s);
     return found;
   };
   dma_wait_all();  // the queries are here: from now on only the DMAs count as loads in flight
   Present present[AHEAD + 1] = {};  // of this tile and the next ones
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
-    if (w.t0 + i < w.t1) present[i] = fetch(w.t0 + i);
+    if (w.t0 + i < w.t1) present[i] = fetch(w.t0 + i, i);
 
-  int t = w.t0;
+  int t = w.t0, stage = 0;  // of tile t
   auto step = [&](auto mask_) {
     constexpr bool mask = decltype(mask_)::value;
     // tile t has landed, and every wave is done with tile t - 1, whose place the next fetch takes
     if (AHEAD == 2 && t + 1 < w.t1) dma_wait_barrier<DMAS>();
     else dma_wait_barrier<0>();
-    if (t + AHEAD < w.t1) present[AHEAD] = fetch(t + AHEAD);
-    const uint16_t* ks = buf[(t - w.t0) % (AHEAD + 1)][0];
-    const uint16_t* vs = buf[(t - w.t0) % (AHEAD + 1)][1];
+    const uint16_t* ks = buf[stage][0];
+    const uint16_t* vs = buf[stage][1];
+    // every key on its way before the first product, and the next fetch's addresses meanwhile
+    u32x4 k[NK][KT];
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+      for (int u = 0; u < KT; ++u) k[i][u] = *reinterpret_cast<const u32x4*>(ks + (32 * u + col) * DH + 8 * ((2 * i + h) ^ swizzle<DH>(col & 15)));
+    if (t + AHEAD < w.t1) present[AHEAD] = fetch(t + AHEAD, stage == 0 ? AHEAD : stage - 1);
     floatx16 s[KT] = {};
 #pragma unroll
     for (int i = 0; i < NK; ++i)
 #pragma unroll
       for (int u = 0; u < KT; ++u) {
-        u32x4 x = *reinterpret_cast<const u32x4*>(ks + (32 * u + col) * DH + 8 * ((2 * i + h) ^ swizzle<DH>(col & 15)));
-        if (!FULL && 2 * i + h > last_piece) x = u32x4{0, 0, 0, 0};
-        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), q[i], s[u], 0, 0, 0);
+        if (!FULL && 2 * i + h > last_piece) k[i][u] = u32x4{0, 0, 0, 0};
+        s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[i][u]), q[i], s[u], 0, 0, 0);
       }
     uint32_t seen[KT];
     if constexpr (mask) {
@@ -601,6 +608,7 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
       }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) present[i] = present[i + 1];
+    stage = stage == AHEAD ? 0 : stage + 1;
     ++t;
   };
   // whether some row of the wave does not see some key of the tile
