@@ -7,7 +7,7 @@ HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
 
 
 def ints(values):
-    return torch.tensor(np.asarray(values), dtype=torch.int32).cuda()
+    return torch.tensor(np.ascontiguousarray(values), dtype=torch.int32).cuda()
 
 
 def pages(rng, n_pages, P, Hkv, dh, dtype, heads_first=False, layers=None):
