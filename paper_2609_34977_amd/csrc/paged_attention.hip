@@ -672,22 +672,27 @@ __global__ void __launch_bounds__(256) paged_join_kernel(ChunkArgs a, ChunkLaunc
   if (w.ns == 1) return;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
   const int64_t part = chunk_part(a, l, w, rr);
+  const int per = a.dh / 4, ng = 64 / per, grp = lane / per, c = 4 * (lane % per);
+  // four splits of a group at a time, the first ones on their way before the maximum is known
+  float2 ml[4];
+  floatx4 o[4];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = min(s0 + u * ng, w.ns - 1);
+      ml[u] = l.part_ml[part + s];
+      o[u] = *reinterpret_cast<const floatx4*>(l.part_o + (part + s) * a.dh + c);
+    }
+  };
+  if (grp < ng) load(grp);
   float mx = -INFINITY;
   for (int s = lane; s < w.ns; s += 64) mx = fmaxf(mx, l.part_ml[part + s].x);
   mx = wave_max(mx);
-  const int per = a.dh / 4, ng = 64 / per, grp = lane / per, c = 4 * (lane % per);
   float sum = 0.f;
   floatx4 x = floatx4{};
   if (grp < ng) {
     for (int s0 = grp; s0 < w.ns; s0 += 4 * ng) {
-      float2 ml[4];
-      floatx4 o[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int s = min(s0 + u * ng, w.ns - 1);
-        ml[u] = l.part_ml[part + s];
-        o[u] = *reinterpret_cast<const floatx4*>(l.part_o + (part + s) * a.dh + c);
-      }
+      if (s0 > grp) load(s0);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         if (s0 + u * ng >= w.ns) break;
