@@ -39,9 +39,9 @@ struct ChunkLaunch {
   float* part_o;    // .. [dh] its unscaled output
   int keys, rows;   // of a tile, of a row block
   int row_blocks, splits;
+  int min_tiles;  // of a split
   int whole;  // each sequence is one row block, and rows of part_* are numbered [b][hk][rows], else as in out
 };
-constexpr int kMinTiles = 8;  // tiles of a split, see chunk_plan
 
 // What a block works on: rows r0 .. of the R rows of a sequence and kv head, tiles [t0, t1) of
 // its keys, which are split `split` of ns.
@@ -51,14 +51,14 @@ struct ChunkWork {
 };
 
 // The tiles that any of the rows of block w.r0 sees, and their splits: at most l.splits, each of
-// at least kMinTiles tiles, and no more of them than have a tile.
+// at least l.min_tiles tiles, and no more of them than have a tile.
 __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const ChunkLaunch& l, ChunkWork& w, int keys) {
   const int G = a.H / a.Hkv, first = w.s.len - w.s.rows + w.r0 / G;
   const int last = w.s.len - w.s.rows + (min(w.r0 + l.rows, w.R) - 1) / G;
   const int lo = a.window > 0 ? max(0, first - a.window + 1) : 0;
   w.t0 = last < 0 ? 0 : lo / keys;
   const int end = last < 0 ? 0 : last / keys + 1, n = end - w.t0;
-  const int most = max(1, min(l.splits, n / kMinTiles));
+  const int most = max(1, min(l.splits, n / l.min_tiles));
   const int per = max(1, (n + most - 1) / most);
   w.ns = most == 1 ? 1 : (n + per - 1) / per;
   w.t0 += w.split * per;
@@ -460,7 +460,8 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
   if (!chunk_work<KEYS, ROWS, false>(a, l, w)) return;
   const uint16_t* kb = reinterpret_cast<const uint16_t*>(a.k) + w.hk * a.p.sh;
   const uint16_t* vb = reinterpret_cast<const uint16_t*>(a.v) + w.hk * a.p.sh;
-  const float sc = fabsf(a.scale) * 1.4426950408889634f;
+  // (with scale 0 the smallest number that leaves -inf, a score that is not seen, what it is)
+  const float sc = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1.17549435e-38f);
   const uint32_t lds0 = lds_offset(&buf[0][0][0]);
   const int last_piece = a.dh / 8 - 1, G = a.H / a.Hkv;
 
@@ -497,7 +498,9 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
 #pragma unroll
     for (int i = 0; i < KD; ++i) {
       const int part = i * NW + wave, j = part * KPD + lane / PIECES, c = (lane % PIECES) ^ swizzle<DH>(j);
-      const int64_t off = ids.at(a, t * KEYS + part * KPD / 8 * 8) + (j & 7) * a.p.ss + 8 * (FULL ? c : min(c, last_piece));
+      // (slots behind the last one, which may hold anything, are not read)
+      const int64_t off = ids.at(a, min(t * KEYS + part * KPD / 8 * 8, (w.s.len - 1) & ~7)) + (min(t * KEYS + j, w.s.len - 1) & 7) * a.p.ss +
+                          8 * (FULL ? c : min(c, last_piece));
       dma16(kb + off, to + part * 1024);
       dma16(vb + off, to + 2 * TILE + part * 1024);
     }
@@ -566,7 +569,6 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], sc, -mc));
-        if constexpr (mask) s[u][r] = (seen[u] >> (r % 4 + 8 * (r / 4))) & 1u ? s[u][r] : 0.f;
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -577,35 +579,62 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
       }
     }
     // 16 lanes read four keys of 16 channels, a lane gets the four keys of channel lane % 16
-    uint32_t bad = 0;
+    auto operand = [&](int k, int c) {
+      u32x4 x;
 #pragma unroll
-    for (int k = 0; k < 2 * KT; ++k) {
-      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[k], sum, 0, 0, 0);
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        u32x4 x;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int j = 16 * k + 8 * e + 4 * h + m / 4, piece = 4 * c + 2 * ((lane >> 4) & 1) + m % 4 / 2;
-          const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ swizzle<DH>(j & 15)) + 4 * (m % 2)));
-          const uint2 z = __builtin_bit_cast(uint2, y);
-          x[2 * e] = z.x;
-          x[2 * e + 1] = z.y;
-        }
-        if constexpr (mask) {
-          // (infinite and NaN values must not reach the rows that do not see them, see below)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = AttnTile<uint16_t, DH>::finite(x[e], bad);
-        }
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), p[k], o[c], 0, 0, 0);
+      for (int e = 0; e < 2; ++e) {
+        const int j = 16 * k + 8 * e + 4 * h + m / 4, piece = 4 * c + 2 * ((lane >> 4) & 1) + m % 4 / 2;
+        const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) short4v*)(vs + j * DH + 8 * (piece ^ swizzle<DH>(j & 15)) + 4 * (m % 2)));
+        const uint2 z = __builtin_bit_cast(uint2, y);
+        x[2 * e] = z.x;
+        x[2 * e + 1] = z.y;
       }
-    }
-    if constexpr (mask)
-      if (__any(bad != 0)) {
+      return x;
+    };
+    // Infinite and NaN values must not reach the rows that do not see them (0 times one of them is
+    // NaN): they leave the product, and what the rows see of them is put right at the end.  That
+    // there are any is looked for first, in two operations per pair of values.
+    auto products = [&](auto drop_) {
+#pragma unroll
+      for (int k = 0; k < 2 * KT; ++k) {
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[k], sum, 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          u32x4 x = operand(k, c);
+          if constexpr (decltype(drop_)::value) {
+            uint32_t bad;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = AttnTile<uint16_t, DH>::finite(x[e], bad);
+          }
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), p[k], o[c], 0, 0, 0);
+        }
+      }
+    };
+    if constexpr (mask) {
+      typedef uint16_t ushort2v __attribute__((ext_vector_type(2)));
+      ushort2v most = {0, 0};
+#pragma unroll
+      for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const u32x4 x = operand(k, c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2v, x[e] & 0x7FFF7FFFu));
+        }
+      const bool drop = __any(max(most[0], most[1]) >= 0x7F80);
+      if (drop) {
         bad0 = min(bad0, t);
         bad1 = max(bad1, t);
       }
+      if (drop || DH == 256) {  // (width 256 has no registers for both)
+        products(std::true_type{});
+      } else {
+        products(std::false_type{});
+      }
+    } else {
+      products(std::false_type{});
+    }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) present[i] = present[i + 1];
     stage = stage == AHEAD ? 0 : stage + 1;
@@ -725,32 +754,39 @@ struct ChunkPlan {
   int nw;   // waves of paged_chunk_kernel, or 0
   int limit;
   ChunkLaunch few, chunk;
-  size_t few_o, chunk_ml, chunk_o, bytes;
+  size_t few_ml, few_o, chunk_ml, chunk_o, bytes;
 };
+// Tiles of a split of few rows.  Measured with 4 / 8 / 16, us on the device: one row of 32 heads
+// over 705 slots 10.6 / 12.1 / 11.5, over 2944 17.9 / 18.2 / 17.2, 4 of them over 705 16.0 / 15.5 /
+// 13.6; one of 8 x 4 heads over 2000 11.2 / 12.2 / 14.6, 32 of them over 705 21.1 / 23.0 / 21.8;
+// fp32, 70 of 2 x 3 heads in a window of 300 13.7 / 15.3 / 15.6, 13 of 8 over 1500 12.6 / 11.3 / 13.1.
+constexpr int kFewTiles = 4;
 
-// slots: of the longest sequence, window (0: none): what a row sees of them.  (Fewer slots never
-// give more splits, so a workspace for all slots serves every window.)
+// slots: of the longest sequence, window (0: none): what a row sees of them.
 ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window, spider_dtype dtype) {
   ChunkPlan p{};
   const bool bf16 = dtype == SPIDER_BF16;
   const int64_t G = H / Hkv, R = N * G;  // rows of a kv head, R / B of an average sequence
   p.dhp = dh <= 64 ? 64 : (dh <= 128 ? 128 : 256);
   const int keys = bf16 ? 32 : 16;
-  // splits of the longest sequence, of row blocks of up to 256 rows
+  // slots that the longest sequence's row blocks, of up to 256 rows, see
   const int64_t reach = window > 0 ? std::min<int64_t>(slots, (int64_t)window + std::min<int64_t>(N, ceil_div(256, (int)G) + 1) + keys) : slots;
-  const int most = std::max(1, (int)((reach + keys - 1) / keys) / kMinTiles);
+  const auto few_splits = [&](int64_t blocks) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((reach + keys - 1) / keys / kFewTiles, 768 / blocks));
+  };
   size_t off = 0;
+  const auto parts = [&](ChunkLaunch& l, size_t rows, size_t* ml, size_t* o) {
+    if (l.splits == 1) return;
+    *ml = off;
+    *o = align_up(off + rows * l.splits * sizeof(float2), 256);
+    off = align_up(*o + rows * l.splits * dh * sizeof(float), 256);
+  };
   if (!bf16 || R <= (int64_t)B * (p.dhp == 256 ? 16 : 32)) {
     p.rt = R <= (int64_t)B * 16 || p.dhp == 256 ? 1 : 2;
     p.limit = 0x7fffffff;
     const int rows = 16 * p.rt, blocks = (int)(R / rows);
-    p.few = ChunkLaunch{nullptr, nullptr, keys, rows, blocks + B, 1, 0};
-    p.few.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 768 / (Hkv * std::max<int64_t>(B, blocks))));
-    if (p.few.splits > 1) {
-      const size_t n = (size_t)N * H * p.few.splits;
-      p.few_o = align_up(n * sizeof(float2), 256);
-      off = align_up(p.few_o + n * dh * sizeof(float), 256);
-    }
+    p.few = ChunkLaunch{nullptr, nullptr, keys, rows, blocks + B, few_splits(Hkv * std::max<int64_t>(B, blocks)), kFewTiles, 0};
+    parts(p.few, (size_t)N * H, &p.few_ml, &p.few_o);
     p.bytes = off;
     return p;
   }
@@ -758,32 +794,38 @@ ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window
   if (B > 1) {
     p.rt = 1;
     p.limit = 16;
-    p.few = ChunkLaunch{nullptr, nullptr, keys, 16, B, 1, 1};
-    p.few.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, 768 / ((int64_t)Hkv * B)));
-    if (p.few.splits > 1) {
-      const size_t n = (size_t)B * Hkv * 16 * p.few.splits;
-      p.few_o = align_up(n * sizeof(float2), 256);
-      off = align_up(p.few_o + n * dh * sizeof(float), 256);
-    }
+    p.few = ChunkLaunch{nullptr, nullptr, keys, 16, B, few_splits((int64_t)Hkv * B), kFewTiles, 1};
+    parts(p.few, (size_t)B * Hkv * 16, &p.few_ml, &p.few_o);
   }
   // (width 256 has registers for one wave per SIMD)
   p.nw = R <= (int64_t)B * 64 ? 2 : (R <= (int64_t)B * 128 || p.dhp == 256 ? 4 : 8);
   const int rows = 32 * p.nw, at_once = p.dhp == 256 ? 256 : 256 * 8 / p.nw;  // blocks that run at once
   const int64_t blocks = Hkv * std::max<int64_t>(1, R / rows);
   const int chunk_keys = p.dhp == 256 || p.nw == 2 ? 32 : 64;
-  p.chunk = ChunkLaunch{nullptr, nullptr, chunk_keys, rows, (int)(R / rows) + B, 1, 0};
-  // The splits that leave the least of the last round of blocks empty; each costs its joining.
-  double best = 1e30;
-  for (int s = 1; s <= std::min(std::max(1, most * keys / chunk_keys), 16); ++s) {
-    const double rounds = (double)((blocks * s + at_once - 1) / at_once) / s * (1.0 + 0.03 * (s - 1));
-    if (rounds < best) best = rounds, p.chunk.splits = s;
-  }
-  if (p.chunk.splits > 1) {
-    const size_t n = (size_t)N * H * p.chunk.splits;
-    p.chunk_ml = off;
-    p.chunk_o = align_up(off + n * sizeof(float2), 256);
-    off = align_up(p.chunk_o + n * dh * sizeof(float), 256);
-  }
+  // Splits by an estimate of the time in us, for sequences that fill the table: a tile of 64 keys
+  // takes 2.1 (dh 128, all CUs busy), a block 3 besides its tiles, a split's partial sums are
+  // written at 5 TB/s, 60 GB/s at most for a block, and joined at 3 TB/s in a launch of 4 or more.
+  // The blocks' rounds end together where their lengths differ (causal rows from the first slot).
+  const double tile = 2.1 * chunk_keys / 64 * dh / 128, row_bytes = 4.0 * dh + 8, n = (double)N / B;
+  const auto chunk_splits = [&](int64_t reach, int most) {
+    const double tiles = (double)reach / chunk_keys, mean = std::max(1.0, (reach - n / 2) / chunk_keys), even = mean / tiles;
+    int splits = 1;
+    double best = 1e30;
+    for (int s = 1; s <= most && (s == 1 || s * 2 <= tiles); ++s) {
+      const double rounds = (double)blocks * s / at_once, full = std::ceil(rounds), share = std::min((double)at_once, (double)blocks * s);
+      const double write = s > 1 ? rows * row_bytes / std::min(60e3, 5e6 / share) : 0.0;
+      double us = (rounds + (full - rounds) * even * even) * (mean * tile / s + 3 + write);
+      us = std::max(us, tiles * tile / s + 3 + write) + (s > 1 ? 4 + (double)N * H * s * row_bytes / 3e6 : 0.0);
+      if (us < best) best = us, splits = s;
+    }
+    return splits;
+  };
+  // (never more than without a window, so that a workspace for all slots serves every window)
+  const int splits = chunk_splits(reach, chunk_splits(slots, 16));
+  // (how long the sequences are is known on the device: where the blocks alone keep half of the CUs
+  // busy, splits of less than 32 tiles would cost more than they save)
+  p.chunk = ChunkLaunch{nullptr, nullptr, chunk_keys, rows, (int)(R / rows) + B, splits, 2 * blocks >= at_once ? 32 : 2, 0};
+  parts(p.chunk, (size_t)N * H, &p.chunk_ml, &p.chunk_o);
   p.bytes = off;
   return p;
 }
@@ -869,7 +911,7 @@ extern "C" spider_status spider_paged_attention(int N, int H, int Hkv, int dh, c
   a.H = H, a.Hkv = Hkv, a.dh = dh, a.window = window, a.scale = scale, a.limit = p.limit;
   char* ws = reinterpret_cast<char*>(workspace);
   if (p.few.splits > 1) {
-    p.few.part_ml = reinterpret_cast<float2*>(ws);
+    p.few.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);
     p.few.part_o = reinterpret_cast<float*>(ws + p.few_o);
   }
   if (p.chunk.splits > 1) {
