@@ -83,39 +83,54 @@ __device__ __forceinline__ int2 block_prefix(int x, int* waves) {
 // one launch and the copies.
 template <bool WHOLE>
 __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
+  __shared__ int old_len[kForkMaxB], from[kForkMaxB], len[kForkMaxB];  // of the old sequences; parent (-1: none) and length of the new ones
   __shared__ int last[kForkMaxB], start[kForkMaxB + 1];  // the page a sequence writes into; its place among the pages taken
   __shared__ int waves[16];
   extern __shared__ int counts[];
   const int tid = threadIdx.x, P = 1 << a.shift;
   int32_t* ref = WHOLE ? counts : a.ref_out;
-  if constexpr (WHOLE) {
+  for (int b = tid; b < a.B_in; b += 1024) old_len[b] = fork_len(a, b);
+  for (int b = tid; b < a.B_out; b += 1024) from[b] = (uint32_t)a.parent[b] < (uint32_t)a.B_in ? a.parent[b] : -1;
+  if constexpr (WHOLE)
     for (int p = tid; p < a.n_pages; p += 1024) ref[p] = a.ref_in[p];
-    __syncthreads();
-    for (int r = tid / 64; r < a.B_in + a.B_out; r += 16) {
-      const bool old = r < a.B_in;
-      const int b = old ? r : r - a.B_in;
-      const int2 from = old ? make_int2(b, fork_len(a, b)) : fork_from(a, b);
-      const int n = fork_pages(a, from.y);
-      for (int i = tid & 63; i < (old ? n : a.max_pages); i += 64) {
-        const int page = i < n ? a.table_in[(int64_t)from.x * a.max_pages + i] : -1;
-        const bool held = (uint32_t)page < (uint32_t)a.n_pages;
-        if (!old) a.table_out[(int64_t)b * a.max_pages + i] = held ? page : -1;
-        if (held) atomicAdd(ref + page, old ? -1 : 1);
+  __syncthreads();
+  for (int b = tid; b < a.B_out; b += 1024) {
+    const int n = from[b] < 0 ? 0 : old_len[from[b]];
+    const int grown = from[b] < 0 ? 0 : (int)min((int64_t)n + (a.n_new ? max(a.n_new[b], 0) : 0), (int64_t)a.max_pages << a.shift);
+    len[b] = n;
+    a.lens_out[b] = grown;
+    const int page = grown > n && n % P ? a.table_in[(int64_t)from[b] * a.max_pages + (n >> a.shift)] : -1;
+    last[b] = (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
+    start[b] = fork_pages(a, grown) - fork_pages(a, n);
+  }
+  __syncthreads();
+  if constexpr (WHOLE) {
+    // four rows of the tables at a time per wave
+    const int rows = a.B_in + a.B_out, wave = tid >> 6;
+    for (int r0 = wave; r0 < rows; r0 += 64) {
+      for (int i = tid & 63; i < a.max_pages; i += 64) {
+        int page[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = r0 + 16 * u, b = r - a.B_in, source = r < a.B_in ? r : (r < rows ? from[b] : -1);
+          const int n = source < 0 ? 0 : fork_pages(a, old_len[source]);
+          page[u] = i < n ? a.table_in[(int64_t)source * a.max_pages + i] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = r0 + 16 * u;
+          const bool held = (uint32_t)page[u] < (uint32_t)a.n_pages;
+          if (r >= a.B_in && r < rows) a.table_out[(int64_t)(r - a.B_in) * a.max_pages + i] = held ? page[u] : -1;
+          if (held) atomicAdd(ref + page[u], r < a.B_in ? -1 : 1);
+        }
       }
     }
+    __syncthreads();
   }
   const auto load = [&](int p) {
     if constexpr (WHOLE) return ref[p];
     else return fork_load(ref + p);
   };
-  for (int b = tid; b < a.B_out; b += 1024) {
-    const int2 from = fork_from(a, b);
-    const int grown = from.x < 0 ? 0 : (int)min((int64_t)from.y + (a.n_new ? max(a.n_new[b], 0) : 0), (int64_t)a.max_pages << a.shift);
-    a.lens_out[b] = grown;
-    const int page = grown > from.y && from.y % P ? a.table_in[(int64_t)from.x * a.max_pages + (from.y >> a.shift)] : -1;
-    last[b] = (uint32_t)page < (uint32_t)a.n_pages ? page : -1;
-  }
-  __syncthreads();
   // The first writer of a page keeps it if nobody but the writers holds it.
   int taken = 0;
   uint32_t copies = 0;  // bit i: of sequence i * 1024 + tid
@@ -123,7 +138,6 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
     const int b = b0 + tid;
     int need = 0;
     if (b < a.B_out) {
-      const int2 from = fork_from(a, b);
       const int page = last[b];
       if (page >= 0) {
         int same = 0, before = 0;
@@ -133,7 +147,7 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
         }
         if (before > 0 || load(page) > same) copies |= 1u << i;
       }
-      need = fork_pages(a, a.lens_out[b]) - fork_pages(a, from.y) + ((copies >> i) & 1u);
+      need = start[b] + ((copies >> i) & 1u);
     }
     const int2 at = block_prefix(need, waves);
     if (b < a.B_out) start[b] = taken + at.x;
@@ -154,15 +168,14 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
   found = min(found, taken);
   __syncthreads();
   for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i) {
-    const int2 from = fork_from(a, b);
     const int copy = (copies >> i) & 1u;
     int4 c = make_int4(-1, -1, 0, 0);
     for (int n = start[b]; n < start[b + 1]; ++n) {
       const int page = n < found ? a.free_list[n] : -1, j = n - start[b];
-      const int at = copy && j == 0 ? from.y >> a.shift : fork_pages(a, from.y) + j - copy;
+      const int at = copy && j == 0 ? len[b] >> a.shift : fork_pages(a, len[b]) + j - copy;
       a.table_out[(int64_t)b * a.max_pages + at] = page;
       if (page >= 0) ref[page] = 1;
-      if (copy && j == 0) c = make_int4(last[b], page, from.y % P, 0);
+      if (copy && j == 0) c = make_int4(last[b], page, len[b] % P, 0);
     }
     a.copies[b] = c;
   }
