@@ -156,7 +156,7 @@ def test_workspace_sizes(L):
     assert L.spider_paged_attention_workspace_size(0, 1, 4, 2, 64, 9000, 1) == 0
     assert L.spider_paged_attention_workspace_size(9, 3, 5, 2, 64, 9000, 1) == 0
     assert L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 0, 1) == 0
-    assert L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 256, 1) == 0 < L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 9000, 1)
+    assert L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 100, 1) == 0 < L.spider_paged_attention_workspace_size(1, 1, 4, 2, 64, 9000, 1)
     assert L.spider_pages_fork_workspace_size(0, 10) == 0 and L.spider_pages_fork_workspace_size(4097, 10) == 0
     assert L.spider_pages_fork_workspace_size(5, 1000) >= 5 * 16 + 4000
     assert L.spider_beam_select_workspace_size(1, 65, 1, 100) == 0 and L.spider_beam_select_workspace_size(1, 1, 1, (1 << 19) + 1) == 0
