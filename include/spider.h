@@ -787,7 +787,8 @@ spider_status spider_paged_attention(int N, int H, int Hkv, int dh, const void* 
  * head); positive where there is more than one, multiples of 16 bytes; 16-byte
  * aligned; dh a multiple of 16 bytes, at most 256.
  * Limits: B_in, B_out <= 4096, L * B_out <= 65535, page_size a power of two from 8
- * to 4096, max_pages * page_size and page_size * Hkv * dh <= 2^30.  Workspace:
+ * to 4096, max_pages * page_size and page_size * Hkv * dh <= 2^30, fewer than 2^31
+ * entries in a table.  Workspace:
  * spider_pages_fork_workspace_size(B_out, n_pages) bytes, 256-byte aligned.
  * ------------------------------------------------------------------------ */
 size_t spider_pages_fork_workspace_size(int B_out, int n_pages);

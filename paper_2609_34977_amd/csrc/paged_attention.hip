@@ -443,8 +443,10 @@ __device__ __forceinline__ int swizzle(int j) {
 // time, so a lane owns row lane % 32 in both, with half h = lane / 32 of the keys: register r of a
 // product holds key (channel) r % 4 + 8 (r / 4) + 4 h.  Eight such registers are the operand of a
 // product over 16 keys as they stand, whose values are read transposed in the same order.
-// The sums of the rounded weights are products with ones on the 16x16x32 unit, half as many cycles:
-// it sees the rows 16 apart in one column, so one half of its ones serves each of them.
+// The sums of the rounded weights are dot products with ones of a tile's pairs, each tile's added
+// to the row's: that instruction's own additions are 0.17 steps low on average, which a tile's 16
+// keep at 2^-23.  (On the matrix unit of 16 rows, which takes as long, a NaN weight would reach
+// the sum of the row 16 on: 0 times NaN.)
 template <int DH, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l) {
   constexpr int KT = DH == 256 || NW == 2 ? 1 : 2, KEYS = 32 * KT, NK = DH / 16, CT = DH / 32, ROWS = 32 * NW;
@@ -480,11 +482,9 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
     }
   }
   floatx16 o[CT] = {};
-  floatx4 sum = {};
+  float sum = 0.f;  // of the lane's half of the keys
   float top = -INFINITY;
   int bad0 = 0x7fffffff, bad1 = -1;  // the first and last masked tile with an infinite or NaN value
-  const uint32_t one = (m >= 8) == ((lane >> 4) & 1) ? 0x3F803F80u : 0u;
-  const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{one, one, one, one});
 
   PageIds ids;
   ids.start(a, w);
@@ -558,12 +558,13 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
       const float nt = fmaxf(top, mx);
       const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - nt) * sc);
       top = nt;
-      sum *= __shfl(f, m + ((lane >> 5) << 4));
+      sum *= f;
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[c] *= f;
     }
     const float mc = top == -INFINITY ? 0.f : top * sc;
     bf16x8 p[2 * KT];  // weights of 16 keys each
+    float part[2] = {};
 #pragma unroll
     for (int u = 0; u < KT; ++u) {
 #pragma unroll
@@ -574,10 +575,15 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
       for (int e = 0; e < 2; ++e) {
         u32x4 x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{s[u][8 * e + 2 * i], s[u][8 * e + 2 * i + 1]}, bf16x2v));
+        for (int i = 0; i < 4; ++i) {
+          const bf16x2v y = __builtin_convertvector(float2v{s[u][8 * e + 2 * i], s[u][8 * e + 2 * i + 1]}, bf16x2v);
+          x[i] = __builtin_bit_cast(uint32_t, y);
+          part[e] = __builtin_amdgcn_fdot2_f32_bf16(y, bf16x2v{(__bf16)1.f, (__bf16)1.f}, part[e], false);
+        }
         p[2 * u + e] = __builtin_bit_cast(bf16x8, x);
       }
     }
+    sum += part[0] + part[1];
     // 16 lanes read four keys of 16 channels, a lane gets the four keys of channel lane % 16
     auto operand = [&](int k, int c) {
       u32x4 x;
@@ -598,7 +604,6 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
     auto products = [&](auto drop_) {
 #pragma unroll
       for (int k = 0; k < 2 * KT; ++k) {
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[k], sum, 0, 0, 0);
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
           u32x4 x = operand(k, c);
@@ -652,7 +657,8 @@ __global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel
     while (t < w.t1 && masked()) step(std::true_type{});
   }
 
-  const float total = __shfl(sum[0], m + ((col >> 4) << 5));
+  const float2 halves = lanes_x32(sum);
+  const float total = halves.x + halves.y;
   if (r0 + col >= w.R) return;
   const int64_t out_row = chunk_row(a, w, rr), part_row = chunk_part(a, l, w, rr);
   if (h == 0 && w.ns > 1) l.part_ml[part_row] = make_float2(top, total);
@@ -908,7 +914,7 @@ extern "C" spider_status spider_paged_attention(int N, int H, int Hkv, int dh, c
   SPIDER_REQUIRE(p.bytes == 0 || reinterpret_cast<uintptr_t>(workspace) % 256 == 0, SPIDER_ERR_INVALID_ARG,
                  "spider_paged_attention: workspace must be 256-byte aligned");
   a.q = q, a.k = cache->k, a.v = cache->v, a.out = out, a.qs = q_stride;
-  a.H = H, a.Hkv = Hkv, a.dh = dh, a.window = window, a.scale = scale, a.limit = p.limit;
+  a.H = H, a.Hkv = Hkv, a.dh = dh, a.window = std::min(window, 1 << 30), a.scale = scale, a.limit = p.limit;
   char* ws = reinterpret_cast<char*>(workspace);
   if (p.few.splits > 1) {
     p.few.part_ml = reinterpret_cast<float2*>(ws + p.few_ml);

@@ -84,7 +84,7 @@ __device__ __forceinline__ int2 block_prefix(int x, int* waves) {
 template <bool WHOLE>
 __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
   __shared__ int old_len[kForkMaxB], from[kForkMaxB], len[kForkMaxB];  // of the old sequences; parent (-1: none) and length of the new ones
-  __shared__ int last[kForkMaxB], start[kForkMaxB + 1];  // the page a sequence writes into; its place among the pages taken
+  __shared__ int last[kForkMaxB], start[kForkMaxB];  // the page a sequence writes into; its place among the pages taken
   __shared__ int waves[16];
   extern __shared__ int counts[];
   const int tid = threadIdx.x, P = 1 << a.shift;
@@ -153,9 +153,12 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
     if (b < a.B_out) start[b] = taken + at.x;
     taken += at.y;
   }
-  if (tid == 0) start[a.B_out] = taken;
-  for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i)
-    if ((copies >> i) & 1u) atomicSub(ref + last[b], 1);
+  int* copies_of = old_len;  // (the old lengths are no longer needed)
+  for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i) {
+    copies_of[b] = (copies >> i) & 1u;
+    a.copies[b] = make_int4(-1, -1, 0, 0);
+    if (copies_of[b]) atomicSub(ref + last[b], 1);
+  }
   __syncthreads();
   int found = 0;
   for (int p0 = 0; p0 < a.n_pages && found < taken; p0 += 1024) {
@@ -167,17 +170,19 @@ __global__ void __launch_bounds__(1024) fork_assign_kernel(ForkArgs a) {
   }
   found = min(found, taken);
   __syncthreads();
-  for (int b = tid, i = 0; b < a.B_out; b += 1024, ++i) {
-    const int copy = (copies >> i) & 1u;
-    int4 c = make_int4(-1, -1, 0, 0);
-    for (int n = start[b]; n < start[b + 1]; ++n) {
-      const int page = n < found ? a.free_list[n] : -1, j = n - start[b];
-      const int at = copy && j == 0 ? len[b] >> a.shift : fork_pages(a, len[b]) + j - copy;
-      a.table_out[(int64_t)b * a.max_pages + at] = page;
-      if (page >= 0) ref[page] = 1;
-      if (copy && j == 0) c = make_int4(last[b], page, len[b] % P, 0);
+  // page n of those taken is the first of its sequence's: the copy, if it has one
+  for (int n = tid; n < taken; n += 1024) {
+    int lo = 0, hi = a.B_out;  // the last sequence that starts at n or before, past those that take none
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (start[mid] <= n) lo = mid;
+      else hi = mid;
     }
-    a.copies[b] = c;
+    const int b = lo, j = n - start[b], copy = copies_of[b], page = n < found ? a.free_list[n] : -1;
+    const int at = copy && j == 0 ? len[b] >> a.shift : fork_pages(a, len[b]) + j - copy;
+    a.table_out[(int64_t)b * a.max_pages + at] = page;
+    if (page >= 0) ref[page] = 1;
+    if (copy && j == 0) a.copies[b] = make_int4(last[b], page, len[b] % P, 0);
   }
   if (tid == 0) a.missing[0] = taken - found;
   if constexpr (WHOLE) {
@@ -243,7 +248,8 @@ extern "C" spider_status spider_pages_fork(int L, int Hkv, int dh, spider_dtype 
                  "spider_pages_fork: at most %d sequences, L * B_out at most 65535", kForkMaxB);
   SPIDER_REQUIRE(page_size >= 8 && page_size <= 4096 && (page_size & (page_size - 1)) == 0, SPIDER_ERR_UNSUPPORTED,
                  "spider_pages_fork: page_size must be a power of two from 8 to 4096, got %d", page_size);
-  SPIDER_REQUIRE((int64_t)max_pages * page_size <= (1 << 30), SPIDER_ERR_UNSUPPORTED, "spider_pages_fork: max_pages * page_size at most 2^30");
+  SPIDER_REQUIRE((int64_t)max_pages * page_size <= (1 << 30) && (int64_t)B_in * max_pages < (1LL << 31) && (int64_t)B_out * max_pages < (1LL << 31),
+                 SPIDER_ERR_UNSUPPORTED, "spider_pages_fork: max_pages * page_size at most 2^30, tables of less than 2^31 entries");
   const int es = dtype == SPIDER_BF16 ? 2 : 4;
   SPIDER_REQUIRE(dh * (int64_t)es % 16 == 0 && dh <= kPagedMaxDh && Hkv <= 65535 && (int64_t)page_size * Hkv * dh <= (1 << 30), SPIDER_ERR_UNSUPPORTED,
                  "spider_pages_fork: dh must be a multiple of 16 bytes and at most %d, a page at most 2^30 elements", kPagedMaxDh);

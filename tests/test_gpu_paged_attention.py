@@ -183,6 +183,40 @@ def test_infinite_and_nan_values_reach_the_rows_that_see_them_and_no_other(dtype
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [7, 30, 60, 100, 200])
+def test_nan_queries_and_keys_stay_with_their_rows(dtype, T):
+    """A NaN in one row's query, and an infinite key that only the last rows see, change no other row."""
+    lib = need_gpu()
+    lens, news = [T + 100], [T]
+    q, kp, vp, table, cu = case(T + 1, 2, 2, 128, 16, lens, news, dtype)
+    args = (ints(table), ints(lens), ints(cu))
+    base = lib.paged_attention(q, kp, vp, *args)
+    for r in (0, T // 2, T - 1):
+        q2 = q.clone()
+        q2[r, 1, 77] = float("nan")
+        out = lib.paged_attention(q2, kp, vp, *args)
+        assert torch.isnan(out[r, 1]).all()
+        out[r, 1] = base[r, 1]
+        assert torch.equal(out, base)
+    j = lens[0] - 3
+    k2 = kp.clone()
+    k2[table[0, j // 16], j % 16, 0, 3] = float("nan")
+    out = lib.paged_attention(q, k2, vp, *args)
+    assert torch.isnan(out[T - 3:, 0]).all()
+    out[T - 3:, 0] = base[T - 3:, 0]
+    assert torch.equal(out, base)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 40, 90])
+def test_the_largest_window(dtype, T):
+    lib = need_gpu()
+    q, kp, vp, table, cu = case(T, 2, 1, 64, 16, [T + 9], [T], dtype)
+    args = (ints(table), ints([T + 9]), ints(cu))
+    assert torch.equal(lib.paged_attention(q, kp, vp, *args, window=2**31 - 1), lib.paged_attention(q, kp, vp, *args))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 4.0])
 def test_scales(dtype, scale):
     lib = need_gpu()

@@ -108,6 +108,12 @@ def test_large_batches_and_pools(B, n_pages, M):
     run(B, B, rng.integers(-1, B, B), rng.integers(0, 3, B), P=8, M=M, n_pages=n_pages, L=1, Hkv=1, dh=8)
 
 
+def test_room_for_long_prompts():
+    """Thousands of pages for few sequences, none for others."""
+    run(9, 5, [0, 4, -1, 2, 2, 1], [20000, 0, 5000, 9000, 0, 1], P=8, M=4000, n_pages=9000, L=1, Hkv=1, dh=8, table=np.full((5, 4000), -1, np.int32),
+        lens=np.zeros(5, int), ref=np.zeros(9000, np.int32))
+
+
 @pytest.mark.parametrize("P,L,Hkv,dh,dtype,heads_first", [
     (8, 1, 1, 8, "bf16", False), (32, 3, 4, 80, "bf16", True), (64, 2, 3, 4, "f32", False), (256, 2, 2, 256, "f32", True), (4096, 1, 2, 16, "bf16", False),
 ])

@@ -119,7 +119,7 @@ FORK = dict(L=2, Hkv=2, dh=64, dt=1, k=P, v=2 * P, st=None, n_pages=10, page=16,
 @pytest.mark.parametrize("change,status", [(dict([(n, None)]), INVALID) for n in ("k", "v", "table", "lens", "ref", "parent", "t_out", "l_out", "r_out", "missing")] + [
     (dict(dt=2), INVALID), (dict(L=0), INVALID), (dict(n_pages=0), INVALID), (dict(M=0), INVALID), (dict(B_in=0), INVALID), (dict(B=0), INVALID),
     (dict(B=4097), UNSUPPORTED), (dict(B_in=4097), UNSUPPORTED), (dict(L=16384, B=4), UNSUPPORTED), (dict(page=4), UNSUPPORTED), (dict(page=48), UNSUPPORTED),
-    (dict(page=8192), UNSUPPORTED), (dict(M=(1 << 26) + 1), UNSUPPORTED), (dict(dh=60), UNSUPPORTED), (dict(dh=264), UNSUPPORTED), (dict(Hkv=65536), UNSUPPORTED),
+    (dict(page=8192), UNSUPPORTED), (dict(M=(1 << 26) + 1), UNSUPPORTED), (dict(B=1024, M=1 << 21), UNSUPPORTED), (dict(B_in=1024, M=1 << 21), UNSUPPORTED), (dict(dh=60), UNSUPPORTED), (dict(dh=264), UNSUPPORTED), (dict(Hkv=65536), UNSUPPORTED),
     (dict(k=P + 8), INVALID), (dict(ws=None), WORKSPACE), (dict(wsb=10), WORKSPACE), (dict(ws=12 * P + 128), INVALID),
     (dict(st=[8192, 2048, 128, 60]), INVALID), (dict(st=[0, 2048, 128, 64]), INVALID), (dict(st=[8192, 0, 128, 64]), INVALID), (dict(st=[8192, 2048, 0, 64]), INVALID),
     (dict(st=[8192, 2048, 128, 0]), INVALID), (dict(st=[8192, -2048, 128, 64]), INVALID),
