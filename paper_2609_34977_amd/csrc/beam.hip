@@ -63,18 +63,19 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // A block per piece of a row.  Every thread holds 32 logits, read 16 bytes at a time wherever the
 // row starts: the order of the sum depends on the tokens alone, so that equal rows have equal
-// sums and beams with them come in their order.  The exponentials' arguments x - top are exact or small for the terms that
-// count; four exponentials are added in fp32, those sums in fp64.
-// A bound below the M-th largest of the piece: in each wave the M-th largest of its lanes'
-// maxima, to 16 bits, found bit by bit with ballots; the largest of the waves' bounds.  What
-// reaches it (about 4 M logits) is ranked.  512 rows of 151000 bf16 logits, M = 8: see below.
+// sums and beams with them come in their order.  The exponentials' arguments x - top are exact or
+// small for the terms that count; four exponentials are added in fp32, those sums in fp64.
+// Bounds below the M-th largest of the piece: in each wave the M-th largest of its lanes' maxima,
+// of which the largest, and the M/4-th, of which the smallest; to 16 bits, found bit by bit with
+// ballots.  What reaches the larger one (about 1.3 M logits) is ranked.  512 rows of 151000 bf16
+// logits, M = 8: 38 us (4.0 TB/s); 64 rows of 32000 fp32, M = 64: 11 us, with the first bound alone 69.
 template <typename LT>
 __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
   constexpr int PER = kBeamPiece / 256, VEC = 16 / sizeof(LT);
   __shared__ uint64_t cand[kCand];
   __shared__ double sums[4];
   __shared__ float tops[4];
-  __shared__ uint32_t bounds[4];
+  __shared__ uint2 bounds[4];
   __shared__ int n_cand;
   __shared__ uint64_t best[4];
   const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -121,20 +122,22 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(BeamArgs a) {
 #pragma unroll
   for (int i = 1; i < PER; ++i) mx = fmaxf(mx, x[i]);
   const uint32_t key16 = float_order_key(mx) >> 16;
-  uint32_t bound = 0;
+  const int fourth = (a.M + 3) / 4;
+  uint32_t bound = 0, bound4 = 0;
 #pragma unroll
   for (int bit = 15; bit >= 0; --bit) {
-    const uint32_t t = bound | (1u << bit);
+    const uint32_t t = bound | (1u << bit), t4 = bound4 | (1u << bit);
     if (__popcll(__ballot(key16 >= t)) >= a.M) bound = t;
+    if (__popcll(__ballot(key16 >= t4)) >= fourth) bound4 = t4;
   }
   const float wm = wave_max(mx);
   if (lane == 0) {
     tops[wave] = wm;
-    bounds[wave] = bound;
+    bounds[wave] = make_uint2(bound, bound4);
   }
   __syncthreads();
   const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  bound = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3]));
+  bound = max(max(max(bounds[0].x, bounds[1].x), max(bounds[2].x, bounds[3].x)), min(min(bounds[0].y, bounds[1].y), min(bounds[2].y, bounds[3].y)));
   // the smallest logit of that bound (-inf and what lies below reach none)
   const float least = bound <= 0x007Fu ? -3.40282347e38f : beam_logit((uint64_t)bound << 48);
   double sum = 0.0;
@@ -220,57 +223,130 @@ __device__ __forceinline__ int2 beam_filled(const BeamArgs& a, int parent) {
   return make_int2(n, parent >= 0 && !(a.done && a.done[parent]) && n < a.cap ? 1 : 0);
 }
 
+// The order of candidates, rounded down to 32 bits.
+__device__ __forceinline__ uint32_t value_key(double x) { return float_order_key(__double2float_rd(x)); }
+
 // A block per sample: a wave per beam joins its pieces' lists, then every entry of the beams'
-// lists finds its rank by a binary search in each of them.
-constexpr int kStage = 512;  // list entries of a wave in LDS
+// lists finds its rank by a binary search in each of them.  What bounds it is the chain of those
+// steps, so with many beams a bound below the n_out-th candidate shortens the lists first: as many
+// lists' first entries as n_out, or a fourth as many lists' fourth entries, whichever is larger.
+// A selection without / with the bound, fp32, us on the device: 4 beams of 32000 13.1 / 14.4, 8 beams
+// 17.5 / 16.9, 64 samples of 8 30.7 / 31.0, 12 beams 22.6 / 20.7, 16 beams 29.7 / 25.7, 64 samples of 32
+// 124 / 97, 32 beams 72 / 36, 64 beams 274 / 76, 4 samples of 64 beams of 7000 201 / 90.
+constexpr int kBounded = 256;  // beams times n_out
+constexpr int kNth = 4;
+static_assert(kBounded >= kNth * kMaxBeams, "a bounded list has its fourth entry");
+constexpr int kStage = 512;     // list entries of a wave in LDS
 template <bool HISTORY>
 __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
-  extern __shared__ double value[];  // [K][M]
+  extern __shared__ double value[];  // [K][M], then int token [K][M], then uint32 heads [2][K][pieces]
   int* token = reinterpret_cast<int*>(value + a.K * a.M);
+  uint32_t* heads = reinterpret_cast<uint32_t*>(token + a.K * a.M);
   __shared__ uint64_t stage[16][kStage];
+  __shared__ float scores[kMaxBeams];
+  __shared__ double lses[kMaxBeams];  // NaN: the beam has no candidates, or is finished
   __shared__ int counts[kMaxBeams];
+  __shared__ uint32_t bound[2];
   __shared__ int2 chosen[kMaxBeams];  // (parent, token) of the new beams
   __shared__ int2 filled[kMaxBeams];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (HISTORY && tid < a.K) filled[tid] = beam_filled(a, b * a.K + tid);
+  const bool fits = a.pieces * a.M <= kStage, bounded = a.K * a.M >= kBounded;
+  const int n_heads = a.K * a.pieces;
   for (int k = wave; k < a.K; k += 16) {
     const int row = b * a.K + k;
     const float score = a.scores[row];
-    int count = 0;
+    double lse = NAN;
+    uint32_t head = 0, fourth = 0;
     if (beam_open(a, row)) {
-      const int64_t piece = (int64_t)row * a.pieces;
-      const uint64_t* lists = a.lists + piece * a.M;
-      if (a.pieces * a.M <= kStage) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int i = lane; i < a.pieces * a.M; i += 64) stage[wave][i] = lists[i];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        lists = stage[wave];
-      }
-      const float top = lane < a.pieces ? a.tops[piece + lane] : -INFINITY, all = wave_max(top);
-      double sum = top == -INFINITY ? 0.0 : a.sums[piece + lane] * exp((double)top - (double)all);
+      const int64_t piece = (int64_t)row * a.pieces + lane;
+      const bool on = lane < a.pieces;
+      const uint64_t key = on ? a.lists[piece * a.M] : 0ull, key4 = on && bounded ? a.lists[piece * a.M + kNth - 1] : 0ull;
+      if (k == wave && fits)  // a wave's first beam: for the join below
+        for (int i = lane; i < a.pieces * a.M; i += 64) stage[wave][i] = a.lists[(int64_t)row * a.pieces * a.M + i];
+      const float top = on ? a.tops[piece] : -INFINITY, all = wave_max(top);
+      double sum = top == -INFINITY ? 0.0 : a.sums[piece] * exp((double)top - (double)all);
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
       if (fabsf(all) < INFINITY) {
-        const double lse = (double)all + log(sum);
-        int next = 0;
-        uint64_t head = lane < a.pieces ? lists[lane * a.M] : 0ull;
-        while (count < a.M) {
-          const uint64_t key = wave_best(head);
-          if (key == 0) break;
-          if (head == key) {
-            ++next;
-            head = next < a.M ? lists[lane * a.M + next] : 0ull;
-            value[k * a.M + count] = (double)score + ((double)beam_logit(key) - lse);
-            token[k * a.M + count] = beam_token(key);
-          }
-          ++count;
-        }
+        lse = (double)all + log(sum);
+        if (bounded && key) head = value_key((double)score + ((double)beam_logit(key) - lse));
+        if (key4) fourth = value_key((double)score + ((double)beam_logit(key4) - lse));
       }
-    } else if (fabsf(score) < INFINITY) {
-      count = 1;
-      if (lane == 0) {
-        value[k * a.M] = score;
-        token[k * a.M] = a.eos;
+    } else if (fabsf(score) < INFINITY && lane == 0) {
+      value[k * a.M] = score;
+      token[k * a.M] = a.eos;
+      head = value_key((double)score);
+    }
+    if (bounded && lane < a.pieces) {
+      heads[k * a.pieces + lane] = head;
+      heads[n_heads + k * a.pieces + lane] = fourth;
+    }
+    if (lane == 0) {
+      lses[k] = lse;
+      scores[k] = score;
+      counts[k] = head != 0 && lse != lse ? 1 : 0;  // a finished beam's own entry
+    }
+  }
+  uint32_t least = 0;
+  if (bounded) {
+    __syncthreads();
+    if (wave < 2) {
+      const uint32_t* of = heads + wave * n_heads;
+      const int least_of = wave == 0 ? a.M : (a.M + kNth - 1) / kNth;
+      uint32_t t = 0, mine[4];  // the first 256 in registers
+#pragma unroll
+      for (int u = 0; u < 4; ++u) mine[u] = 64 * u + lane < n_heads ? of[64 * u + lane] : 0u;
+      for (int bit = 31; bit >= 12; --bit) {
+        const uint32_t to = t | (1u << bit);
+        int reach = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) reach += (int)__popcll(__ballot(mine[u] >= to));
+        for (int i = 256; i < n_heads; i += 64) reach += (int)__popcll(__ballot(i + lane < n_heads && of[i + lane] >= to));
+        if (reach >= least_of) t = to;
+      }
+      if (lane == 0) bound[wave] = t;
+    }
+    __syncthreads();
+    least = max(bound[0], bound[1]);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (what follows reads the wave's own writes)
+  for (int k = wave; k < a.K; k += 16) {
+    const double lse = lses[k];
+    if (lse != lse) continue;
+    const float score = scores[k];
+    const uint64_t* lists = a.lists + (int64_t)(b * a.K + k) * a.pieces * a.M;
+    if (fits) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (k != wave)
+        for (int i = lane; i < a.pieces * a.M; i += 64) stage[wave][i] = lists[i];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      lists = stage[wave];
+    }
+    int count = 0;
+    if (a.pieces == 1) {  // already in order
+      const uint64_t key = lane < a.M ? lists[lane] : 0ull;
+      const double x = (double)score + ((double)beam_logit(key) - lse);
+      const bool in = key != 0 && !(bounded && value_key(x) < least);
+      if (in) {
+        value[k * a.M + lane] = x;
+        token[k * a.M + lane] = beam_token(key);
+      }
+      count = (int)__popcll(__ballot(in));
+    } else {
+      uint64_t key = lane < a.pieces ? lists[lane * a.M] : 0ull;
+      int next = 0;
+      while (count < a.M) {
+        const uint64_t best = wave_best(key);
+        const double x = (double)score + ((double)beam_logit(best) - lse);
+        if (best == 0 || (bounded && value_key(x) < least)) break;
+        if (key == best) {
+          ++next;
+          key = next < a.M ? lists[lane * a.M + next] : 0ull;
+          value[k * a.M + count] = x;
+          token[k * a.M + count] = beam_token(best);
+        }
+        ++count;
       }
     }
     if (lane == 0) counts[k] = count;
@@ -283,7 +359,7 @@ __global__ void __launch_bounds__(1024) beam_join_kernel(BeamArgs a) {
     if (j >= counts[k]) continue;
     const double x = value[i];
     int rank = j;
-    for (int u = 0; u < a.K; ++u) {
+    for (int u = 0; u < a.K && rank < a.M; ++u) {
       if (u == k) continue;
       int lo = 0, hi = counts[u];  // entries of beam u that come first
       while (lo < hi) {
@@ -329,8 +405,11 @@ __global__ void __launch_bounds__(256) beam_history_kernel(BeamArgs a) {
   beam_history(a, row, parent, f.x, f.y, a.token[row], blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
-// Entries of history that a wave copies at the end of the join, at most.
-constexpr int kWithJoin = 4096;
+// Entries of history of a sample that its block copies at the end of the join, at most.  A selection
+// with the copy in the join / in a launch of its own, us on the device: 4 beams with 700 entries
+// 11.5 / 12.3, with 4000 12.7 / 12.4, with 16000 17.1 / 12.3; 32 beams with 2000 39.9 / 34.8; 64 samples of
+// 8 with 2000 17.0 / 17.5, with 8000 22.5 / 20.9; the launch costs the host 3 us.
+constexpr int kWithJoin = 32768;
 
 size_t beam_layout(int B, int K, int M, int V, char* at, BeamArgs* a) {
   const size_t n = (size_t)B * K * ceil_div(V, kBeamPiece);
@@ -405,9 +484,8 @@ extern "C" spider_status spider_beam_select(int B, int K, int n_out, int V, cons
   if (dtype == SPIDER_BF16) beam_scan_kernel<uint16_t><<<grid, 256, 0, st>>>(a);
   else beam_scan_kernel<float><<<grid, 256, 0, st>>>(a);
   SPIDER_LAUNCHED("beam_scan");
-  // Short histories go with the join, a wave or more per new beam.
-  const bool with = any && (int64_t)ceil_div(n_out, 16) * history_cap <= kWithJoin;
-  const unsigned lds = (unsigned)(K * n_out * (sizeof(double) + sizeof(int)));
+  const bool with = any && (int64_t)n_out * history_cap <= kWithJoin;
+  const unsigned lds = (unsigned)(K * n_out * (sizeof(double) + sizeof(int)) + (size_t)2 * K * a.pieces * sizeof(uint32_t));
   if (with) beam_join_kernel<true><<<(unsigned)B, 1024, lds, st>>>(a);
   else beam_join_kernel<false><<<(unsigned)B, 1024, lds, st>>>(a);
   SPIDER_LAUNCHED("beam_join");

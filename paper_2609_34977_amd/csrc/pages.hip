@@ -213,8 +213,11 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(ForkCopyArgs a) {
   *reinterpret_cast<u32x4*>(a.kv[1] + at + copy.y * a.sp) = v;
 }
 
-// Pools and tables that one block counts.
-constexpr int kForkLdsPages = 16384, kForkLdsEntries = 65536;
+// Pools and tables (entries of the old and new ones) that one block counts.  Measured, all launches
+// of a call on the device / with a block per row of the tables, us: 2 x 4 sequences of 9 pages 8.1 /
+// 10.5, 2 x 32 of 45 9.7 / 12.7, 2 x 32 of 186 11.6 / 13.7, 2 x 128 of 46 16.3 / 17.0, of 186 23.1 /
+// 18.6; its two launches less are 6 us of the host's.
+constexpr int kForkLdsPages = 16384, kForkLdsEntries = 32768;
 
 bool fork_shape_ok(int B_out, int n_pages) { return B_out >= 1 && B_out <= kForkMaxB && n_pages >= 1; }
 

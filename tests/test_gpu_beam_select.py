@@ -125,6 +125,30 @@ def test_beams_that_differ_by_less_than_fp32_resolves():
     assert got["parent"].cpu().tolist() == [[2, 0, 1]]
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,M,V", [(16, 16, 9000), (64, 64, 300), (40, 7, 17000), (4, 64, 8200), (64, 4, 5000)])
+def test_many_beams(dtype, K, M, V):
+    """The bounds of what a beam lists: beams that lead by far, beams alike, finished ones, ones that a grammar leaves
+    one token or none, fewer candidates than new beams."""
+    rng = np.random.default_rng(K + M)
+    x = logits(rng, 6, K, V, dtype).cpu()
+    scores = rng.uniform(-4, 0, (6, K))
+    scores[0, K // 2] += 40.0  # every new beam from one
+    scores[1] = -3.0
+    x[1] = x[1, :1]  # ties between beams
+    x[2, :, 1:] = -np.inf  # one candidate a beam
+    x[3] = -np.inf
+    x[3, :2, 5:8] = 1.0  # six
+    x[4, ::2] = np.nan
+    scores[4, 1::4] = -np.inf
+    x[5] = torch.from_numpy(rng.integers(0, 3, (K, V)).astype(np.float32))
+    scores[5] = np.round(scores[5])
+    done = rng.integers(0, 2, (6, K))
+    check(x.cuda(), scores, M)
+    check(x.cuda(), scores, M, done, 2)
+    check(x.cuda(), scores, M, np.ones((6, K)), 2)
+
+
 def test_same_bits_on_every_call_and_captured():
     lib = need_gpu()
     rng = np.random.default_rng(5)

@@ -102,7 +102,7 @@ def test_absent_pages_empty_sequences_and_lengths_out_of_range():
         run(4, 3, [0, 1, 2, 0, 5, -1], [1, 1, 1, 3, 9, 9], M=3, n_pages=9, table=table, lens=np.array(lens), ref=ref)
 
 
-@pytest.mark.parametrize("B,n_pages,M", [(1, 1, 1), (40, 16384, 300), (40, 16385, 300), (512, 3000, 64), (512, 3000, 65), (300, 5000, 30), (1500, 70000, 40), (4096, 9000, 3)])
+@pytest.mark.parametrize("B,n_pages,M", [(1, 1, 1), (40, 16384, 300), (40, 16385, 300), (256, 3000, 64), (256, 3000, 65), (300, 5000, 30), (1500, 70000, 40), (4096, 9000, 3)])
 def test_large_batches_and_pools(B, n_pages, M):
     rng = np.random.default_rng(B)
     run(B, B, rng.integers(-1, B, B), rng.integers(0, 3, B), P=8, M=M, n_pages=n_pages, L=1, Hkv=1, dh=8)

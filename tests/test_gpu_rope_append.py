@@ -81,7 +81,7 @@ def test_layouts_and_far_positions(dtype, P, heads_first, packed, at):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("N", [1023, 1024, 1025, 1027])
+@pytest.mark.parametrize("N", [1027, 2047, 2048, 2049, 2051])
 def test_several_tokens_per_block(dtype, N):
     run(dtype, 2, 1, 32, 32, [6, 5, 5], False, [N - 7, 9], [N - 7, 7], 32)
 
