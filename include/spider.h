@@ -737,8 +737,8 @@ spider_status spider_rope_append(int N, int H, int Hkv, int dh, int rot, int n_a
 /* ------------------------------------------------------------------------
  * spider_paged_attention - attention of the new tokens over the pages, for grouped
  * heads (query head h reads kv head h / (H / Hkv)): chunks of a prompt, single
- * decoded tokens (one row per sequence), or both in one batch.  For row r at position p, head h
- * and its kv head:
+ * decoded tokens (one row per sequence), or both in one batch.  For row r at
+ * position p, head h and its kv head:
  *   s(j) = scale * q[r,h] . k[j]   over the slots max(0, p - window + 1) <= j <= p
  *          (window 0: all j <= p) whose page is present
  *   out  = sum_j softmax(s)(j) v[j]   (0 where it sees no slot)
@@ -746,7 +746,8 @@ spider_status spider_rope_append(int N, int H, int Hkv, int dh, int rot, int n_a
  * infinite or NaN value of a slot that it sees makes its output infinite or NaN.
  * q element (r,h,c) at q[r*q_stride + h*dh + c]; out [N][H][dh] contiguous in q's
  * dtype, overlapping no input.
- * Precision: products exact, sums, maxima and exponentials fp32, out rounded once.
+ * Precision: products exact, sums, maxima and exponentials fp32, out rounded once
+ * (scores s of magnitude below 2^29; a row with larger ones may become NaN).
  * bf16: the softmax numerators enter the product with v rounded to bf16 once, and
  * the sum that divides them is that of the rounded ones.
  * Requires H % Hkv == 0, H <= 65535, N * H < 2^24, B * Hkv < 2^22, q and out 16-byte
@@ -823,9 +824,9 @@ spider_status spider_pages_fork(int L, int Hkv, int dh, spider_dtype dtype, void
  * must be NULL).  scores_out fp32, parent_out, token_out, done_out int32
  * [B][n_out].  history int32 [B*K] rows of history_cap entries at history_stride,
  * history_out [B*n_out] at history_out_stride; n_history [B*K], n_history_out
- * [B*n_out].  All on the device; outputs overlap no input.
- * Precision: exponentials within 2^-23 relative, their sum, the logarithm and the candidates in
- * fp64; scores_out rounded once.
+ * [B*n_out].  All on the device; outputs overlap neither inputs nor each other.
+ * Precision: exponentials within 2^-23 relative, their sum, the logarithm and the
+ * candidates in fp64; scores_out rounded once.
  * Limits: K, n_out <= 64, V <= 2^19, B*K and B*n_out <= 65535, history_cap <= 2^24.
  * Workspace: spider_beam_select_workspace_size(B, K, n_out, V) bytes, 256-byte
  * aligned.

@@ -455,18 +455,25 @@ extern "C" spider_status spider_beam_select(int B, int K, int n_out, int V, cons
                  "spider_beam_select: history, n_history, history_out and n_history_out go together, with a capacity");
   SPIDER_REQUIRE(!any || (history_cap <= (1 << 24) && (B * K == 1 || history_stride >= history_cap) && (B * n_out == 1 || history_out_stride >= history_cap)),
                  SPIDER_ERR_SHAPE, "spider_beam_select: history strides of at least the capacity, which is at most 2^24");
-  // (every row of a sample reads what another one's block would write)
-  const auto apart = [](const void* p, size_t n, const void* q, size_t m) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
-    return !p || !q || x + n <= y || y + m <= x;
-  };
+  // (a sample's block reads while another one's writes)
   const size_t in = (size_t)B * K * 4, out = (size_t)B * n_out * 4;
-  for (const void* p : {(const void*)scores_out, (const void*)parent_out, (const void*)token_out, (const void*)done_out, (const void*)n_history_out})
-    SPIDER_REQUIRE(apart(p, out, scores, in) && apart(p, out, done, in) && apart(p, out, n_history, in), SPIDER_ERR_INVALID_ARG,
-                   "spider_beam_select: outputs must not overlap inputs");
+  const size_t logits_n = ((size_t)(B * K - 1) * (B * K == 1 ? 0 : logits_stride) + V) * (dtype == SPIDER_BF16 ? 2 : 4);
   const size_t h_in = any ? ((size_t)(B * K - 1) * (B * K == 1 ? 0 : history_stride) + history_cap) * 4 : 0;
   const size_t h_out = any ? ((size_t)(B * n_out - 1) * (B * n_out == 1 ? 0 : history_out_stride) + history_cap) * 4 : 0;
-  SPIDER_REQUIRE(apart(history_out, h_out, history, h_in), SPIDER_ERR_INVALID_ARG, "spider_beam_select: outputs must not overlap inputs");
+  struct Span {
+    const void* p;
+    size_t n;
+  };
+  const Span ins[5] = {{logits, logits_n}, {scores, in}, {done, in}, {n_history, in}, {history, h_in}};
+  const Span outs[6] = {{scores_out, out}, {parent_out, out}, {token_out, out}, {done_out, out}, {n_history_out, out}, {history_out, h_out}};
+  const auto apart = [](const Span& x, const Span& y) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(x.p), q = reinterpret_cast<uintptr_t>(y.p);
+    return !x.p || !y.p || p + x.n <= q || q + y.n <= p;
+  };
+  for (int o = 0; o < 6; ++o) {
+    for (int i = 0; i < 5; ++i) SPIDER_REQUIRE(apart(outs[o], ins[i]), SPIDER_ERR_INVALID_ARG, "spider_beam_select: outputs must not overlap inputs");
+    for (int i = 0; i < o; ++i) SPIDER_REQUIRE(apart(outs[o], outs[i]), SPIDER_ERR_INVALID_ARG, "spider_beam_select: outputs must not overlap each other");
+  }
   const size_t need = beam_layout(B, K, n_out, V, nullptr, nullptr);
   SPIDER_REQUIRE(workspace && workspace_bytes >= need, SPIDER_ERR_WORKSPACE, "spider_beam_select: workspace of %zu bytes needed, %zu given", need,
                  workspace ? workspace_bytes : 0);

@@ -149,6 +149,11 @@ def test_many_beams(dtype, K, M, V):
     check(x.cuda(), scores, M, np.ones((6, K)), 2)
 
 
+def test_the_largest():
+    rng = np.random.default_rng(6)
+    check(logits(rng, 1, 64, 524288), rng.uniform(-4, 0, (1, 64)), 64)
+
+
 def test_same_bits_on_every_call_and_captured():
     lib = need_gpu()
     rng = np.random.default_rng(5)

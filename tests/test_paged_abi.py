@@ -144,6 +144,8 @@ BEAM = dict(B=2, K=3, M=4, V=100, x=P, xs=100, dt=0, scores=2 * P, done=3 * P, e
     (dict(eos=-1), INVALID), (dict(x=P + 2), INVALID), (dict(cap=0), INVALID), (dict(hs=49), SHAPE), (dict(hos=49), SHAPE), (dict(cap=(1 << 24) + 1, hs=1 << 25, hos=1 << 25), SHAPE),
     (dict(ws=None), WORKSPACE), (dict(wsb=100), WORKSPACE), (dict(ws=12 * P + 8), INVALID), (dict(s_out=2 * P), INVALID), (dict(d_out=3 * P + 20), INVALID),
     (dict(nh_out=9 * P), INVALID), (dict(h_out=8 * P), INVALID), (dict(h_out=8 * P + 4 * 299), INVALID),
+    (dict(s_out=P + 4 * 599), INVALID), (dict(t_out=8 * P + 4 * 290), INVALID), (dict(t_out=5 * P + 28), INVALID), (dict(h_out=7 * P - 4), INVALID),
+    (dict(h_out=3 * P), INVALID), (dict(nh_out=4 * P - 28), INVALID),
 ])
 def test_beam_select_refusals(L, change, status):
     a = dict(BEAM)
