@@ -227,6 +227,29 @@ def test_scales(dtype, scale):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+@pytest.mark.parametrize("news", [1, 40, 240])
+def test_the_largest_scores(dtype, scale, news):
+    """Scores of 2^20 to 2^28, 2^20 apart: every weight but the largest is 0 (e^-2^20), so the output is the value of
+    that slot: one product, one division and its own rounding off."""
+    lib = need_gpu()
+    n, H, dh = 250, 4, 128
+    q, kp, vp, table, cu = case(news, H, 2, dh, 16, [n], [news], dtype)
+    order = np.random.default_rng(news).permutation(n) + 1.0
+    q[:, :, 0] = 2.0 ** 20
+    kp.zero_()
+    v, first = f64(vp), n - news
+    for j in range(n):
+        kp[int(table[0, j // 16]), j % 16, :, 0] = float(order[j])
+    got = f64(lib.paged_attention(q, kp, vp, ints(table), ints([n]), ints(cu), scale=scale))
+    for r in range(news):
+        seen = order[:first + r + 1]
+        j = int(seen.argmax() if scale > 0 else seen.argmin())
+        want = np.repeat(v[int(table[0, j // 16]), j % 16], H // 2, axis=0)
+        assert (np.abs(got[r] - want) <= (HALF_STEP[dtype] + 2.0 ** -22) * np.abs(want)).all(), r
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_equal_scores_of_a_long_row(dtype):
     """All weights alike, far more of them than the mantissa of the sum's type has steps."""
     lib = need_gpu()
