@@ -5,8 +5,8 @@
 // window, whose page is present.
 //
 // The rows of a kv head (tokens x heads of its group) read the same keys and values.  Few rows are
-// bound by those reads (paged_few_kernel), many by the softmax and the products
-// (paged_chunk_kernel); splits of the keys meet in paged_join_kernel.  The softmax numerators
+// bound by those reads (few_block), many by the softmax and the products (paged_chunk_kernel);
+// splits of the keys meet in paged_join_kernel.  The softmax numerators
 // enter the product with v in v's type, rounded once, and their sum is that of the rounded ones:
 // in bf16 an output is then about 1.3 times as far from the exact one as its own rounding makes it.
 #include <algorithm>
@@ -70,16 +70,17 @@ __device__ __forceinline__ void chunk_tiles(const ChunkArgs& a, const ChunkLaunc
 // later rows of a sequence, which see more, come first.  Blocks of a (kv head, split) lie on one
 // XCD, whose L2 then holds its keys and values, where their number is a multiple of the 8 XCDs.
 template <int KEYS, int ROWS, bool FEW>
-__device__ __forceinline__ bool chunk_work(const ChunkArgs& a, const ChunkLaunch& l, ChunkWork& w) {
+__device__ __forceinline__ bool chunk_work(const ChunkArgs& a, const ChunkLaunch& l, int block, ChunkWork& w) {
   const int units = a.Hkv * l.splits, G = a.H / a.Hkv;
+  if (block >= units * l.row_blocks) return false;
   int unit, rb;
   if (units % 8 == 0) {
-    const int slot = blockIdx.x >> 3;
-    unit = slot / l.row_blocks * 8 + (blockIdx.x & 7);
+    const int slot = block >> 3;
+    unit = slot / l.row_blocks * 8 + (block & 7);
     rb = slot % l.row_blocks;
   } else {
-    unit = blockIdx.x % units;
-    rb = blockIdx.x / units;
+    unit = block % units;
+    rb = block / units;
   }
   w.hk = unit % a.Hkv;
   w.split = unit / a.Hkv;
@@ -315,21 +316,27 @@ __device__ __forceinline__ float seen_nonfinite(const ChunkArgs& a, int b, const
   return sum;
 }
 
-// Few rows: bound by the reads of keys and values, which go straight from memory to the registers
-// of the wave that uses them, the next tile's keys on their way during the softmax.  Each of the
-// 4 waves takes a run of the block's tiles; their sums meet in LDS.
-template <typename AT, int DH, int RT, bool FULL>
-__global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(ChunkArgs a, ChunkLaunch l) {
+// A block of few rows: bound by the reads of keys and values, which go straight from memory to the
+// registers of the wave that uses them, the next tile's keys on their way during the softmax.
+// Each of the NW waves takes a run of the block's tiles; their sums meet in LDS.  16 tokens of 32
+// heads over 8 x 32768 slots: 374 us with the join's 6, 5.7 TB/s.
+template <int DH, int RT, int NW>
+struct FewShared {
+  float m[NW][16 * RT], l[NW][16 * RT], o[NW][16 * RT][DH + 4];
+};
+template <typename AT, int DH, int RT, int NW, bool FULL>
+__device__ __forceinline__ void few_block(const ChunkArgs& a, const ChunkLaunch& l, int block, FewShared<DH, RT, NW>& x_) {
   using Rows = ChunkRows<AT, DH, RT>;
   using T = typename Rows::T;
   constexpr int KEYS = T::KEYS, CPL = T::CPL;
-  constexpr int ROWS = 16 * RT, LD = DH + 4;
-  __shared__ float xm[4][ROWS], xl[4][ROWS];
-  __shared__ float xo[4][ROWS][LD];
+  constexpr int ROWS = 16 * RT;
+  auto& xm = x_.m;
+  auto& xl = x_.l;
+  auto& xo = x_.o;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, g = lane >> 4;
   ChunkWork w;
-  if (!chunk_work<KEYS, ROWS, true>(a, l, w)) return;
+  if (!chunk_work<KEYS, ROWS, true>(a, l, block, w)) return;
   const AT* kb = reinterpret_cast<const AT*>(a.k) + w.hk * a.p.sh;
   const AT* vb = reinterpret_cast<const AT*>(a.v) + w.hk * a.p.sh;
   const float sc = fabsf(a.scale) * 1.4426950408889634f;
@@ -344,7 +351,7 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
 #pragma unroll
     for (int t = 0; t < T::KT; ++t) T::template load_k_row<FULL>(k, t, kb + (m < 8 ? off[2 * t] : off[2 * t + 1]) + k_at, g, a.dh);
   };
-  const int each = (w.t1 - w.t0 + 3) / 4, end = min(w.t1, w.t0 + (wave + 1) * each);
+  const int each = (w.t1 - w.t0 + NW - 1) / NW, end = min(w.t1, w.t0 + (wave + 1) * each);
   int t = w.t0 + wave * each;
   int64_t off[KEYS / 8] = {};  // of the tile's groups of eight keys
   uint32_t present = 0;
@@ -405,14 +412,14 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
     }
   }
   __syncthreads();
-  constexpr int PER = 256 / ROWS;  // threads of a row
+  constexpr int PER = 64 * NW / ROWS;  // threads of a row
   const int c0 = 4 * (tid % PER), row = tid / PER;
   if (row >= w.R - w.r0) return;
-  float mx = -INFINITY, sum = 0.f, f[4];
+  float mx = -INFINITY, sum = 0.f, f[NW];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) mx = fmaxf(mx, xm[u][row]);
+  for (int u = 0; u < NW; ++u) mx = fmaxf(mx, xm[u][row]);
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
+  for (int u = 0; u < NW; ++u) {
     f[u] = xm[u][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm[u][row] - mx) * sc);
     // (a row whose scores are all NaN has no maximum, but its sum is NaN and stays)
     sum += xm[u][row] == -INFINITY ? xl[u][row] : xl[u][row] * f[u];
@@ -422,12 +429,18 @@ __global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(C
   for (int c = c0; c < a.dh; c += 4 * PER) {
     floatx4 x = floatx4{};
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < NW; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] += rescaled(xo[u][row][c + i], f[u]);
     if (w.ns > 1) *reinterpret_cast<floatx4*>(l.part_o + part_row * a.dh + c) = x;
     else attn_store<AT>(a.out, out_row * a.dh + c, x, sum);
   }
+}
+
+template <typename AT, int DH, int RT, bool FULL>
+__global__ void __launch_bounds__(256, DH* RT <= 128 ? 3 : 1) paged_few_kernel(ChunkArgs a, ChunkLaunch l) {
+  __shared__ FewShared<DH, RT, 4> x;
+  few_block<AT, DH, RT, 4, FULL>(a, l, blockIdx.x, x);
 }
 
 // 16-byte piece c of key j of a tile lies at piece c ^ swizzle(j).  16 lanes read one piece of 16
@@ -438,7 +451,8 @@ __device__ __forceinline__ int swizzle(int j) {
   return DH == 64 ? (((j & 2) << 1) | ((j & 4) >> 1) | ((j & 8) >> 3)) : (((j & 3) << 2) | ((j & 4) >> 1) | ((j & 8) >> 3));
 }
 
-// Many rows (bf16): NW waves of 32 rows each share the keys and values, which come through LDS by
+// Many rows (bf16), bound by the matrix and vector units in turn: 4096 tokens of 32 heads over
+// 8 x 32768 slots 1.98 ms, 1.04 PFLOP/s.  NW waves of 32 rows each share the keys and values, which come through LDS by
 // DMA.  A wave computes S^T = K Q^T and O^T += V^T P^T with 32x32x16 MFMAs on KT * 32 keys at a
 // time, so a lane owns row lane % 32 in both, with half h = lane / 32 of the keys: register r of a
 // product holds key (channel) r % 4 + 8 (r / 4) + 4 h.  Eight such registers are the operand of a
@@ -448,18 +462,26 @@ __device__ __forceinline__ int swizzle(int j) {
 // keep at 2^-23.  (On the matrix unit of 16 rows, which takes as long, a NaN weight would reach
 // the sum of the row 16 on: 0 times NaN.)
 template <int DH, int NW, bool FULL>
-__global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l) {
+__global__ void __launch_bounds__(64 * NW, DH == 256 ? 1 : 2) paged_chunk_kernel(ChunkArgs a, ChunkLaunch l, ChunkLaunch few) {
   constexpr int KT = DH == 256 || NW == 2 ? 1 : 2, KEYS = 32 * KT, NK = DH / 16, CT = DH / 32, ROWS = 32 * NW;
   constexpr int PIECES = DH / 8, KPD = 64 / PIECES;           // 16-byte pieces of a row, keys of a DMA
   constexpr int TILE = KEYS * DH;                              // elements of a key or value tile
   constexpr int AHEAD = KT == 2 && NW < 8 ? 1 : 2;             // tiles on their way during the products
   constexpr int KD = TILE / 512 / NW, DMAS = 2 * KD;           // DMAs of a wave and tile
   static_assert(KD >= 1, "every wave fetches");
-  __shared__ __align__(16) uint16_t buf[AHEAD + 1][2][TILE];
+  typedef uint16_t Stage[2][TILE];
+  __shared__ __align__(16) char lds[(AHEAD + 1) * sizeof(Stage)];
+  static_assert(sizeof(FewShared<DH, 1, NW>) <= sizeof(lds), "the blocks of few rows share it");
+  Stage* buf = reinterpret_cast<Stage*>(lds);
+  const int few0 = (a.Hkv * l.splits * l.row_blocks + 7) & ~7;  // (the others' order on the XCDs)
+  if ((int)blockIdx.x >= few0) {
+    few_block<uint16_t, DH, 1, NW, FULL>(a, few, blockIdx.x - few0, *reinterpret_cast<FewShared<DH, 1, NW>*>(lds));
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5, m = lane & 15;
   ChunkWork w;
-  if (!chunk_work<KEYS, ROWS, false>(a, l, w)) return;
+  if (!chunk_work<KEYS, ROWS, false>(a, l, blockIdx.x, w)) return;
   const uint16_t* kb = reinterpret_cast<const uint16_t*>(a.k) + w.hk * a.p.sh;
   const uint16_t* vb = reinterpret_cast<const uint16_t*>(a.v) + w.hk * a.p.sh;
   // (with scale 0 the smallest number that leaves -inf, a score that is not seen, what it is)
@@ -749,11 +771,14 @@ __global__ void __launch_bounds__(256) paged_join_kernel(ChunkArgs a, ChunkLaunc
   if (grp == 0) attn_store<AT>(a.out, r * a.dh + c, y, total);
 }
 
-// The launches of a call, and its workspace.  The few-row kernel serves 16 or 32 rows of a
-// sequence and kv head per block, the other one (bf16) up to 256.  How many rows a sequence has is
-// known on the device only: a batch whose average is within 32 rows goes to the first kernel,
-// whatever its sequences are, one sequence to the other; else both are launched, and the
-// sequences of up to 16 rows are the first one's.
+// The launches of a call, and its workspace.  How many rows a sequence has is known on the device
+// only: a batch whose average is within 32 rows goes to paged_few_kernel, whatever its sequences
+// are, one sequence to paged_chunk_kernel (bf16; blocks of up to 256 rows).  In other batches the
+// sequences of up to 16 rows go to blocks of few rows behind the others, which fill the CUs as
+// those end.  Measured against a launch of their own, us: a prompt of 705 and 15 single tokens over
+// 8192 slots of 8 kv heads 278 / 288, 8 and 8 913 / 910, 1 of 2944 and 7 of 32 kv heads 187 / 269; taking
+// turns with the others' instead 271, 1025 and 190, and where a long chunk then has to wait (512 and 1
+// over 32768) 526 / 343.
 struct ChunkPlan {
   int dhp;  // kernel width: 64, 128 or 256
   int rt;   // row tiles of a wave of paged_few_kernel, or 0: not launched
@@ -762,11 +787,11 @@ struct ChunkPlan {
   ChunkLaunch few, chunk;
   size_t few_ml, few_o, chunk_ml, chunk_o, bytes;
 };
-// Tiles of a split of few rows.  Measured with 4 / 8 / 16, us on the device: one row of 32 heads
-// over 705 slots 10.6 / 12.1 / 11.5, over 2944 17.9 / 18.2 / 17.2, 4 of them over 705 16.0 / 15.5 /
+// Tiles of a split of few rows, per wave.  Measured with 1 / 2 / 4, us on the device: one row of 32
+// heads over 705 slots 10.6 / 12.1 / 11.5, over 2944 17.9 / 18.2 / 17.2, 4 of them over 705 16.0 / 15.5 /
 // 13.6; one of 8 x 4 heads over 2000 11.2 / 12.2 / 14.6, 32 of them over 705 21.1 / 23.0 / 21.8;
 // fp32, 70 of 2 x 3 heads in a window of 300 13.7 / 15.3 / 15.6, 13 of 8 over 1500 12.6 / 11.3 / 13.1.
-constexpr int kFewTiles = 4;
+constexpr int kFewTiles = 1;
 
 // slots: of the longest sequence, window (0: none): what a row sees of them.
 ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window, spider_dtype dtype) {
@@ -777,8 +802,8 @@ ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window
   const int keys = bf16 ? 32 : 16;
   // slots that the longest sequence's row blocks, of up to 256 rows, see
   const int64_t reach = window > 0 ? std::min<int64_t>(slots, (int64_t)window + std::min<int64_t>(N, ceil_div(256, (int)G) + 1) + keys) : slots;
-  const auto few_splits = [&](int64_t blocks) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>((reach + keys - 1) / keys / kFewTiles, 768 / blocks));
+  const auto few_splits = [&](int64_t blocks, int waves) {  // of blocks of so many waves
+    return (int)std::max<int64_t>(1, std::min<int64_t>((reach + keys - 1) / keys / (waves * kFewTiles), 3072 / waves / blocks));
   };
   size_t off = 0;
   const auto parts = [&](ChunkLaunch& l, size_t rows, size_t* ml, size_t* o) {
@@ -791,20 +816,19 @@ ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window
     p.rt = R <= (int64_t)B * 16 || p.dhp == 256 ? 1 : 2;
     p.limit = 0x7fffffff;
     const int rows = 16 * p.rt, blocks = (int)(R / rows);
-    p.few = ChunkLaunch{nullptr, nullptr, keys, rows, blocks + B, few_splits(Hkv * std::max<int64_t>(B, blocks)), kFewTiles, 0};
+    p.few = ChunkLaunch{nullptr, nullptr, keys, rows, blocks + B, few_splits(Hkv * std::max<int64_t>(B, blocks), 4), 4 * kFewTiles, 0};
     parts(p.few, (size_t)N * H, &p.few_ml, &p.few_o);
     p.bytes = off;
     return p;
   }
   p.limit = -1;
-  if (B > 1) {
-    p.rt = 1;
-    p.limit = 16;
-    p.few = ChunkLaunch{nullptr, nullptr, keys, 16, B, few_splits((int64_t)Hkv * B), kFewTiles, 1};
-    parts(p.few, (size_t)B * Hkv * 16, &p.few_ml, &p.few_o);
-  }
   // (width 256 has registers for one wave per SIMD)
   p.nw = R <= (int64_t)B * 64 ? 2 : (R <= (int64_t)B * 128 || p.dhp == 256 ? 4 : 8);
+  if (B > 1) {
+    p.limit = 16;
+    p.few = ChunkLaunch{nullptr, nullptr, keys, 16, B, few_splits((int64_t)Hkv * B, p.nw), p.nw * kFewTiles, 1};
+    parts(p.few, (size_t)B * Hkv * 16, &p.few_ml, &p.few_o);
+  }
   const int rows = 32 * p.nw, at_once = p.dhp == 256 ? 256 : 256 * 8 / p.nw;  // blocks that run at once
   const int64_t blocks = Hkv * std::max<int64_t>(1, R / rows);
   const int chunk_keys = p.dhp == 256 || p.nw == 2 ? 32 : 64;
@@ -845,19 +869,20 @@ void launch_few(const ChunkArgs& a, const ChunkLaunch& l, hipStream_t st) {
 }
 
 template <int DH, int NW>
-void launch_chunk(const ChunkArgs& a, const ChunkLaunch& l, hipStream_t st) {
-  if (a.dh == DH) paged_chunk_kernel<DH, NW, true><<<chunk_blocks(a, l), 64 * NW, 0, st>>>(a, l);
-  else paged_chunk_kernel<DH, NW, false><<<chunk_blocks(a, l), 64 * NW, 0, st>>>(a, l);
+void launch_chunk(const ChunkArgs& a, const ChunkLaunch& l, const ChunkLaunch& few, hipStream_t st) {
+  const unsigned blocks = (chunk_blocks(a, l) + 7) / 8 * 8 + chunk_blocks(a, few);
+  if (a.dh == DH) paged_chunk_kernel<DH, NW, true><<<blocks, 64 * NW, 0, st>>>(a, l, few);
+  else paged_chunk_kernel<DH, NW, false><<<blocks, 64 * NW, 0, st>>>(a, l, few);
 }
 
 template <typename AT, int DH>
 spider_status run_chunk(const ChunkArgs& a, const ChunkPlan& p, hipStream_t st) {
   ProfScope ps(KC_PAGED_ATTN, st);
   if constexpr (sizeof(AT) == 2) {
-    if (p.nw == 2) launch_chunk<DH, 2>(a, p.chunk, st);
-    if (p.nw == 4) launch_chunk<DH, 4>(a, p.chunk, st);
+    if (p.nw == 2) launch_chunk<DH, 2>(a, p.chunk, p.few, st);
+    if (p.nw == 4) launch_chunk<DH, 4>(a, p.chunk, p.few, st);
     if constexpr (DH <= 128)
-      if (p.nw == 8) launch_chunk<DH, 8>(a, p.chunk, st);
+      if (p.nw == 8) launch_chunk<DH, 8>(a, p.chunk, p.few, st);
   }
   if (p.rt == 1) launch_few<AT, DH, 1>(a, p.few, st);
   if constexpr (DH <= 128)
