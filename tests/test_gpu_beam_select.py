@@ -103,6 +103,15 @@ def test_finished_beams_and_histories(dtype):
     check(x, scores, 5, None, -1, history, n)
 
 
+@pytest.mark.parametrize("M,cap", [(1, 32768), (1, 32769), (4, 8192), (4, 9001), (64, 700)])
+def test_long_histories(M, cap):
+    rng = np.random.default_rng(cap)
+    B, K, V = 2, 3, 500
+    history = rng.integers(0, V, (B * K, cap)).astype(np.int32)
+    n = np.array([0, cap - 1, cap, 17, cap // 2, 1])
+    check(logits(rng, B, K, V), rng.uniform(-2, 0, (B, K)), M, rng.integers(0, 2, (B, K)), 4, history, n)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strided_rows(dtype):
     """Rows of odd width and start within a wider matrix (read one by one), and rows at a distance."""

@@ -226,6 +226,17 @@ def test_scales(dtype, scale):
     check(out, q, kp, vp, table, lens, cu, dtype, scale=scale)
 
 
+@pytest.mark.parametrize("dh", [24, 80, 120, 200])
+@pytest.mark.parametrize("T", [40, 100, 200])
+def test_chunks_narrower_than_the_kernel(dh, T):
+    """One sequence, and one among others of a few tokens (G = 2 rows per token: blocks of 64 to 256 rows)."""
+    lib = need_gpu()
+    for lens, news in (([T + 150], [T]), ([T + 33, 900, T, 70], [T, 2, T, 8])):
+        q, kp, vp, table, cu = case(dh + T, 4, 2, dh, 16, lens, news, "bf16")
+        out = lib.paged_attention(q, kp, vp, ints(table), ints(lens), ints(cu))
+        check(out, q, kp, vp, table, lens, cu, "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale", [1.0, -1.0])
 @pytest.mark.parametrize("news", [1, 40, 240])
