@@ -30,10 +30,10 @@ struct ChunkArgs {
   int64_t qs;
   int H, Hkv, dh, window;
   float scale;
-  int limit;  // sequences of up to this many rows per kv head are the few-row kernel's, the others the other's
+  int limit;  // sequences of up to this many rows per kv head go to blocks of few rows
 };
 
-// A launch of one of the two kernels.
+// The blocks of few rows, or the others, of a call.
 struct ChunkLaunch {
   float2* part_ml;  // [rows][splits] (largest raw score, sum) of a split
   float* part_o;    // .. [dh] its unscaled output
@@ -802,8 +802,9 @@ ChunkPlan chunk_plan(int N, int B, int H, int Hkv, int dh, int slots, int window
   const int keys = bf16 ? 32 : 16;
   // slots that the longest sequence's row blocks, of up to 256 rows, see
   const int64_t reach = window > 0 ? std::min<int64_t>(slots, (int64_t)window + std::min<int64_t>(N, ceil_div(256, (int)G) + 1) + keys) : slots;
-  const auto few_splits = [&](int64_t blocks, int waves) {  // of blocks of so many waves
-    return (int)std::max<int64_t>(1, std::min<int64_t>((reach + keys - 1) / keys / (waves * kFewTiles), 3072 / waves / blocks));
+  // of blocks of so many waves: twelve waves per CU
+  const auto few_splits = [&](int64_t blocks, int waves) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>((reach + keys - 1) / keys / (waves * kFewTiles), 12 * 256 / waves / blocks));
   };
   size_t off = 0;
   const auto parts = [&](ChunkLaunch& l, size_t rows, size_t* ml, size_t* o) {
