@@ -226,6 +226,31 @@ def test_scales(dtype, scale):
     check(out, q, kp, vp, table, lens, cu, dtype, scale=scale)
 
 
+@pytest.mark.parametrize("dh", [64, 128, 256])
+@pytest.mark.parametrize("T", [130, 400, 800])
+def test_few_rows_among_chunks(dh, T):
+    """Single tokens, some tokens, none and a chunk in one batch, over pages whose free slots hold anything: equal
+    bits with NaN and infinities there."""
+    lib = need_gpu()
+    lens, news = [1000, 33, T + 40, 500, 77, 1, 2100], [1, 4, T, 0, 17, 1, 8]
+    q, kp, vp, table, cu = case(dh + T, 4, 2, dh, 16, lens, news, "bf16", packed=True)
+    out = lib.paged_attention(q, kp, vp, ints(table), ints(lens), ints(cu))
+    check(out, q, kp, vp, table, lens, cu, "bf16")
+    free = np.ones((kp.shape[0], 16), bool)
+    for b, n in enumerate(lens):
+        for j in range(n):
+            free[table[b, j // 16], j % 16] = False
+    free = torch.from_numpy(free).cuda()
+    for bad in (float("nan"), float("inf")):
+        kp[free] = bad
+        vp[free] = -bad
+        assert torch.equal(lib.paged_attention(q, kp, vp, ints(table), ints(lens), ints(cu)), out)
+        window = lib.paged_attention(q, kp, vp, ints(table), ints(lens), ints(cu), window=90)
+        kp[free] = 0.0
+        vp[free] = 0.0
+        check(window, q, kp, vp, table, lens, cu, "bf16", 90)
+
+
 @pytest.mark.parametrize("dh", [24, 80, 120, 200])
 @pytest.mark.parametrize("T", [40, 100, 200])
 def test_chunks_narrower_than_the_kernel(dh, T):
